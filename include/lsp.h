@@ -395,6 +395,102 @@ int32_t lsp_commit_step(const lsp_commit_desc *desc, const float *margin, const 
                         int32_t *step_counts, void *stream);
 
 /* ------------------------------------------------------------------------- *
+ * What a step says about its tokens: for every sequence b and active row
+ * i < N_b, over the row z = logits[b,i,:] with log p(v) = z[v] - log sum_u exp(z[u]):
+ *     logprob[b,i]          = log p(token_id[b,i]); -inf for an id outside [0,V)
+ *     entropy[b,i]          = - sum_v p(v) log p(v), in nats
+ *     alt_id[b,i,0..K)      = the K likeliest entries, in descending order; equal
+ *                             logits: the lower id first
+ *     alt_logprob[b,i,0..K) = log p of each
+ * in fp32 throughout.  Rows i >= N_b are neither read nor written.  -inf entries
+ * have probability 0 (as do those of the type's lowest value beside ordinary ones); a row of nothing but -inf
+ * gives -inf everywhere and entropy 0.  Where V < K the list ends with id -1 and
+ * -inf.  Precondition: no NaN and no +inf in the row.
+ * ------------------------------------------------------------------------- */
+/* Bytes of a workspace with which few long rows are shared by several workgroups each; 0 where it is of no use. */
+size_t lsp_token_scores_workspace_bytes(int32_t B, int32_t S, int32_t V, int32_t num_alt);
+
+/*
+ * logits, row_stride, batch_stride, suffix_len: as for lsp_confidence (any alignment of
+ * at least the element size; suffix_len NULL = all S rows active).  token_id: device
+ * int32 [B,S]; it and logprob (fp32 [B,S]) are given together, or both NULL.  entropy:
+ * device fp32 [B,S].  num_alt = K: 0..32; alt_id (int32), alt_logprob (fp32): device
+ * [B,S,K], NULL where K = 0.  workspace: device, 16-byte aligned, of any content, for this
+ * call alone until it has run; with NULL or fewer bytes than
+ * lsp_token_scores_workspace_bytes a row is one workgroup's.
+ */
+int32_t lsp_token_scores(int32_t dtype, const void *logits, int32_t B, int32_t S, int32_t V, int64_t row_stride,
+                         int64_t batch_stride, const int32_t *suffix_len, const int32_t *token_id, int32_t num_alt,
+                         float *logprob, float *entropy, int32_t *alt_id, float *alt_logprob, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- *
+ * The attention mass that the keys of a step received, accumulated over steps: the
+ * weight by which lsp_kv_evict chooses the rows that stay.  With p[h,i,t] the
+ * soft-max of lsp_attn_step over its P_b + N_b keys, per layer, sequence b and KV head g
+ *     mass[t] = sum over the query heads h of g and the active rows i < N_b of p[h,i,t]
+ *     weights[b,g,t] = decay * weights[b,g,t] + mass[t]    cached rows, t < P_b
+ *     weights[b,g,t] = mass[t]          suffix row t - P_b, P_b <= t < min(P_b + N_b, C)
+ * (a suffix row that is committed becomes cache row t, with the mass it received in
+ * that step to begin with).  The rest of weights is neither read nor written, nothing
+ * of sequences with N_b = 0 is; with decay = 0 nothing is read.  fp32 sums in an order
+ * of the kernel's own, the same at every call.
+ * ------------------------------------------------------------------------- */
+size_t lsp_attn_key_weights_workspace_bytes(const lsp_attn_desc *desc, int32_t num_layers);
+
+/*
+ * desc and q_layers, k_suf_layers, k_cache_layers, prefix_len, suffix_len: as for
+ * lsp_attn_step_layers (o_stride is not used; V is not needed).  decay: 0 to 1.
+ * weights: device fp32 [num_layers, B, Hkv, C], dense.  workspace: device, 16-byte
+ * aligned, lsp_attn_key_weights_workspace_bytes(desc, num_layers) bytes of any
+ * content, for this call alone until it has run.  Limit: B * Hq <= 65535.
+ */
+int32_t lsp_attn_key_weights(const lsp_attn_desc *desc, int32_t num_layers, const void *const *q_layers,
+                             const void *const *k_suf_layers, const void *const *k_cache_layers,
+                             const int32_t *prefix_len, const int32_t *suffix_len, float decay, float *weights,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- *
+ * Eviction from a cache by accumulated attention weight.  Every sequence b with
+ * P_b > high rows is cut back to `keep` rows, for each layer and KV head g by itself:
+ *   rows t < first and t >= P_b - recent stay; of the others those of the largest
+ *   weights[b,g,t] (equal weights: the lower row; NaN below everything), `keep` rows in all.
+ *   Rows below `keep` that stay do not move.  Rows from `keep` on that stay take, in
+ *   ascending order, the places below `keep` that have become free, in ascending order.
+ * The order of cached rows has no meaning to lsp_attn_step (keys carry their positions,
+ * there is no mask); rows appended since the last eviction are behind all others.  Per row
+ * j < min(P_b, keep) kept_index[b,g,j] = the row that is at j now, else -1;
+ * new_weights[b,g,j] = its weight; new_len[b] = keep.  Sequences with
+ * P_b <= high keep their rows, weights and length.  Rows and weights from new_len[b]
+ * on are left as they are.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t kv_dtype;       /* lsp_dtype of the caches */
+  int32_t B, Hkv, D, C;   /* cache [B, C, Hkv, D]; the bytes of D elements must be a multiple of 16 */
+  int32_t num_layers;
+  int32_t keep;           /* 1..C */
+  int32_t high;           /* >= keep: only sequences with more rows than this are cut */
+  int32_t first, recent;  /* rows that stay whatever their weight; first + recent <= keep */
+  int64_t cache_batch_stride; /* elements between sequences; 0 = C*Hkv*D */
+} lsp_evict_desc;
+
+size_t lsp_kv_evict_workspace_bytes(const lsp_evict_desc *desc);
+
+/*
+ * weights: device fp32 [num_layers, B, Hkv, C].  prefix_len: device int32[B], clamped to
+ * 0..C.  k_cache_layers, v_cache_layers: HOST arrays of num_layers DEVICE pointers,
+ * 16-byte aligned; rows move inside these buffers.  new_weights: device, shape of weights,
+ * may be weights itself.  new_len: device int32[B], may be prefix_len itself.
+ * kept_index: device int32 [num_layers, B, Hkv, keep], or NULL.  workspace: device,
+ * 16-byte aligned, lsp_kv_evict_workspace_bytes(desc) bytes of any content, for this call
+ * alone until it has run.  Limits: B, Hkv <= 65535.
+ */
+int32_t lsp_kv_evict(const lsp_evict_desc *desc, const float *weights, const int32_t *prefix_len,
+                     void *const *k_cache_layers, void *const *v_cache_layers, float *new_weights,
+                     int32_t *new_len, int32_t *kept_index, void *workspace, size_t workspace_bytes,
+                     void *stream);
+
+/* ------------------------------------------------------------------------- *
  * Measurement helper (used by the benchmark, not part of the scheduler step):
  * a bare streaming read of `bytes` bytes of device memory by `workgroups`
  * workgroups of 512 threads (16-byte non-temporal loads, each workgroup one

@@ -52,11 +52,19 @@ class CommitDesc(ctypes.Structure):
                 ("alpha", ctypes.c_float), ("beta", ctypes.c_float), ("max_commit", ctypes.c_int32)]
 
 
+class EvictDesc(ctypes.Structure):
+    _fields_ = [("kv_dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("C", ctypes.c_int32), ("num_layers", ctypes.c_int32), ("keep", ctypes.c_int32), ("high", ctypes.c_int32),
+                ("first", ctypes.c_int32), ("recent", ctypes.c_int32), ("cache_batch_stride", ctypes.c_int64)]
+
+
 EXPORTS = ["lsp_version", "lsp_last_error", "lsp_attn_workspace_bytes", "lsp_attn_step", "lsp_attn_step_layers",
            "lsp_confidence_workspace_bytes", "lsp_confidence", "lsp_confidence_static_scratch_bytes",
            "lsp_confidence_static", "lsp_commit_workspace_bytes",
            "lsp_commit", "lsp_commit_step", "lsp_flip_update", "lsp_poll_lengths", "lsp_poll_progress", "lsp_select_scattered", "lsp_kv_gather_append",
-           "lsp_attn_step_gather", "lsp_lm_head_confidence_workspace_bytes", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma"]
+           "lsp_attn_step_gather", "lsp_lm_head_confidence_workspace_bytes", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma",
+           "lsp_token_scores_workspace_bytes", "lsp_token_scores", "lsp_attn_key_weights_workspace_bytes", "lsp_attn_key_weights",
+           "lsp_kv_evict_workspace_bytes", "lsp_kv_evict"]
 
 # entry points that the native module calls, in the order of its table
 NATIVE_ENTRIES = ("lsp_attn_workspace_bytes", "lsp_attn_step", "lsp_attn_step_layers", "lsp_confidence_workspace_bytes", "lsp_confidence",
@@ -75,10 +83,11 @@ def lib() -> ctypes.CDLL:
         L.lsp_version.restype = ctypes.c_char_p
         L.lsp_last_error.restype = ctypes.c_char_p
         for n in ("lsp_attn_workspace_bytes", "lsp_confidence_workspace_bytes", "lsp_commit_workspace_bytes",
-                  "lsp_lm_head_confidence_workspace_bytes", "lsp_confidence_static_scratch_bytes"):
+                  "lsp_lm_head_confidence_workspace_bytes", "lsp_confidence_static_scratch_bytes", "lsp_token_scores_workspace_bytes",
+                  "lsp_attn_key_weights_workspace_bytes", "lsp_kv_evict_workspace_bytes"):
             getattr(L, n).restype = ctypes.c_size_t
         for n in ("lsp_attn_step", "lsp_attn_step_layers", "lsp_confidence", "lsp_confidence_static", "lsp_commit", "lsp_commit_step", "lsp_flip_update", "lsp_poll_lengths", "lsp_select_scattered",
-                  "lsp_kv_gather_append", "lsp_attn_step_gather", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma"):
+                  "lsp_kv_gather_append", "lsp_attn_step_gather", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma", "lsp_token_scores", "lsp_attn_key_weights", "lsp_kv_evict"):
             getattr(L, n).restype = ctypes.c_int32
         try:
             from . import _binding
@@ -633,6 +642,150 @@ def kv_gather_append(sel_index, count, prefix_len, layers: LayerTable, appended=
                                     _ptr(appended), _stream())
     _check(rc, "lsp_kv_gather_append")
     return appended
+
+
+def _here(*ts):
+    """Device tensors of the current device, on whose stream the work goes."""
+    _dev(*ts)
+    for t in ts:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise LspError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}: make it the current one "
+                           "(torch.cuda.device) for the call")
+
+
+def _call_workspace(given, need, device):
+    """The caller's workspace where it will do, or one of the call's own (of the stream's pool, so that streams cannot meet in it)."""
+    if (isinstance(given, torch.Tensor) and given.is_cuda and given.is_contiguous() and given.numel() * given.element_size() >= need
+            and given.data_ptr() % 16 == 0 and given.device == device):
+        return given
+    return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+
+def token_scores_workspace_bytes(B, S, V, num_alt) -> int:
+    return lib().lsp_token_scores_workspace_bytes(B, S, V, num_alt)
+
+
+def token_scores(logits, token_id=None, suffix_len=None, num_alt=0, out=None, workspace=None):
+    """lsp_token_scores: logits [B,S,V], token_id int32 [B,S] or None -> (logprob [B,S] or None, entropy [B,S],
+    alt_id int32 [B,S,num_alt], alt_logprob [B,S,num_alt]; both None where num_alt = 0), fp32.  num_alt: 0 to 32.
+    Rows >= suffix_len[b] are not written.
+    workspace: contiguous device memory of token_scores_workspace_bytes(B, S, V, num_alt) bytes and any content, aligned to 16
+    bytes, for this call alone until it has run; without one that will do, a call that wants one takes its own from torch's allocator."""
+    _here(logits, token_id, suffix_len)
+    if logits.dim() != 3 or logits.stride(2) != 1:
+        raise LspError("logits are [batch, row, vocabulary] with contiguous rows")
+    B, S, V = logits.shape
+    K = int(num_alt)
+    if not 0 <= K <= 32:
+        raise LspError(f"num_alt must be 0..32, got {K}")
+    _need("token_id", token_id, torch.int32, (B, S), optional=True)
+    _need("suffix_len", suffix_len, torch.int32, (B,), optional=True)
+    if out is None:
+        f = dict(dtype=torch.float32, device=logits.device)
+        out = (None if token_id is None else torch.empty((B, S), **f), torch.empty((B, S), **f),
+               torch.empty((B, S, K), dtype=torch.int32, device=logits.device) if K else None, torch.empty((B, S, K), **f) if K else None)
+    if len(out) != 4:
+        raise LspError("out must be (logprob, entropy, alt_id, alt_logprob)")
+    _here(*out)
+    if token_id is None and out[0] is not None:
+        raise LspError("out[0] (logprob) needs token_id")
+    if token_id is not None:
+        _need("out[0] (logprob)", out[0], torch.float32, (B, S))
+    _need("out[1] (entropy)", out[1], torch.float32, (B, S))
+    if K:
+        _need("out[2] (alt_id)", out[2], torch.int32, (B, S, K))
+        _need("out[3] (alt_logprob)", out[3], torch.float32, (B, S, K))
+    need = lib().lsp_token_scores_workspace_bytes(B, S, V, K)
+    workspace = _call_workspace(workspace, need, logits.device)
+    rc = lib().lsp_token_scores(_dtype(logits), _ptr(logits), B, S, V, ctypes.c_int64(logits.stride(1)), ctypes.c_int64(logits.stride(0)),
+                                _ptr(suffix_len), _ptr(token_id), K, _ptr(out[0]), _ptr(out[1]), _ptr(out[2] if K else None),
+                                _ptr(out[3] if K else None), _ptr(workspace), ctypes.c_size_t(need), _stream())
+    _check(rc, "lsp_token_scores")
+    return out
+
+
+def attn_key_weights_workspace_bytes(dtype, B, S, Hq, Hkv, D, C, num_layers=1) -> int:
+    d = AttnDesc(dtype=dtype, B=B, S=S, Hq=Hq, Hkv=Hkv, D=D, C=C)
+    return lib().lsp_attn_key_weights_workspace_bytes(ctypes.byref(d), num_layers)
+
+
+def _key_weights(d, n, q, k_suf, k_cache, prefix_len, suffix_len, weights, shape, decay, scale, workspace):
+    _here(prefix_len, suffix_len, weights)
+    _need("prefix_len", prefix_len, torch.int32, (d.B,))
+    _need("suffix_len", suffix_len, torch.int32, (d.B,))
+    _need("weights", weights, torch.float32, shape)
+    d.scale = float(scale)
+    need = lib().lsp_attn_key_weights_workspace_bytes(ctypes.byref(d), n)
+    workspace = _call_workspace(workspace, need, weights.device)
+    rc = lib().lsp_attn_key_weights(ctypes.byref(d), n, q, k_suf, k_cache, _ptr(prefix_len), _ptr(suffix_len), ctypes.c_float(decay),
+                                    _ptr(weights), _ptr(workspace), ctypes.c_size_t(need), _stream())
+    _check(rc, "lsp_attn_key_weights")
+    return weights
+
+
+def attn_key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay=1.0, scale=0.0, workspace=None):
+    """lsp_attn_key_weights for one layer: q [B,S,Hq,D], k_suf [B,S,Hkv,D], k_cache [B,C,Hkv,D] as in attn_step; weights fp32
+    [B,Hkv,C], updated in place and returned.  Cached rows' weights become decay * weight + the attention mass of this step, those of the
+    suffix rows, at prefix_len[b] on, that mass alone; the rest is left as it is.
+    workspace: contiguous device memory of attn_key_weights_workspace_bytes(...) bytes and any content, aligned to 16 bytes, for this
+    call alone until it has run; without one that will do, the call takes its own from torch's allocator."""
+    _here(q, k_suf, k_cache)
+    if q.dim() != 4 or k_suf.dim() != 4 or k_cache.dim() != 4:
+        raise LspError("attention operands are [batch, row, head, D]")
+    B, S, Hq, D = q.shape
+    Hkv, C = k_suf.shape[2], k_cache.shape[1]
+    for name, t, shape in (("k_suf", k_suf, (B, S, Hkv, D)), ("k_cache", k_cache, (B, C, Hkv, D))):
+        if t.dtype != q.dtype or tuple(t.shape) != shape:
+            raise LspError(f"{name} must be {q.dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    d = AttnDesc(dtype=_dtype(q), B=B, S=S, Hq=Hq, Hkv=Hkv, D=D, C=C)
+    d.q_stride, d.kv_suf_stride, d.cache_stride = _strides3(q), _strides3(k_suf), _strides3(k_cache)
+    one = ctypes.c_void_p * 1
+    return _key_weights(d, 1, one(q.data_ptr()), one(k_suf.data_ptr()), one(k_cache.data_ptr()), prefix_len, suffix_len, weights, (B, Hkv, C),
+                        decay, scale, workspace)
+
+
+def attn_key_weights_layers(table: AttnLayerTable, prefix_len, suffix_len, weights, decay=1.0, scale=0.0, workspace=None):
+    """lsp_attn_key_weights for every layer of `table` in the launches of one: weights fp32 [layers,B,Hkv,C], as in attn_key_weights."""
+    d, a = table.desc, table.arrays
+    return _key_weights(d, table.n, a[0], a[1], a[3], prefix_len, suffix_len, weights, (table.n, d.B, d.Hkv, d.C), decay, scale, workspace)
+
+
+def _evict_desc(layers, keep, high, first, recent):
+    keep = int(keep)
+    return EvictDesc(kv_dtype=layers.kv_dtype, B=layers.B, Hkv=layers.Hkv, D=layers.D, C=layers.C, num_layers=layers.n, keep=keep,
+                     high=keep if high is None else int(high), first=int(first), recent=int(recent), cache_batch_stride=layers.cache_bs)
+
+
+def kv_evict_workspace_bytes(layers: LayerTable, keep, high=None, first=0, recent=0) -> int:
+    return lib().lsp_kv_evict_workspace_bytes(ctypes.byref(_evict_desc(layers, keep, high, first, recent)))
+
+
+def kv_evict(weights, prefix_len, layers: LayerTable, keep, high=None, first=0, recent=0, new_weights=None, new_len=None, kept_index=None,
+             workspace=None):
+    """lsp_kv_evict: sequences of more than `high` (default: keep) cached rows are cut back to `keep`, per layer and KV head those of the
+    largest weights [layers,B,Hkv,C] beside the first `first` and the last `recent` ones; rows move inside the caches of `layers`.
+    new_weights, new_len: where weights and lengths after it go (default: in place).  kept_index int32 [layers,B,Hkv,keep], when given,
+    receives the former row of each.  Returns new_len.
+    workspace: contiguous device memory of kv_evict_workspace_bytes(...) bytes and any content, aligned to 16 bytes, for this call alone
+    until it has run; without one that will do, the call takes its own from torch's allocator."""
+    if new_weights is None:
+        new_weights = weights
+    if new_len is None:
+        new_len = prefix_len
+    _here(weights, prefix_len, new_weights, new_len, kept_index)
+    shape = (layers.n, layers.B, layers.Hkv, layers.C)
+    _need("weights", weights, torch.float32, shape)
+    _need("new_weights", new_weights, torch.float32, shape)
+    _need("prefix_len", prefix_len, torch.int32, (layers.B,))
+    _need("new_len", new_len, torch.int32, (layers.B,))
+    d = _evict_desc(layers, keep, high, first, recent)
+    _need("kept_index", kept_index, torch.int32, (*shape[:3], d.keep), optional=True)
+    need = lib().lsp_kv_evict_workspace_bytes(ctypes.byref(d))
+    workspace = _call_workspace(workspace, need, weights.device)
+    rc = lib().lsp_kv_evict(ctypes.byref(d), _ptr(weights), _ptr(prefix_len), layers.arrays[2], layers.arrays[3], _ptr(new_weights), _ptr(new_len),
+                            _ptr(kept_index), _ptr(workspace), ctypes.c_size_t(need), _stream())
+    _check(rc, "lsp_kv_evict")
+    return new_len
 
 
 def bench_read(buffer, workgroups, out):

@@ -347,6 +347,8 @@ __device__ __forceinline__ int cache_row(const AttnArgs &a, int b, int t) {
   return min(max(r, 0), a.C - 1);  // a bad index must not leave the buffer
 }
 
+// shapes, strides and scale of a descriptor, checked and resolved
+int32_t check_attn(const lsp_attn_desc *d, AttnArgs &a);
 int32_t launch_attn_f32(const AttnArgs &a, hipStream_t st);
 int32_t launch_attn_bf16(const AttnArgs &a, const AttnLayers &layers, hipStream_t st);
 size_t attn_f32_workspace_bytes(int32_t B, int32_t S, int32_t Hq, int32_t Hkv, int32_t D, int32_t C);  // 0: of no use

@@ -19,7 +19,9 @@ bool resolve(const int64_t in[3], int64_t out[3], int64_t rows, int64_t heads, i
   return in[2] >= D && in[1] > 0 && in[0] >= 0;
 }
 
-int32_t check(const lsp_attn_desc *d, AttnArgs &a) {
+}  // namespace
+
+int32_t check_attn(const lsp_attn_desc *d, AttnArgs &a) {
   LSP_CHECK_ARG(d != nullptr, "lsp_attn: null descriptor");
   LSP_CHECK_ARG(d->dtype == LSP_F32 || d->dtype == LSP_BF16, "lsp_attn: unknown dtype %d", d->dtype);
   LSP_CHECK_ARG(d->B > 0 && d->S > 0 && d->Hq > 0 && d->Hkv > 0 && d->D > 0 && d->C > 0,
@@ -44,7 +46,6 @@ int32_t check(const lsp_attn_desc *d, AttnArgs &a) {
   return LSP_OK;
 }
 
-}  // namespace
 }  // namespace lsp
 
 extern "C" size_t lsp_attn_workspace_bytes(const lsp_attn_desc *d) {
@@ -65,7 +66,7 @@ int32_t attn_entry(const lsp_attn_desc *d, const void *q, const void *k_suf, con
                    const int32_t *prefix_len, const int32_t *suffix_len, void *out, void *workspace,
                    size_t workspace_bytes, void *stream) {
   AttnArgs a;
-  const int32_t rc = check(d, a);
+  const int32_t rc = check_attn(d, a);
   if (rc != LSP_OK) return rc;
   LSP_CHECK_ARG(q && k_suf && v_suf && k_cache && v_cache && prefix_len && suffix_len && out,
                 "lsp_attn_step: null pointer");
@@ -94,7 +95,7 @@ extern "C" int32_t lsp_attn_step_layers(const lsp_attn_desc *d, int32_t num_laye
                                         void *stream) {
   using namespace lsp;
   AttnArgs a;
-  const int32_t rc = check(d, a);
+  const int32_t rc = check_attn(d, a);
   if (rc != LSP_OK) return rc;
   LSP_CHECK_ARG(num_layers > 0, "lsp_attn_step_layers: num_layers must be positive");
   LSP_CHECK_ARG(q_layers && k_suf_layers && v_suf_layers && k_cache_layers && v_cache_layers && out_layers &&

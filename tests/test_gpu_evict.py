@@ -1,0 +1,125 @@
+"""lsp_kv_evict against its definition: rows, weights, lengths and indices exactly."""
+import math
+
+import pytest
+import torch
+
+from oracle import serving
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lsp():
+    import paper_2603_05454_amd as m
+    assert torch.cuda.is_available()
+    return m
+
+
+def _bits(t):
+    return t.contiguous().view({2: torch.int16, 4: torch.int32}[t.element_size()])
+
+
+def _run(lsp, L, B, Hkv, D, C, P, keep, high=None, first=0, recent=0, dtype=torch.bfloat16, w=None, seed=0, in_place=True, pad=0):
+    g = torch.Generator().manual_seed(seed)
+    kc, vc = (torch.randn((L, B, C + pad, Hkv, D), generator=g).to(dtype) for _ in range(2))
+    w = torch.rand((L, B, Hkv, C), generator=g) if w is None else w
+    P = torch.tensor(P, dtype=torch.int32)
+    dk, dv = kc.cuda(), vc.cuda()
+    suf = [torch.zeros((B, 1, Hkv, D), dtype=dtype, device="cuda") for _ in range(L)]
+    table = lsp.LayerTable(suf, suf, list(dk[:, :, :C].unbind(0)), list(dv[:, :, :C].unbind(0)))
+    dw, dp = w.cuda(), P.cuda()
+    kept = torch.full((L, B, Hkv, keep), -5, dtype=torch.int32, device="cuda")
+    kw = {} if in_place else dict(new_weights=torch.full_like(dw, -9.0), new_len=torch.full_like(dp, -9))
+    new_len = lsp.kv_evict(dw, dp, table, keep=keep, high=high, first=first, recent=recent, kept_index=kept, **kw)
+    torch.cuda.synchronize()
+    rk, rv = kc.clone(), vc.clone()
+    new_w, length, index = serving.evict(w, P.clamp(0, C), keep, high, first, recent, caches=[rk[:, :, :C], rv[:, :, :C]])
+    assert torch.equal(new_len.cpu(), length) and torch.equal(kept.cpu(), index)
+    assert torch.equal(_bits(dk.cpu()), _bits(rk)) and torch.equal(_bits(dv.cpu()), _bits(rv))
+    if in_place:
+        assert torch.equal(_bits(dw.cpu()), _bits(new_w)) and new_len.data_ptr() == dp.data_ptr()
+    else:
+        got = kw["new_weights"].cpu()
+        for b in range(B):
+            n = int(length[b])
+            assert torch.equal(_bits(got[:, b, :, :n]), _bits(new_w[:, b, :, :n])) and (got[:, b, :, n:] == -9).all()
+        assert torch.equal(_bits(dw.cpu()), _bits(w)) and torch.equal(dp.cpu(), P)
+    return dw, dp
+
+
+CASES = [   # L, B, Hkv, D, C, P, keep, high, first, recent
+    (1, 1, 1, 8, 2, [2], 1, None, 0, 0), (1, 1, 1, 64, 5, [5], 4, None, 1, 2), (2, 3, 2, 64, 40, [40, 20, 21], 20, None, 0, 0),
+    (1, 2, 4, 128, 300, [300, 257], 256, None, 4, 64), (3, 2, 2, 128, 700, [700, 600], 255, None, 1, 33), (1, 1, 3, 64, 1000, [999], 998, None, 2, 500),
+    (1, 1, 2, 64, 900, [900], 100, None, 40, 60), (2, 2, 1, 64, 513, [513, 0], 1, None, 0, 1), (1, 4, 2, 64, 200, [100, 120, 121, 200], 80, 120, 3, 9),
+    (1, 1, 1, 128, 9000, [8999], 4100, None, 4, 256), (1, 2, 1, 64, 20000, [19999, 18001], 12000, None, 0, 1000), (35, 1, 2, 64, 50, [50], 30, None, 0, 4),
+    (1, 2, 2, 64, 60, [60, 60], 60, None, 0, 0), (1, 1, 1, 64, 70001, [70001], 35000, None, 4, 100),
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+@pytest.mark.parametrize("in_place", [True, False])
+def test_against_the_definition(lsp, case, in_place):
+    L, B, Hkv, D, C, P, keep, high, first, recent = CASES[case]
+    _run(lsp, L, B, Hkv, D, C, P, keep, high, first, recent, seed=case, in_place=in_place)
+
+
+def test_fp32_caches_with_a_batch_stride(lsp):
+    _run(lsp, 2, 3, 4, 64, 130, [130, 99, 128], 90, None, 2, 20, dtype=torch.float32, pad=7)
+
+
+@pytest.mark.parametrize("values", ["equal", "few", "extremes", "rising", "falling"])
+def test_weights_of_every_kind(lsp, values):
+    """Ties, zeros of both signs, infinities, NaN, negative weights, neighbours in the last bit."""
+    g = torch.Generator().manual_seed(2)
+    shape = (2, 2, 3, 3000)
+    w = {"equal": torch.full(shape, 0.5), "few": (torch.rand(shape, generator=g) * 4).floor() - 1,
+         "rising": torch.arange(3000.0).expand(shape).clone(), "falling": torch.arange(3000.0).flip(0).expand(shape).clone(),
+         "extremes": torch.randn(shape, generator=g)}[values]
+    if values == "extremes":
+        odd = torch.tensor([math.nan, -math.nan, math.inf, -math.inf, 0.0, -0.0, 1e-45, -1e-45, 3e38, -3e38, 1.0, 1.0 + 2.0 ** -23])
+        w = torch.where(torch.rand(shape, generator=g) < 0.8, odd[torch.randint(0, len(odd), shape, generator=g)], w)
+    _run(lsp, 2, 2, 3, 64, 3000, [3000, 2900], 1500, None, 3, 100, w=w)
+
+
+def test_lengths_beyond_the_buffers_are_clamped(lsp):
+    _run(lsp, 1, 3, 2, 64, 100, [400, -2, 100], 40, None, 4, 10, in_place=False)
+
+
+def test_nothing_to_do(lsp):
+    _run(lsp, 2, 2, 2, 64, 100, [40, 12], 40)
+    _run(lsp, 2, 2, 2, 64, 100, [60, 12], 40, high=60)
+
+
+def test_again_after_rows_were_appended(lsp):
+    """What an eviction leaves is what the next one starts from."""
+    dw, dp = _run(lsp, 1, 1, 2, 64, 200, [200], 100, None, 2, 30, seed=4)
+    w = dw.cpu()
+    w[..., 100:] = torch.rand(1, 1, 2, 100, generator=torch.Generator().manual_seed(9))
+    _run(lsp, 1, 1, 2, 64, 200, [180], 100, None, 2, 30, w=w, seed=5)
+
+
+def test_graph_replays(lsp):
+    g = torch.Generator().manual_seed(6)
+    L, B, H, D, C, keep = 2, 2, 2, 64, 400, 200
+    k0, v0, w0 = torch.randn((L, B, C, H, D), generator=g).cuda(), torch.randn((L, B, C, H, D), generator=g).cuda(), torch.rand((L, B, H, C), generator=g).cuda()
+    p0 = torch.tensor([400, 333], dtype=torch.int32, device="cuda")
+    k, v, w, p = k0.clone(), v0.clone(), w0.clone(), p0.clone()
+    suf = [torch.zeros((B, 1, H, D), device="cuda") for _ in range(L)]
+    table = lsp.LayerTable(suf, suf, list(k.unbind(0)), list(v.unbind(0)))
+    kept = torch.zeros((L, B, H, keep), dtype=torch.int32, device="cuda")
+    lsp.kv_evict(w, p, table, keep=keep, first=2, recent=40, kept_index=kept)
+    want = [t.clone() for t in (k, v, w, p, kept)]
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            lsp.kv_evict(w, p, table, keep=keep, first=2, recent=40, kept_index=kept)
+    for _ in range(4):
+        for t, s in ((k, k0), (v, v0), (w, w0), (p, p0)):
+            t.copy_(s)
+        kept.fill_(-3)
+        lsp.kv_evict(w0.clone(), p0.clone(), lsp.LayerTable(suf, suf, list(k0.clone().unbind(0)), list(v0.clone().unbind(0))), keep=keep // 2)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((k, v, w, p, kept), want))
