@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <chrono>
 #include <stdint.h>
 #include <stdio.h>
 
@@ -52,6 +53,19 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline size_t elem_size(int32_t dtype) { return dtype == LSP_F32 ? 4 : 2; }
 
 constexpr int kWave = 64;
+
+// The tag of one call: another one for the next four thousand million calls of the process, not 0, and scrambled so that
+// memory is not likely to hold it.
+inline uint32_t call_tag() {
+  static std::atomic<uint32_t> count{uint32_t(std::chrono::steady_clock::now().time_since_epoch().count() >> 10)};
+  uint32_t x;
+  do {
+    x = count.fetch_add(1, std::memory_order_relaxed) * 0x9e3779b1u;  // odd factors and shifted copies of itself: a permutation
+    x = (x ^ x >> 15) * 0x85ebca6bu;
+    x ^= x >> 13;
+  } while (x == 0);
+  return x;
+}
 
 // Kernel arguments that are wanted now.  The compiler fetches an argument where it is first used, so that those used behind
 // a length or a branch on one cost a trip to memory of their own there, 0.2-0.4 us of a kernel of a few

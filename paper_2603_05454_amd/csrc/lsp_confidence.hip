@@ -27,7 +27,6 @@
 #include <float.h>
 #include <limits.h>
 
-#include <chrono>
 #include <mutex>
 #include <type_traits>
 
@@ -529,19 +528,6 @@ inline int unsplit_threads(int64_t rows, int nt) {
 
 // what a call writes into its workspace: four numbers of each segment, each beside the tag
 constexpr size_t kSplitBytes = size_t(kSplitTarget) * 4 * sizeof(unsigned long long);
-
-// The tag of one call: another one for the next four thousand million calls of the process, not 0, and scrambled so that
-// memory is not likely to hold it.
-inline uint32_t call_tag() {
-  static std::atomic<uint32_t> count{uint32_t(std::chrono::steady_clock::now().time_since_epoch().count() >> 10)};
-  uint32_t x;
-  do {
-    x = count.fetch_add(1, std::memory_order_relaxed) * 0x9e3779b1u;  // odd factors and shifted copies of itself: a permutation
-    x = (x ^ x >> 15) * 0x85ebca6bu;
-    x ^= x >> 13;
-  } while (x == 0);
-  return x;
-}
 
 template <typename T>
 void launch_rows(int nt, hipStream_t st, const T *z, int B, int S, int V, int64_t row_stride, int64_t batch_stride,
