@@ -69,7 +69,8 @@ EXPORTS = ["lsp_version", "lsp_last_error", "lsp_attn_workspace_bytes", "lsp_att
 # entry points that the native module calls, in the order of its table
 NATIVE_ENTRIES = ("lsp_attn_workspace_bytes", "lsp_attn_step", "lsp_attn_step_layers", "lsp_confidence_workspace_bytes", "lsp_confidence",
                   "lsp_lm_head_confidence_workspace_bytes", "lsp_lm_head_confidence", "lsp_commit", "lsp_flip_update", "lsp_poll_lengths", "lsp_commit_step",
-                  "lsp_poll_progress")
+                  "lsp_poll_progress", "lsp_token_scores_workspace_bytes", "lsp_token_scores", "lsp_attn_key_weights_workspace_bytes",
+                  "lsp_attn_key_weights", "lsp_kv_evict_workspace_bytes", "lsp_kv_evict")
 
 
 def lib() -> ctypes.CDLL:
@@ -653,6 +654,11 @@ def _here(*ts):
                            "(torch.cuda.device) for the call")
 
 
+def _table_here(t):
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        _here(t)
+
+
 def _call_workspace(given, need, device):
     """The caller's workspace where it will do, or one of the call's own (of the stream's pool, so that streams cannot meet in it)."""
     if (isinstance(given, torch.Tensor) and given.is_cuda and given.is_contiguous() and given.numel() * given.element_size() >= need
@@ -671,10 +677,19 @@ def token_scores(logits, token_id=None, suffix_len=None, num_alt=0, out=None, wo
     Rows >= suffix_len[b] are not written.
     workspace: contiguous device memory of token_scores_workspace_bytes(B, S, V, num_alt) bytes and any content, aligned to 16
     bytes, for this call alone until it has run; without one that will do, a call that wants one takes its own from torch's allocator."""
+    if _nat is not None and out is not None:
+        rc = _nat.token_scores(logits, token_id, suffix_len, num_alt, out, workspace)
+        if rc is not None:
+            _check(rc, "lsp_token_scores")
+            return out
     _here(logits, token_id, suffix_len)
     if logits.dim() != 3 or logits.stride(2) != 1:
         raise LspError("logits are [batch, row, vocabulary] with contiguous rows")
     B, S, V = logits.shape
+    row = V if S == 1 else logits.stride(1)
+    batch = S * row if B == 1 else logits.stride(0)
+    if row == 0 or batch == 0:      # (which would stand for dense rows)
+        raise LspError("logits must not be broadcast")
     K = int(num_alt)
     if not 0 <= K <= 32:
         raise LspError(f"num_alt must be 0..32, got {K}")
@@ -697,7 +712,7 @@ def token_scores(logits, token_id=None, suffix_len=None, num_alt=0, out=None, wo
         _need("out[3] (alt_logprob)", out[3], torch.float32, (B, S, K))
     need = lib().lsp_token_scores_workspace_bytes(B, S, V, K)
     workspace = _call_workspace(workspace, need, logits.device)
-    rc = lib().lsp_token_scores(_dtype(logits), _ptr(logits), B, S, V, ctypes.c_int64(logits.stride(1)), ctypes.c_int64(logits.stride(0)),
+    rc = lib().lsp_token_scores(_dtype(logits), _ptr(logits), B, S, V, ctypes.c_int64(row), ctypes.c_int64(batch),
                                 _ptr(suffix_len), _ptr(token_id), K, _ptr(out[0]), _ptr(out[1]), _ptr(out[2] if K else None),
                                 _ptr(out[3] if K else None), _ptr(workspace), ctypes.c_size_t(need), _stream())
     _check(rc, "lsp_token_scores")
@@ -729,6 +744,11 @@ def attn_key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay=1
     suffix rows, at prefix_len[b] on, that mass alone; the rest is left as it is.
     workspace: contiguous device memory of attn_key_weights_workspace_bytes(...) bytes and any content, aligned to 16 bytes, for this
     call alone until it has run; without one that will do, the call takes its own from torch's allocator."""
+    if _nat is not None:
+        rc = _nat.attn_key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay, scale, workspace)
+        if rc is not None:
+            _check(rc, "lsp_attn_key_weights")
+            return weights
     _here(q, k_suf, k_cache)
     if q.dim() != 4 or k_suf.dim() != 4 or k_cache.dim() != 4:
         raise LspError("attention operands are [batch, row, head, D]")
@@ -737,6 +757,8 @@ def attn_key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay=1
     for name, t, shape in (("k_suf", k_suf, (B, S, Hkv, D)), ("k_cache", k_cache, (B, C, Hkv, D))):
         if t.dtype != q.dtype or tuple(t.shape) != shape:
             raise LspError(f"{name} must be {q.dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    if 0 in (q.stride(2), k_suf.stride(2), k_cache.stride(2)):      # (strides of 0 stand for a dense tensor)
+        raise LspError("attention operands must not be broadcast over heads")
     d = AttnDesc(dtype=_dtype(q), B=B, S=S, Hq=Hq, Hkv=Hkv, D=D, C=C)
     d.q_stride, d.kv_suf_stride, d.cache_stride = _strides3(q), _strides3(k_suf), _strides3(k_cache)
     one = ctypes.c_void_p * 1
@@ -747,6 +769,12 @@ def attn_key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay=1
 def attn_key_weights_layers(table: AttnLayerTable, prefix_len, suffix_len, weights, decay=1.0, scale=0.0, workspace=None):
     """lsp_attn_key_weights for every layer of `table` in the launches of one: weights fp32 [layers,B,Hkv,C], as in attn_key_weights."""
     d, a = table.desc, table.arrays
+    _table_here(table.keep[0][0])
+    if _nat is not None:
+        rc = _nat.attn_key_weights_layers(d, table.n, a, prefix_len, suffix_len, weights, decay, scale, workspace)
+        if rc is not None:
+            _check(rc, "lsp_attn_key_weights")
+            return weights
     return _key_weights(d, table.n, a[0], a[1], a[3], prefix_len, suffix_len, weights, (table.n, d.B, d.Hkv, d.C), decay, scale, workspace)
 
 
@@ -772,6 +800,14 @@ def kv_evict(weights, prefix_len, layers: LayerTable, keep, high=None, first=0, 
         new_weights = weights
     if new_len is None:
         new_len = prefix_len
+    _table_here(layers.keep[2][0])
+    if _nat is not None:
+        rc = _nat.kv_evict(weights, prefix_len, layers, (keep, keep if high is None else high, first, recent), new_weights, new_len, kept_index, workspace)
+        if rc is not None:
+            _check(rc, "lsp_kv_evict")
+            return new_len
+    if layers.cache_bs == 0 and layers.B > 1:
+        raise LspError("caches must not be broadcast")
     _here(weights, prefix_len, new_weights, new_len, kept_index)
     shape = (layers.n, layers.B, layers.Hkv, layers.C)
     _need("weights", weights, torch.float32, shape)

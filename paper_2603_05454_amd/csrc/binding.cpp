@@ -12,10 +12,12 @@
 #include <hip/hip_runtime_api.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <chrono>
+#include <initializer_list>
 
 #include "binding_workspace.h"
 #include "lsp.h"
@@ -36,8 +38,14 @@ struct Entry {
   decltype(&lsp_poll_lengths) poll_lengths;
   decltype(&lsp_commit_step) commit_step;
   decltype(&lsp_poll_progress) poll_progress;
+  decltype(&lsp_token_scores_workspace_bytes) token_scores_workspace_bytes;
+  decltype(&lsp_token_scores) token_scores;
+  decltype(&lsp_attn_key_weights_workspace_bytes) attn_key_weights_workspace_bytes;
+  decltype(&lsp_attn_key_weights) attn_key_weights;
+  decltype(&lsp_kv_evict_workspace_bytes) kv_evict_workspace_bytes;
+  decltype(&lsp_kv_evict) kv_evict;
 } g;
-constexpr int kEntries = 12;
+constexpr int kEntries = 18;
 
 const at::Tensor *tensor(PyObject *o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
 const at::Tensor *device_tensor(PyObject *o) {
@@ -155,6 +163,12 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   g.poll_lengths = reinterpret_cast<decltype(g.poll_lengths)>(p[9]);
   g.commit_step = reinterpret_cast<decltype(g.commit_step)>(p[10]);
   g.poll_progress = reinterpret_cast<decltype(g.poll_progress)>(p[11]);
+  g.token_scores_workspace_bytes = reinterpret_cast<decltype(g.token_scores_workspace_bytes)>(p[12]);
+  g.token_scores = reinterpret_cast<decltype(g.token_scores)>(p[13]);
+  g.attn_key_weights_workspace_bytes = reinterpret_cast<decltype(g.attn_key_weights_workspace_bytes)>(p[14]);
+  g.attn_key_weights = reinterpret_cast<decltype(g.attn_key_weights)>(p[15]);
+  g.kv_evict_workspace_bytes = reinterpret_cast<decltype(g.kv_evict_workspace_bytes)>(p[16]);
+  g.kv_evict = reinterpret_cast<decltype(g.kv_evict)>(p[17]);
   Py_RETURN_NONE;
 }
 
@@ -251,6 +265,81 @@ PyObject *lm_head_confidence(PyObject *, PyObject *const *a, Py_ssize_t n) {
                 data<void>(ws), size_t(bytes_of(ws)), stream());
 }
 
+// a contiguous tensor of the current device, of this element type and shape
+const at::Tensor *dense(PyObject *o, at::ScalarType type, std::initializer_list<int64_t> shape) {
+  const at::Tensor *t = plain(o, type);
+  return t && t->sizes() == at::IntArrayRef(shape.begin(), shape.size()) && t->device().index() == c10::hip::current_device() ? t : nullptr;
+}
+const at::Tensor *local_tensor(PyObject *o) {
+  const at::Tensor *t = device_tensor(o);
+  return t && t->device().index() == c10::hip::current_device() ? t : nullptr;
+}
+
+// Strides of rows and sequences as lsp_token_scores takes them, which has a meaning of its own for 0.
+bool row_strides(const at::Tensor &z, int64_t &row, int64_t &batch) {
+  row = z.size(1) == 1 ? z.size(2) : z.stride(1);
+  batch = z.size(0) == 1 ? row * z.size(1) : z.stride(0);
+  return row > 0 && batch > 0;
+}
+// (logits, token_id or None, suffix_len or None, num_alt, out, workspace or None)
+PyObject *token_scores(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(6);
+  const at::Tensor *z = local_tensor(a[0]);
+  int32_t type;
+  long K;
+  ORDINARY(z && z->dim() == 3 && z->stride(2) == 1 && element_type(*z, type) && integer(a[3], K) && K >= 0 && K <= 32);
+  const int64_t B = z->size(0), S = z->size(1), V = z->size(2);
+  int64_t row, batch;
+  ORDINARY(row_strides(*z, row, batch));
+  const at::Tensor *id = a[1] == Py_None ? nullptr : dense(a[1], at::kInt, {B, S}), *sl = a[2] == Py_None ? nullptr : dense(a[2], at::kInt, {B});
+  ORDINARY((id || a[1] == Py_None) && (sl || a[2] == Py_None) && PyTuple_Check(a[4]) && PyTuple_GET_SIZE(a[4]) == 4);
+  PyObject *const *o = &PyTuple_GET_ITEM(a[4], 0);
+  const at::Tensor *lp = id ? dense(o[0], at::kFloat, {B, S}) : nullptr, *h = dense(o[1], at::kFloat, {B, S}),
+                   *ai = K ? dense(o[2], at::kInt, {B, S, K}) : nullptr, *al = K ? dense(o[3], at::kFloat, {B, S, K}) : nullptr;
+  ORDINARY((lp || (!id && o[0] == Py_None)) && h && (!K || (ai && al)));
+  // (without memory for a workspace every row is one workgroup's)
+  const Workspace work(g.token_scores_workspace_bytes(int32_t(B), int32_t(S), int32_t(V), int32_t(K)), local_tensor(a[5]));
+  return status(g.token_scores, type, z->const_data_ptr(), int32_t(B), int32_t(S), int32_t(V), row, batch, data<int32_t>(sl),
+                data<int32_t>(id), int32_t(K), data<float>(lp), data<float>(h), data<int32_t>(ai), data<float>(al), work.at, work.bytes, stream());
+}
+
+PyObject *key_weights(lsp_attn_desc &d, long layers, const void *const *q, const void *const *ks, const void *const *kc, const at::Tensor *pl,
+                      const at::Tensor *sl, const at::Tensor *w, PyObject *decay, PyObject *scale, PyObject *workspace) {
+  float f;
+  ORDINARY(pl && sl && w && number(decay, f) && number(scale, d.scale));
+  const Workspace work(g.attn_key_weights_workspace_bytes(&d, int32_t(layers)), local_tensor(workspace));
+  const int32_t rc = unlocked(g.attn_key_weights, &d, int32_t(layers), q, ks, kc, data<int32_t>(pl), data<int32_t>(sl), f, data<float>(w), work.at,
+                              work.bytes, stream());
+  ORDINARY(rc != LSP_ERR_WORKSPACE);  // (no memory for it: the general path raises)
+  return PyLong_FromLong(rc);
+}
+// (q, k_suf, k_cache, prefix_len, suffix_len, weights, decay, scale, workspace or None)
+PyObject *attn_key_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(9);
+  const at::Tensor *q = local_tensor(a[0]), *ks = local_tensor(a[1]), *kc = local_tensor(a[2]);
+  ORDINARY(q && ks && kc && q->dim() == 4 && ks->dim() == 4 && kc->dim() == 4);
+  const int64_t B = q->size(0), S = q->size(1), Hq = q->size(2), D = q->size(3), Hkv = ks->size(2), C = kc->size(1);
+  ORDINARY(ks->scalar_type() == q->scalar_type() && kc->scalar_type() == q->scalar_type() && shape4(*ks, B, S, Hkv, D) && shape4(*kc, B, C, Hkv, D));
+  lsp_attn_desc d = {};
+  ORDINARY(element_type(*q, d.dtype) && strides3(*q, d.q_stride) && strides3(*ks, d.kv_suf_stride) && strides3(*kc, d.cache_stride));
+  ORDINARY(d.q_stride[2] > 0 && d.kv_suf_stride[2] > 0 && d.cache_stride[2] > 0);  // (strides of 0 stand for a dense tensor)
+  d.B = int32_t(B); d.S = int32_t(S); d.Hq = int32_t(Hq); d.Hkv = int32_t(Hkv); d.D = int32_t(D); d.C = int32_t(C);
+  const void *at[3] = {q->const_data_ptr(), ks->const_data_ptr(), kc->const_data_ptr()};
+  return key_weights(d, 1, &at[0], &at[1], &at[2], dense(a[3], at::kInt, {B}), dense(a[4], at::kInt, {B}), dense(a[5], at::kFloat, {B, Hkv, C}), a[6],
+                     a[7], a[8]);
+}
+// (table descriptor, layers, list of six tables, prefix_len, suffix_len, weights, decay, scale, workspace or None)
+PyObject *attn_key_weights_layers(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(9);
+  Memory desc, tab[6];
+  long layers;
+  ORDINARY(integer(a[1], layers) && layers > 0 && desc.of(a[0], sizeof(lsp_attn_desc)) && tables(a[2], tab, layers));
+  lsp_attn_desc own = *static_cast<const lsp_attn_desc *>(desc.view.buf);
+  auto in = [&](int k) { return static_cast<const void *const *>(tab[k].view.buf); };
+  return key_weights(own, layers, in(0), in(1), in(3), dense(a[3], at::kInt, {own.B}), dense(a[4], at::kInt, {own.B}),
+                     dense(a[5], at::kFloat, {layers, own.B, own.Hkv, own.C}), a[6], a[7], a[8]);
+}
+
 // int32[4] of host memory, as lsp_poll_lengths wants it
 int32_t *host_words(PyObject *o) {
   const at::Tensor *t = tensor(o);
@@ -345,6 +434,35 @@ PyObject *commit(PyObject *, PyObject *const *a, Py_ssize_t n) {
                 static_cast<void *const *>(tab[3].view.buf), data<int32_t>(tokens), data<int32_t>(pl), data<int32_t>(sl), data<uint8_t>(mask),
                 data<int32_t>(raw), data<int32_t>(snapped), data<int32_t>(len),
                 data<int32_t>(flags), data<float>(tau), nullptr, 0, stream());
+}
+
+// (weights, prefix_len, layer table, (keep, high, first, recent), new_weights, new_len, kept_index or None, workspace or None)
+PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(8);
+  long i[4], t[9];
+  ORDINARY(PyTuple_Check(a[3]) && PyTuple_GET_SIZE(a[3]) == 4);
+  for (int k = 0; k < 4; ++k) ORDINARY(integer(PyTuple_GET_ITEM(a[3], k), i[k]) && i[k] == int32_t(i[k]));
+  for (int k = 0; k < 9; ++k) {
+    Object x(PyObject_GetAttr(a[2], k_numbers[k]));
+    ORDINARY(integer(x.o, t[k]));
+  }
+  Memory tab[4];
+  Object arrays(PyObject_GetAttr(a[2], k_arrays));
+  ORDINARY(t[6] > 0 && (t[8] > 0 || t[1] == 1) && tables(arrays.o, tab, t[6]));
+  lsp_evict_desc d = {};
+  d.kv_dtype = int32_t(t[0]); d.B = int32_t(t[1]); d.Hkv = int32_t(t[3]); d.D = int32_t(t[4]); d.C = int32_t(t[5]); d.num_layers = int32_t(t[6]);
+  d.cache_batch_stride = t[8];
+  d.keep = int32_t(i[0]); d.high = int32_t(i[1]); d.first = int32_t(i[2]); d.recent = int32_t(i[3]);
+  const at::Tensor *w = dense(a[0], at::kFloat, {t[6], t[1], t[3], t[5]}), *pl = dense(a[1], at::kInt, {t[1]}),
+                   *nw = dense(a[4], at::kFloat, {t[6], t[1], t[3], t[5]}), *nl = dense(a[5], at::kInt, {t[1]}),
+                   *kept = a[6] == Py_None ? nullptr : dense(a[6], at::kInt, {t[6], t[1], t[3], i[0]});
+  ORDINARY(w && pl && nw && nl && (kept || a[6] == Py_None));
+  const Workspace work(g.kv_evict_workspace_bytes(&d), local_tensor(a[7]));
+  const int32_t rc = unlocked(g.kv_evict, &d, data<float>(w), data<int32_t>(pl), static_cast<void *const *>(tab[2].view.buf),
+                              static_cast<void *const *>(tab[3].view.buf), data<float>(nw), data<int32_t>(nl), data<int32_t>(kept), work.at, work.bytes,
+                              stream());
+  ORDINARY(rc != LSP_ERR_WORKSPACE);
+  return PyLong_FromLong(rc);
 }
 
 // (top1_id, prefix_len, suffix_len, base_prefix_len, last_id, counters, window_lo, window_hi, step_counts or None)
@@ -483,7 +601,9 @@ PyMethodDef fast(const char *name) {
 PyMethodDef methods[] = {fast<bind>("bind"), fast<attn_step>("attn_step"), fast<attn_step_layers>("attn_step_layers"),
                          fast<confidence>("confidence"), fast<lm_head_confidence>("lm_head_confidence"), fast<commit<false>>("commit"), fast<commit<true>>("commit_step"),
                          fast<flip_update>("flip_update"), fast<poll_lengths>("poll_lengths"),
-                         fast<poll_start>("poll_start"), fast<poll_wait>("poll_wait"), fast<addresses>("addresses"), {nullptr, nullptr, 0, nullptr}};
+                         fast<poll_start>("poll_start"), fast<poll_wait>("poll_wait"), fast<addresses>("addresses"),
+                         fast<token_scores>("token_scores"), fast<attn_key_weights>("attn_key_weights"),
+                         fast<attn_key_weights_layers>("attn_key_weights_layers"), fast<kv_evict>("kv_evict"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -123,3 +123,24 @@ def test_graph_replays(lsp):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((k, v, w, p, kept), want))
+
+
+def test_native_and_general_path_agree(lsp, monkeypatch):
+    g = torch.Generator().manual_seed(7)
+    made = []
+    for native in (True, False):
+        g.manual_seed(7)
+        k, v = (torch.randn((2, 60, 2, 64), generator=g).cuda() for _ in range(2))
+        w, p = torch.rand((1, 2, 2, 60), generator=g).cuda(), torch.tensor([60, 41], dtype=torch.int32, device="cuda")
+        table = lsp.LayerTable([k[:, :3].contiguous()], [k[:, :3].contiguous()], [k], [v])
+        if native:
+            assert lsp._nat.kv_evict(w, p, table, (30, 40, 1, 5), w, p, None, None) == 0
+            assert lsp._nat.kv_evict(w, p.long(), table, (30, 40, 1, 5), w, p, None, None) is None
+            assert lsp._nat.kv_evict(w, p, table, (30, 2 ** 40, 1, 5), w, p, None, None) is None
+            with pytest.raises(lsp.LspError, match="first"):
+                lsp.kv_evict(w, p, table, 30, first=20, recent=11)
+        else:
+            monkeypatch.setattr(lsp, "_nat", None)
+            lsp.kv_evict(w, p, table, 30, high=40, first=1, recent=5)
+        made.append((k, v, w, p))
+    assert all(torch.equal(a, b) for a, b in zip(*made))

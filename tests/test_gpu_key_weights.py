@@ -155,3 +155,21 @@ def test_mass_of_a_long_batch_adds_up(lsp):
     for h in (0, 7):
         want = serving.key_weights(q[0][:, :, h:h + 1], k[0][:, :, h:h + 1], c[0][:, :, h:h + 1], P, N, torch.zeros(B, 1, C))
         _close(got[:, h:h + 1], want, torch.zeros(B, 1, C), P, N, C)
+
+
+def test_native_and_general_path_agree(lsp, monkeypatch):
+    q, k, c, w = (t[0].cuda() for t in _operands(2, 9, 4, 2, 64, 30, torch.float32, seed=8))
+    P, N = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([20, 3], [9, 4]))
+    table = lsp.AttnLayerTable([q], [k], [k], [c], [c], [torch.zeros_like(q)])
+    a, b = w.clone(), w.clone()[None]
+    assert lsp._nat.attn_key_weights(q, k, c, P, N, a, 0.5, 0.1, None) == 0
+    assert lsp._nat.attn_key_weights_layers(table.desc, 1, table.arrays, P, N, b, 0.5, 0.1, None) == 0
+    assert lsp._nat.attn_key_weights(q, k, c, P, N.long(), a, 0.5, 0.1, None) is None
+    assert lsp._nat.attn_key_weights(q, k, c, P, N, a[:, :, :29], 0.5, 0.1, None) is None
+    assert lsp._nat.attn_key_weights(q, k, c.bfloat16(), P, N, a, 0.5, 0.1, None) is None
+    monkeypatch.setattr(lsp, "_nat", None)
+    x = lsp.attn_key_weights(q, k, c, P, N, w.clone(), decay=0.5, scale=0.1)
+    y = lsp.attn_key_weights_layers(table, P, N, w.clone()[None], decay=0.5, scale=0.1)
+    assert torch.equal(a, x) and torch.equal(b, y) and torch.equal(x, y[0])
+    with pytest.raises(lsp.LspError, match="decay"):
+        lsp.attn_key_weights(q, k, c, P, N, w, decay=-0.1)

@@ -194,3 +194,24 @@ def test_graph_replays_and_other_streams(lsp):
         lsp.token_scores(z, ids, N, num_alt=20, out=got)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_native_and_general_path_agree(lsp, monkeypatch):
+    """The native module takes the ordinary calls and leaves the others to the checks in Python."""
+    z = torch.randn((2, 5, 30000), generator=torch.Generator().manual_seed(1)).cuda()
+    ids, N = torch.zeros((2, 5), dtype=torch.int32, device="cuda"), torch.tensor([5, 2], dtype=torch.int32, device="cuda")
+    cases = [(ids, N, 3), (None, None, 0), (None, N, 32), (ids, None, 0)]
+    for t, n, K in cases:
+        out = _out(2, 5, K, t)
+        assert lsp._nat.token_scores(z, t, n, K, out, None) == 0
+        with monkeypatch.context() as m:
+            m.setattr(lsp, "_nat", None)
+            other = lsp.token_scores(z, t, n, num_alt=K, out=_out(2, 5, K, t))
+        assert all(a is b is None or torch.equal(a, b) for a, b in zip(out, other))
+    out = _out(2, 5, 3, ids)
+    for bad in ((ids.long(), N, 3, out), (ids, N, 4, out), (ids, N, 33, out), (None, N, 3, out), (ids, N.long(), 3, out), (ids, N, 3, out[:3]),
+                (ids, N, 3, (None, *out[1:]))):
+        assert lsp._nat.token_scores(z, *bad, None) is None
+        with pytest.raises(lsp.LspError):
+            lsp.token_scores(z, bad[0], bad[1], num_alt=bad[2], out=bad[3])
+    assert lsp._nat.token_scores(z[:1, :1].expand(2, 5, 30000), ids, N, 3, out, None) is None

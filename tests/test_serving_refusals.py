@@ -93,6 +93,9 @@ def test_the_binding_refuses_wrong_tensors(monkeypatch):
         ("weights must have shape", lambda: m.kv_evict(f32(2, 2, 16), i32(2), lay, 8)),
         ("new_weights must", lambda: m.kv_evict(f32(1, 2, 2, 16), i32(2), lay, 8, new_weights=f32(1, 2, 2, 8))),
         ("new_len must", lambda: m.kv_evict(f32(1, 2, 2, 16), i32(2), lay, 8, new_len=i32(3))),
+        ("broadcast", lambda: m.token_scores(f32(1, 1, 64).expand(2, 4, 64), i32(2, 4))),
+        ("broadcast", lambda: m.attn_key_weights(f32(1, 1, 1, 64).expand(2, 4, 4, 64), k, c, i32(2), i32(2), f32(2, 2, 16))),
+        ("broadcast", lambda: m.kv_evict(f32(1, 2, 2, 16), i32(2), m.LayerTable([k], [k], [c[:1].expand(2, 16, 2, 64)], [c[:1].expand(2, 16, 2, 64)]), 8)),
         ("kept_index must", lambda: m.kv_evict(f32(1, 2, 2, 16), i32(2), lay, 8, kept_index=i32(1, 2, 2, 9))),
     ]
     for text, call in cases:
