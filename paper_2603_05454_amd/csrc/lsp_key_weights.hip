@@ -2,8 +2,16 @@
 //
 // With c = scale log2(e) and L[h,i] the base-2 logarithm of the sum over all keys of 2^(c q.k):
 //   mass[g,t] = sum over heads h of group g and rows i < N of 2^(c q[i,h].k[t,g] - L[h,i])
-// Two kernels: one computes L of every row, the other the sums down the columns, each from its own product of queries and
-// keys.  (The products kept instead would be 1.3e9 numbers a layer at 8 x 1024 rows of 32 heads on 4096.)
+// Two kernels: row_log_kernel computes L of every row, key_sum_kernel the sums down the columns, each from its own product of queries
+// and keys.  (The products kept instead would be 1.3e9 numbers a layer at 8 x 1024 rows of 32 heads on 4096.)
+//
+// Both are the same loop with the operands exchanged.  A wave holds NS blocks of 32 rows of one operand as matrix fragments in registers (queries for
+// the logarithms, keys for the sums) and all four waves of the workgroup read the other one from LDS, 32 rows at a time, from a ring that
+// is filled by loads that go straight to LDS.  Scores come out transposed, keys x queries (v_mfma_f32_32x32x16_bf16, or 32x32x2 in fp32),
+// so a lane's 16 scores are of ONE query: its reference and sum, or its L, are per-lane numbers, and nothing crosses lanes in the loop:
+// the logarithm joins two lanes at the end, the sums of a key stay one register for each of the wave's 32 x NS keys and are reduced over
+// 32 lanes once.  The rows of all heads of a group are one list (entry e: row e % N of head e / N), since they meet the same keys.
+// Everything is summed in fp32, in an order that sizes alone decide.
 #include <math.h>
 
 #include "lsp_attn.h"
@@ -11,83 +19,424 @@
 namespace lsp {
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kStages = 4;           // of the ring: the tile in use, two that are on their way or there, one that is being asked for
+constexpr int kLogs = 4096;          // rows whose L are in LDS at a time
+constexpr int kMaxParts = 16;        // of the keys, where rows are few
+constexpr int kPartKeys = 128;       // a part has at least
+constexpr int kEnough = 512;         // workgroups: two to a compute unit
+constexpr float kFarBelow = -1.7e38f;  // a reference below all scores
 
 struct WeightArgs {
   const int32_t *prefix_len, *suffix_len;
-  int32_t B, S, Hq, Hkv, D, C, rep;
+  int32_t B, S, Hq, Hkv, D, C, rep, layers;
+  int32_t units, tiles, spread, max_parts;  // (layer, sequence, KV head)s; workgroups of one; each unit in 2^spread pieces
   float scale, decay;
-  int64_t qs[3], ks[3], cs[3];
-  float *row_log;  // [layers of the launch, B, Hq, S]
+  int64_t qs[3], ks[3], cs[3];  // bytes: batch, row, head
+  float *row_log;  // [max_parts, units, rep * S]
   float *weights;  // of the launch's first layer: [layers, B, Hkv, C]
 };
 struct WeightLayers {
-  const void *q[kMaxAttnLayers], *k_suf[kMaxAttnLayers], *k_cache[kMaxAttnLayers];
+  const char *q[kMaxAttnLayers], *k_suf[kMaxAttnLayers], *k_cache[kMaxAttnLayers];
 };
 
-__device__ __forceinline__ float element(const float *p) { return *p; }
-__device__ __forceinline__ float element(const uint16_t *p) { return bf16_to_f32(*p); }
-
-template <typename T>
-__device__ __forceinline__ const T *key_row(const WeightArgs &a, const WeightLayers &L, int l, int b, int g, int t, int P) {
-  if (t < P) return static_cast<const T *>(L.k_cache[l]) + b * a.cs[0] + int64_t(t) * a.cs[1] + g * a.cs[2];
-  return static_cast<const T *>(L.k_suf[l]) + b * a.ks[0] + int64_t(t - P) * a.ks[1] + g * a.ks[2];
-}
-template <typename T>
-__device__ __forceinline__ float dot(const T *x, const T *y, int D) {
-  float s = 0.f;
-  for (int d = 0; d < D; ++d) s = fmaf(element(x + d), element(y + d), s);
-  return s;
-}
-
-// One wave per row.
-template <typename T>
-__global__ __launch_bounds__(kWave) void row_log_kernel(WeightArgs a, WeightLayers L) {
-  const int i = blockIdx.x, h = blockIdx.y % a.Hq, b = blockIdx.y / a.Hq, l = blockIdx.z;
-  const int N = min(max(a.suffix_len[b], 0), a.S), P = min(max(a.prefix_len[b], 0), a.C);
-  if (i >= N) return;
-  const T *q = static_cast<const T *>(L.q[l]) + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
-  float m = -INFINITY, s = 0.f;
-  for (int t = threadIdx.x; t < P + N; t += kWave) {
-    const float x = dot(q, key_row<T>(a, L, l, b, h / a.rep, t, P), a.D) * a.scale * kLog2e;
-    const float n = fmaxf(m, x);
-    s = s * exp2f(m - n) + exp2f(x - n);
-    m = n;
+// Geometry of a tile of 32 rows in LDS.  16-byte pieces of a row are exchanged so that the 32 lanes that read the same piece of 32 rows meet
+// all banks alike: piece p of row r is at p ^ (r % 16) of its 256 bytes; where two rows share 256 bytes, at (8 (r % 2) + p) ^ (r / 2 % 8).
+template <typename T, int D>
+struct Tile {
+  static constexpr int kRowBytes = D * int(sizeof(T));     // 128, 256 or 512
+  static constexpr int kFrags = kRowBytes / 32;            // pieces of a row that a lane has: lane l those of row l % 32 with number % 2 = l / 32
+  static constexpr int kBytes = 32 * kRowBytes;
+  static constexpr int kLoads = kFrags / kWaves;           // wave-wide loads of 1 KB that a wave makes for a tile
+  // where lane's fragment c is
+  static __device__ __forceinline__ int frag_at(int lane, int c) {
+    const int r = lane & 31, p = 2 * c + (lane >> 5);
+    if (kRowBytes == 128) return (r >> 1) * 256 + 16 * ((8 * (r & 1) + p) ^ (r >> 1 & 7));
+    return r * kRowBytes + (p >> 4) * 256 + 16 * ((p & 15) ^ (r & 15));
   }
-  float M = m;
-  for (int k = 1; k < kWave; k <<= 1) M = fmaxf(M, __shfl_xor(M, k));
-  s *= exp2f(m - M);
-  for (int k = 1; k < kWave; k <<= 1) s += __shfl_xor(s, k);
-  if (threadIdx.x == 0) a.row_log[((int64_t(l) * a.B + b) * a.Hq + h) * a.S + i] = M + log2f(s);
+  // row and byte of it that belong to 16-byte place y
+  static __device__ __forceinline__ void place(int y, int &row, int &byte) {
+    const int line = y >> 4, x = y & 15;
+    if (kRowBytes == 128) {
+      const int z = x ^ (line & 7);
+      row = 2 * line + (z >> 3);
+      byte = 16 * (z & 7);
+    } else {
+      constexpr int kLines = kRowBytes < 256 ? 1 : kRowBytes / 256;
+      row = line / kLines;
+      byte = 256 * (line % kLines) + 16 * (x ^ (row & 15));
+    }
+  }
+};
+
+// scores += A x B for one fragment of each
+__device__ __forceinline__ void step(f32x16 &s, const u32x4 &a, const u32x4 &b, const uint16_t *) {
+  s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), s, 0, 0, 0);
+}
+__device__ __forceinline__ void step(f32x16 &s, const u32x4 &a, const u32x4 &b, const float *) {
+  const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], s, 0, 0, 0);
+}
+// row of the product that register r of a lane holds (its column: lane % 32)
+__device__ __forceinline__ int product_row(int lane, int r) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
 }
 
-// One key per lane.
-template <typename T>
-__global__ __launch_bounds__(kWave) void key_sum_kernel(WeightArgs a, WeightLayers L) {
-  const int t = blockIdx.x * kWave + threadIdx.x, g = blockIdx.y % a.Hkv, b = blockIdx.y / a.Hkv, l = blockIdx.z;
-  const int N = min(max(a.suffix_len[b], 0), a.S), P = min(max(a.prefix_len[b], 0), a.C);
-  if (N == 0 || t >= min(P + N, a.C)) return;
-  const T *k = key_row<T>(a, L, l, b, g, t, P);
-  float sum = 0.f;
-  for (int h = g * a.rep; h < (g + 1) * a.rep; ++h)
-    for (int i = 0; i < N; ++i) {
-      const T *q = static_cast<const T *>(L.q[l]) + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
-      sum += exp2f(dot(q, k, a.D) * a.scale * kLog2e - a.row_log[((int64_t(l) * a.B + b) * a.Hq + h) * a.S + i]);
+struct Unit {
+  int l, b, g, w, N, P;
+  bool valid;
+};
+// Workgroups of a unit read the same stream; ids that are equal modulo 8 share an XCD's L2.
+__device__ __forceinline__ Unit unit_of(const WeightArgs &a, int n) {
+  const int pieces = a.units << a.spread, per_piece = (a.tiles + (1 << a.spread) - 1) >> a.spread;
+  const int rest = n >> 3, piece = rest / per_piece * 8 + (n & 7), u = piece >> a.spread;
+  Unit r;
+  r.w = ((rest % per_piece) << a.spread) + (piece & ((1 << a.spread) - 1));
+  r.valid = piece < pieces && r.w < a.tiles;
+  r.g = u % a.Hkv;
+  r.b = u / a.Hkv % a.B;
+  r.l = u / a.Hkv / a.B;
+  r.N = r.P = 0;
+  if (r.valid) {
+    r.N = min(max(a.suffix_len[r.b], 0), a.S);
+    r.P = min(max(a.prefix_len[r.b], 0), a.C);
+  }
+  return r;
+}
+int64_t place_grid(WeightArgs &a) {
+  a.spread = 0;
+  if (a.units < 32)
+    while ((a.units << a.spread) % 8 != 0) ++a.spread;
+  const int64_t pieces8 = ((int64_t(a.units) << a.spread) + 7) / 8, per_piece = (a.tiles + (1 << a.spread) - 1) >> a.spread;
+  return pieces8 * 8 * per_piece;
+}
+// Parts of the keys of a sequence: both kernels go by this.
+__device__ __forceinline__ int parts_of(const WeightArgs &a, int rows, int keys, int rows_of_group) {
+  if (a.max_parts == 1 || rows > kLogs) return 1;
+  const int groups = a.units * ((rows + rows_of_group - 1) / rows_of_group);
+  return max(1, min(min(kEnough / groups, a.max_parts), keys / kPartKeys));
+}
+
+// A ring of tiles.  fetch(tile, place's row, place's byte) says where a lane's 16 bytes are.
+template <typename T, int D>
+struct Ring {
+  typedef Tile<T, D> G;
+  char *lds;
+  int wave, row[G::kLoads], byte[G::kLoads];
+  __device__ __forceinline__ Ring(char *at) : lds(at) {
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+    for (int k = 0; k < G::kLoads; ++k) G::place((k * kWaves + wave) * kWave + (threadIdx.x & (kWave - 1)), row[k], byte[k]);
+  }
+  template <typename F>
+  __device__ __forceinline__ void ask(int stage, F fetch) {
+#pragma unroll
+    for (int k = 0; k < G::kLoads; ++k)
+      __builtin_amdgcn_global_load_lds(fetch(k, row[k], byte[k]),
+                                       (__attribute__((address_space(3))) void *)(lds + stage * G::kBytes + (k * kWaves + wave) * 1024), 16, 0, 0);
+  }
+  // all but the newest TILES tiles asked for are there, for every wave, and what it read before is in registers
+  template <int TILES>
+  static __device__ __forceinline__ void wait() {
+    constexpr int kCount = TILES * G::kLoads;
+    __builtin_amdgcn_s_waitcnt(0x0070 | (kCount & 15) | (kCount >> 4) << 14);  // vmcnt(kCount) lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  __device__ __forceinline__ void read(u32x4 (&f)[G::kFrags], int stage, const int (&at)[G::kFrags]) const {
+#pragma unroll
+    for (int c = 0; c < G::kFrags; ++c) f[c] = *reinterpret_cast<const u32x4 *>(lds + stage * G::kBytes + at[c]);
+  }
+};
+
+// A lane's fragments of one row.
+template <int F>
+__device__ __forceinline__ void load_row(u32x4 (&f)[F], const char *row, int lane) {
+#pragma unroll
+  for (int c = 0; c < F; ++c) f[c] = *reinterpret_cast<const u32x4 *>(row + 32 * c + 16 * (lane >> 5));
+}
+
+// tile j of the stream is in stage j % kStages; body(stage, j) for all of [first, end), with the next ones asked for meanwhile
+template <typename T, int D, typename F, typename Body>
+__device__ __forceinline__ void run_ring(Ring<T, D> &ring, int first, int end, F ask, Body body) {
+  // (tiles beyond the end are asked for again as the last one, so that as many loads are under way everywhere)
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k) ask(min(first + k, end - 1), k);
+  Ring<T, D>::template wait<kStages - 2>();
+  int stage = 0;
+  for (int j = first; j < end; ++j) {
+    const int free = stage == 0 ? kStages - 1 : stage - 1;
+    ask(min(j + kStages - 1, end - 1), free);
+    body(stage, j);
+    Ring<T, D>::template wait<kStages - 2>();
+    stage = stage == kStages - 1 ? 0 : stage + 1;
+  }
+}
+
+template <typename T, int D, int NS>
+__global__ __launch_bounds__(kThreads, 2) void row_log_kernel(WeightArgs a, WeightLayers L) {
+  typedef Tile<T, D> G;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Unit u = unit_of(a, blockIdx.x);
+  if (!u.valid) return;
+  const int rows = a.rep * u.N, keys = u.P + u.N, e0 = u.w * kWaves * 32 * NS;
+  if (e0 >= rows) return;
+  const int parts = parts_of(a, rows, keys, kWaves * 32 * NS), part = blockIdx.y;
+  if (part >= parts) return;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), e1 = e0 + wave * 32 * NS;
+  const char *q = L.q[u.l] + u.b * a.qs[0], *kc = L.k_cache[u.l] + u.b * a.cs[0] + u.g * a.cs[2], *ks = L.k_suf[u.l] + u.b * a.ks[0] + u.g * a.ks[2];
+
+  u32x4 qf[NS][G::kFrags];
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const int e = min(e1 + 32 * n + (lane & 31), rows - 1), h = e / u.N, i = e - h * u.N;
+    load_row(qf[n], q + i * a.qs[1] + (u.g * a.rep + h) * a.qs[2], lane);
+  }
+  int at[G::kFrags];
+#pragma unroll
+  for (int c = 0; c < G::kFrags; ++c) at[c] = G::frag_at(lane, c);
+
+  Ring<T, D> ring(lds);
+  int from_cache[G::kLoads], from_suffix[G::kLoads];  // within a tile, from its first row
+#pragma unroll
+  for (int k = 0; k < G::kLoads; ++k) {
+    from_cache[k] = ring.row[k] * int(a.cs[1]) + ring.byte[k];
+    from_suffix[k] = ring.row[k] * int(a.ks[1]) + ring.byte[k];
+  }
+  auto ask = [&](int j, int stage) {
+    const int t = 32 * j;
+    if (t + 32 <= u.P) {
+      const char *base = kc + t * a.cs[1];
+      ring.ask(stage, [&](int k, int, int) { return base + from_cache[k]; });
+    } else if (t >= u.P && t + 32 <= keys) {
+      const char *base = ks + (t - u.P) * a.ks[1];
+      ring.ask(stage, [&](int k, int, int) { return base + from_suffix[k]; });
+    } else {
+      ring.ask(stage, [&](int, int row, int byte) {
+        const int r = min(t + row, keys - 1);
+        return (r < u.P ? kc + r * a.cs[1] : ks + (r - u.P) * a.ks[1]) + byte;
+      });
     }
-  float *w = a.weights + ((int64_t(l) * a.B + b) * a.Hkv + g) * a.C + t;
-  *w = t < P && a.decay != 0.f ? a.decay * *w + sum : sum;
+  };
+  const float sc = a.scale * kLog2e;
+  float ref[NS], sum[NS];
+#pragma unroll
+  for (int n = 0; n < NS; ++n) ref[n] = kFarBelow, sum[n] = 0.f;
+  const int tiles = (keys + 31) / 32;
+  const bool live = e1 < rows;
+  run_ring(ring, int(int64_t(tiles) * part / parts), int(int64_t(tiles) * (part + 1) / parts), ask, [&](int stage, int j) {
+    if (!live) return;
+    u32x4 kf[G::kFrags];
+    ring.read(kf, stage, at);
+    f32x16 s[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < G::kFrags; ++c) step(s[n], kf[c], qf[n][c], static_cast<const T *>(nullptr));
+    }
+    if (32 * j + 32 > keys) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[n][r] = 32 * j + product_row(lane, r) < keys ? s[n][r] : -INFINITY;
+    }
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      float top = max3(s[n][0], s[n][1], s[n][2]);
+#pragma unroll
+      for (int r = 3; r < 15; r += 2) top = max3(top, s[n][r], s[n][r + 1]);
+      top = fmaxf(top, s[n][15]) * sc;
+      if (top > ref[n] + 8.f) {  // (seldom: sums of 2^8 at most for each key are far from the end of fp32's range)
+        sum[n] *= __builtin_amdgcn_exp2f(ref[n] - top);
+        ref[n] = top;
+      }
+      float p = 0.f, p2 = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        p += __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], sc, -ref[n]));
+        p2 += __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r + 1], sc, -ref[n]));
+      }
+      sum[n] += p + p2;
+    }
+  });
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // nothing is still on its way into LDS
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const float other = __shfl_xor(ref[n], 32), top = fmaxf(ref[n], other);
+    float all = sum[n] * __builtin_amdgcn_exp2f(ref[n] - top);
+    all += __shfl_xor(all, 32);
+    const int e = e1 + 32 * n + (lane & 31);
+    if (lane < 32 && e < rows)
+      a.row_log[(int64_t(part) * a.units + (u.l * a.B + u.b) * a.Hkv + u.g) * (int64_t(a.rep) * a.S) + e] = top + __builtin_amdgcn_logf(all);
+  }
+}
+
+template <typename T, int D, int NS>
+__global__ __launch_bounds__(kThreads, 2) void key_sum_kernel(WeightArgs a, WeightLayers L, int log_rows) {
+  typedef Tile<T, D> G;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Unit u = unit_of(a, blockIdx.x);
+  if (!u.valid) return;
+  const int rows = a.rep * u.N, keys = u.P + u.N, cols = min(keys, a.C), t0 = u.w * kWaves * 32 * NS;
+  if (rows == 0 || t0 >= cols) return;
+  const int parts = parts_of(a, rows, keys, log_rows);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), t1 = t0 + wave * 32 * NS;
+  const char *q = L.q[u.l] + u.b * a.qs[0] + u.g * a.rep * a.qs[2], *kc = L.k_cache[u.l] + u.b * a.cs[0] + u.g * a.cs[2],
+             *ks = L.k_suf[u.l] + u.b * a.ks[0] + u.g * a.ks[2];
+  float *logs = reinterpret_cast<float *>(lds + kStages * G::kBytes);
+  const float *row_log = a.row_log + ((u.l * a.B + u.b) * a.Hkv + u.g) * (int64_t(a.rep) * a.S);
+  const int64_t part_stride = int64_t(a.units) * a.rep * a.S;
+
+  u32x4 kf[NS][G::kFrags];
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const int t = min(t1 + 32 * n + (lane & 31), cols - 1);
+    load_row(kf[n], t < u.P ? kc + t * a.cs[1] : ks + (t - u.P) * a.ks[1], lane);
+  }
+  int at[G::kFrags];
+#pragma unroll
+  for (int c = 0; c < G::kFrags; ++c) at[c] = G::frag_at(lane, c);
+  const float sc = a.scale * kLog2e;
+  const bool live = t1 < cols;
+  f32x16 mass[NS];
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mass[n][r] = 0.f;
+
+  Ring<T, D> ring(lds);
+  // entry e + 32 is `down` rows and `over` heads on from entry e, or one head more and N rows less
+  const int over = 32 / u.N, down = 32 - over * u.N;
+  for (int chunk = 0; chunk < rows; chunk += kLogs) {
+    const int here = min(rows - chunk, kLogs), padded = (here + 31) & ~31;
+    if (chunk > 0) __syncthreads();
+    for (int e = threadIdx.x; e < padded; e += kThreads) {
+      float x = INFINITY;  // rows that are not there: probability 0
+      if (e < here) {
+        x = row_log[chunk + e];
+        if (parts > 1) {
+          float top = x, sum = 0.f;
+          for (int p = 1; p < parts; ++p) top = fmaxf(top, row_log[p * part_stride + chunk + e]);
+          for (int p = 0; p < parts; ++p) sum += __builtin_amdgcn_exp2f(row_log[p * part_stride + chunk + e] - top);
+          x = top + __builtin_amdgcn_logf(sum);
+        }
+      }
+      logs[e] = x;
+    }
+    int head[G::kLoads], pos[G::kLoads];  // of the entries that this lane asks for
+#pragma unroll
+    for (int k = 0; k < G::kLoads; ++k) {
+      head[k] = (chunk + ring.row[k]) / u.N;
+      pos[k] = chunk + ring.row[k] - head[k] * u.N;
+    }
+    const int tiles = padded / 32;
+    int asked = 0;
+    auto ask = [&](int j, int stage) {
+      ring.ask(stage, [&](int k, int, int byte) {
+        const bool there = head[k] < a.rep;  // (an entry behind the last one: some row)
+        return q + (there ? pos[k] : 0) * a.qs[1] + (there ? head[k] : 0) * a.qs[2] + byte;
+      });
+      if (j == asked) {  // (uniform: not where the last tile is asked for again)
+        ++asked;
+#pragma unroll
+        for (int k = 0; k < G::kLoads; ++k) {
+          pos[k] += down;
+          head[k] += over;
+          if (pos[k] >= u.N) pos[k] -= u.N, ++head[k];
+        }
+      }
+    };
+    __syncthreads();  // (the logarithms are there)
+    run_ring(ring, 0, tiles, ask, [&](int stage, int j) {
+      if (!live) return;
+      u32x4 qf[G::kFrags];
+      ring.read(qf, stage, at);
+      const float log = logs[32 * j + (lane & 31)];
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        f32x16 s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < G::kFrags; ++c) step(s, kf[n][c], qf[c], static_cast<const T *>(nullptr));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mass[n][r] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -log));
+      }
+    });
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // nothing is still on its way into LDS
+  }
+  // over the 32 lanes that hold the same keys
+  float *w = a.weights + ((u.l * a.B + u.b) * int64_t(a.Hkv) + u.g) * a.C;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float x = mass[n][r];
+#pragma unroll
+      for (int m = 1; m < 32; m <<= 1) x += __shfl_xor(x, m);
+      const int t = t1 + 32 * n + product_row(lane, r);
+      if ((lane & 31) == r && t < cols) w[t] = t < u.P && a.decay != 0.f ? __builtin_fmaf(a.decay, w[t], x) : x;
+    }
 }
 
 int layers_at_once(int32_t n) { return n < kMaxAttnLayers ? n : kMaxAttnLayers; }
+int max_parts(const lsp_attn_desc *d, int32_t num_layers) {
+  const int64_t units = int64_t(layers_at_once(num_layers)) * d->B * d->Hkv, keys = (int64_t(d->C) + d->S) / kPartKeys;
+  const int64_t n = units < kEnough ? kEnough / units : 1;
+  return int(n < keys ? (n < kMaxParts ? n : kMaxParts) : (keys < 1 ? 1 : keys < kMaxParts ? keys : kMaxParts));
+}
 size_t row_log_bytes(const lsp_attn_desc *d, int32_t num_layers) {
-  return size_t(layers_at_once(num_layers)) * d->B * d->Hq * d->S * sizeof(float);
+  return size_t(max_parts(d, num_layers)) * layers_at_once(num_layers) * d->B * d->Hq * d->S * sizeof(float);
+}
+
+template <typename T, int D>
+int32_t launch(WeightArgs a, const WeightLayers &L, hipStream_t st) {
+  constexpr int kMost = D * sizeof(T) == 512 ? 1 : 2;  // (512-byte rows: 64 registers a block)
+  constexpr int kRing = kStages * Tile<T, D>::kBytes, kLds = kRing + kLogs * int(sizeof(float));
+  static std::atomic<uint64_t> done[4];
+  auto start = [&](auto kernel, std::atomic<uint64_t> &mark, int ns, int64_t length, int bytes, int parts, auto... more) -> int32_t {
+    const int32_t rc = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), bytes, mark, "lsp_attn_key_weights");
+    if (rc != LSP_OK) return rc;
+    a.tiles = int((length + 32 * ns * kWaves - 1) / (32 * ns * kWaves));
+    const int64_t grid = place_grid(a);
+    if (grid > (int64_t(1) << 23)) {
+      set_error("lsp_attn_key_weights: %lld workgroups are too many", (long long)grid);
+      return LSP_ERR_UNSUPPORTED;
+    }
+    kernel<<<dim3(unsigned(grid), parts), kThreads, bytes, st>>>(a, L, more...);
+    LSP_CHECK_LAUNCH("lsp_attn_key_weights: launch");
+    return LSP_OK;
+  };
+  // two blocks of 32 to a wave where that leaves two workgroups to a compute unit
+  const int64_t rows = int64_t(a.rep) * a.S, cols = a.C;
+  const bool two_rows = kMost == 2 && a.units * ((rows + 255) / 256) >= kEnough, two_cols = kMost == 2 && a.units * ((cols + 255) / 256) >= kEnough;
+  const int log_rows = 32 * kWaves * (two_rows ? 2 : 1);
+  const int32_t rc = two_rows ? start(row_log_kernel<T, D, kMost>, done[0], 2, rows, kRing, a.max_parts)
+                              : start(row_log_kernel<T, D, 1>, done[1], 1, rows, kRing, a.max_parts);
+  if (rc != LSP_OK) return rc;
+  return two_cols ? start(key_sum_kernel<T, D, kMost>, done[2], 2, cols, kLds, 1, log_rows) : start(key_sum_kernel<T, D, 1>, done[3], 1, cols, kLds, 1, log_rows);
 }
 
 }  // namespace
 }  // namespace lsp
 
 extern "C" size_t lsp_attn_key_weights_workspace_bytes(const lsp_attn_desc *d, int32_t num_layers) {
-  if (d == nullptr || num_layers <= 0 || d->B <= 0 || d->S <= 0 || d->Hq <= 0) return 0;
+  if (d == nullptr || num_layers <= 0 || d->B <= 0 || d->S <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->C <= 0) return 0;
   return lsp::row_log_bytes(d, num_layers);
 }
 
@@ -117,29 +466,29 @@ extern "C" int32_t lsp_attn_key_weights(const lsp_attn_desc *d, int32_t num_laye
     set_error("lsp_attn_key_weights: workspace of %zu bytes (16-byte aligned) required, got %zu", need, workspace_bytes);
     return LSP_ERR_WORKSPACE;
   }
-  WeightArgs a = {prefix_len, suffix_len, at.B, at.S, at.Hq, at.Hkv, at.D, at.C, at.Hq / at.Hkv, at.scale, decay, {}, {}, {}, static_cast<float *>(workspace), weights};
-  for (int k = 0; k < 3; ++k) a.qs[k] = at.qs[k], a.ks[k] = at.ks[k], a.cs[k] = at.cs[k];
+  WeightArgs a = {};
+  a.prefix_len = prefix_len; a.suffix_len = suffix_len;
+  a.B = at.B; a.S = at.S; a.Hq = at.Hq; a.Hkv = at.Hkv; a.D = at.D; a.C = at.C; a.rep = at.Hq / at.Hkv;
+  a.scale = at.scale; a.decay = decay;
+  const int64_t es = int64_t(elem_size(d->dtype));
+  for (int k = 0; k < 3; ++k) a.qs[k] = at.qs[k] * es, a.ks[k] = at.ks[k] * es, a.cs[k] = at.cs[k] * es;
+  a.row_log = static_cast<float *>(workspace);
+  a.max_parts = max_parts(d, num_layers);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int keys = at.C;
   for (int l0 = 0; l0 < num_layers; l0 += kMaxAttnLayers) {
-    const int nl = layers_at_once(num_layers - l0);
+    a.layers = layers_at_once(num_layers - l0);
+    a.units = a.layers * a.B * a.Hkv;
     WeightLayers L;
     for (int l = 0; l < kMaxAttnLayers; ++l) {
-      const int s = l < nl ? l0 + l : l0;
-      L.q[l] = q_layers[s]; L.k_suf[l] = k_suf_layers[s]; L.k_cache[l] = k_cache_layers[s];
+      const int s = l < a.layers ? l0 + l : l0;  // unused slots repeat a valid layer
+      L.q[l] = static_cast<const char *>(q_layers[s]);
+      L.k_suf[l] = static_cast<const char *>(k_suf_layers[s]);
+      L.k_cache[l] = static_cast<const char *>(k_cache_layers[s]);
     }
     a.weights = weights + int64_t(l0) * at.B * at.Hkv * at.C;
-    const dim3 rows(at.S, at.B * at.Hq, nl), cols((keys + kWave - 1) / kWave, at.B * at.Hkv, nl);
-    if (d->dtype == LSP_BF16) {
-      row_log_kernel<uint16_t><<<rows, kWave, 0, st>>>(a, L);
-      LSP_CHECK_LAUNCH("lsp_attn_key_weights: row launch");
-      key_sum_kernel<uint16_t><<<cols, kWave, 0, st>>>(a, L);
-    } else {
-      row_log_kernel<float><<<rows, kWave, 0, st>>>(a, L);
-      LSP_CHECK_LAUNCH("lsp_attn_key_weights: row launch");
-      key_sum_kernel<float><<<cols, kWave, 0, st>>>(a, L);
-    }
-    LSP_CHECK_LAUNCH("lsp_attn_key_weights: column launch");
+    const int32_t r = d->dtype == LSP_BF16 ? (d->D == 64 ? launch<uint16_t, 64>(a, L, st) : launch<uint16_t, 128>(a, L, st))
+                                           : (d->D == 64 ? launch<float, 64>(a, L, st) : launch<float, 128>(a, L, st));
+    if (r != LSP_OK) return r;
   }
   return LSP_OK;
 }
