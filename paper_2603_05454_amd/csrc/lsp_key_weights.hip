@@ -94,6 +94,25 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// Sum over lane % 32 of 16 numbers: lane l gets the one with number l % 16.  Every step halves what a lane has to send: the partner is the
+// mirror image within 16, 8, 4 and 2 lanes, so that it agrees in the bits that earlier steps went by (46 instructions, 80 for each by itself).
+template <int CTRL, int HALF>
+__device__ __forceinline__ void fold(float (&x)[16], int lane) {
+  const bool upper = lane & HALF;
+#pragma unroll
+  for (int r = 0; r < HALF; ++r) {
+    const float keep = upper ? x[r + HALF] : x[r], send = upper ? x[r] : x[r + HALF];
+    x[r] = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), CTRL, 0xf, 0xf, true));
+  }
+}
+__device__ __forceinline__ float sum_of_lanes(float (&x)[16], int lane) {
+  fold<0x140, 8>(x, lane);  // row_mirror
+  fold<0x141, 4>(x, lane);  // row_half_mirror
+  fold<0x1b, 2>(x, lane);   // quad_perm [3,2,1,0]
+  fold<0xb1, 1>(x, lane);   // quad_perm [1,0,3,2]
+  return x[0] + __shfl_xor(x[0], 16);
+}
+
 struct Unit {
   int l, b, g, w, N, P;
   bool valid;
@@ -127,6 +146,20 @@ __device__ __forceinline__ int parts_of(const WeightArgs &a, int rows, int keys,
   if (a.max_parts == 1 || rows > kLogs) return 1;
   const int groups = a.units * ((rows + rows_of_group - 1) / rows_of_group);
   return max(1, min(min(kEnough / groups, a.max_parts), keys / kPartKeys));
+}
+
+// Which units few_rows_kernel takes; the other two leave these alone.
+constexpr int kFewWaves = 8;
+template <int RS>
+constexpr int kFewTiles = RS == 1 ? 8 : 4;  // a wave's: 128 registers of scores
+template <typename T, int D>
+constexpr bool kHasFew = Tile<T, D>::kRowBytes <= 256;
+template <int RS>
+__host__ __device__ constexpr int few_keys() { return kFewWaves * 32 * kFewTiles<RS>; }
+// blocks of 32 rows (0: too many, or too many keys)
+template <typename T, int D>
+__host__ __device__ constexpr int few_rows(int64_t rows, int64_t keys) {
+  return !kHasFew<T, D> ? 0 : rows <= 32 && keys <= few_keys<1>() ? 1 : rows <= 64 && keys <= few_keys<2>() ? 2 : 0;
 }
 
 // A ring of tiles.  fetch(tile, place's row, place's byte) says where a lane's 16 bytes are.
@@ -193,7 +226,7 @@ __global__ __launch_bounds__(kThreads, 2) void row_log_kernel(WeightArgs a, Weig
   const Unit u = unit_of(a, blockIdx.x);
   if (!u.valid) return;
   const int rows = a.rep * u.N, keys = u.P + u.N, e0 = u.w * kWaves * 32 * NS;
-  if (e0 >= rows) return;
+  if (e0 >= rows || few_rows<T, D>(rows, keys)) return;
   const int parts = parts_of(a, rows, keys, kWaves * 32 * NS), part = blockIdx.y;
   if (part >= parts) return;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), e1 = e0 + wave * 32 * NS;
@@ -286,6 +319,12 @@ __global__ __launch_bounds__(kThreads, 2) void row_log_kernel(WeightArgs a, Weig
   }
 }
 
+// Lanes with l % 32 < 16 have a key's mass.
+__device__ __forceinline__ void store_mass(const WeightArgs &a, float *w, int t, int cols, int P, float mass, int lane) {
+  if ((lane & 16) || t >= cols) return;
+  w[t] = t < P && a.decay != 0.f ? __builtin_fmaf(a.decay, w[t], mass) : mass;
+}
+
 template <typename T, int D, int NS>
 __global__ __launch_bounds__(kThreads, 2) void key_sum_kernel(WeightArgs a, WeightLayers L, int log_rows) {
   typedef Tile<T, D> G;
@@ -293,7 +332,7 @@ __global__ __launch_bounds__(kThreads, 2) void key_sum_kernel(WeightArgs a, Weig
   const Unit u = unit_of(a, blockIdx.x);
   if (!u.valid) return;
   const int rows = a.rep * u.N, keys = u.P + u.N, cols = min(keys, a.C), t0 = u.w * kWaves * 32 * NS;
-  if (rows == 0 || t0 >= cols) return;
+  if (rows == 0 || t0 >= cols || few_rows<T, D>(rows, keys)) return;
   const int parts = parts_of(a, rows, keys, log_rows);
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), t1 = t0 + wave * 32 * NS;
   const char *q = L.q[u.l] + u.b * a.qs[0] + u.g * a.rep * a.qs[2], *kc = L.k_cache[u.l] + u.b * a.cs[0] + u.g * a.cs[2],
@@ -383,15 +422,142 @@ __global__ __launch_bounds__(kThreads, 2) void key_sum_kernel(WeightArgs a, Weig
   // over the 32 lanes that hold the same keys
   float *w = a.weights + ((u.l * a.B + u.b) * int64_t(a.Hkv) + u.g) * a.C;
 #pragma unroll
-  for (int n = 0; n < NS; ++n)
+  for (int n = 0; n < NS; ++n) {
+    float x[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      float x = mass[n][r];
+    for (int r = 0; r < 16; ++r) x[r] = mass[n][r];
+    store_mass(a, w, t1 + 32 * n + product_row(lane, lane & 15), cols, u.P, sum_of_lanes(x, lane), lane);
+  }
+}
+
+// Few rows: all of a unit's scores are kept in registers, so that K is read once and every score and exponential computed once.  The rows
+// (32 RS of them at most) are every wave's; the waves share the keys, in tiles of 32 that each fetches for itself, two ahead.  Maxima and sums of
+// the rows meet in LDS.
+template <typename T, int D>
+constexpr int kFewStages = Tile<T, D>::kRowBytes == 128 ? 4 : 2;
+
+template <typename T, int D, int RS>
+__device__ __forceinline__ void few_rows_body(const WeightArgs &a, const WeightLayers &L, const Unit &u, char *lds) {
+  typedef Tile<T, D> G;
+  constexpr int kLoads = G::kBytes / 1024, kStages2 = kFewStages<T, D>, kTiles = kFewTiles<RS>;
+  __shared__ float s_row[2][kFewWaves][32 * RS];
+  const int rows = a.rep * u.N, keys = u.P + u.N, tiles = (keys + 31) / 32, cols = min(keys, a.C);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const char *q = L.q[u.l] + u.b * a.qs[0], *kc = L.k_cache[u.l] + u.b * a.cs[0] + u.g * a.cs[2], *ks = L.k_suf[u.l] + u.b * a.ks[0] + u.g * a.ks[2];
+  char *own = lds + wave * kStages2 * G::kBytes;
+  auto ask = [&](int j, int stage) {
 #pragma unroll
-      for (int m = 1; m < 32; m <<= 1) x += __shfl_xor(x, m);
-      const int t = t1 + 32 * n + product_row(lane, r);
-      if ((lane & 31) == r && t < cols) w[t] = t < u.P && a.decay != 0.f ? __builtin_fmaf(a.decay, w[t], x) : x;
+    for (int k = 0; k < kLoads; ++k) {
+      int row, byte;
+      G::place(k * kWave + lane, row, byte);
+      const int t = min(32 * j + row, keys - 1);
+      __builtin_amdgcn_global_load_lds((t < u.P ? kc + t * a.cs[1] : ks + (t - u.P) * a.ks[1]) + byte,
+                                       (__attribute__((address_space(3))) void *)(own + stage * G::kBytes + k * 1024), 16, 0, 0);
     }
+  };
+  u32x4 qf[RS][G::kFrags];
+#pragma unroll
+  for (int n = 0; n < RS; ++n) {
+    const int e = min(32 * n + (lane & 31), rows - 1), h = e / u.N, i = e - h * u.N;
+    load_row(qf[n], q + i * a.qs[1] + (u.g * a.rep + h) * a.qs[2], lane);
+  }
+#pragma unroll
+  for (int k = 0; k < kStages2; ++k)
+    if (wave + k * kFewWaves < tiles) ask(wave + k * kFewWaves, k);
+
+  f32x16 s[kTiles][RS];
+  float top[RS];
+#pragma unroll
+  for (int n = 0; n < RS; ++n) top[n] = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kTiles; ++k) {
+    const int j = wave + k * kFewWaves;
+    if (j < tiles) {
+      const int stage = k % kStages2;
+      // the newer tiles that were asked for may be under way
+      if (kStages2 == 4 && j + 3 * kFewWaves < tiles) __builtin_amdgcn_s_waitcnt(0x0F70 | 3 * kLoads);
+      else if (kStages2 == 2 && j + kFewWaves < tiles) __builtin_amdgcn_s_waitcnt(0x0F70 | kLoads);
+      else __builtin_amdgcn_s_waitcnt(0x0F70);
+      asm volatile("" ::: "memory");
+      u32x4 kf[G::kFrags];
+#pragma unroll
+      for (int c = 0; c < G::kFrags; ++c) kf[c] = *reinterpret_cast<const u32x4 *>(own + stage * G::kBytes + G::frag_at(lane, c));
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage may be written again
+      asm volatile("" ::: "memory");
+      if (k + kStages2 < kTiles && j + kStages2 * kFewWaves < tiles) ask(j + kStages2 * kFewWaves, stage);
+#pragma unroll
+      for (int n = 0; n < RS; ++n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[k][n][r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < G::kFrags; ++c) step(s[k][n], kf[c], qf[n][c], static_cast<const T *>(nullptr));
+        if (32 * j + 32 > keys) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[k][n][r] = 32 * j + product_row(lane, r) < keys ? s[k][n][r] : -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) top[n] = max3(top[n], s[k][n][r], s[k][n][r + 1]);
+      }
+    }
+  }
+  // of each row over all waves; lanes l and l + 32 have the same row
+  auto over_waves = [&](int slot, float (&x)[RS], auto op) {
+#pragma unroll
+    for (int n = 0; n < RS; ++n) {
+      x[n] = op(x[n], __shfl_xor(x[n], 32));
+      if (lane < 32) s_row[slot][wave][32 * n + lane] = x[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < RS; ++n) {
+      x[n] = s_row[slot][0][32 * n + (lane & 31)];
+#pragma unroll
+      for (int w = 1; w < kFewWaves; ++w) x[n] = op(x[n], s_row[slot][w][32 * n + (lane & 31)]);
+    }
+  };
+  over_waves(0, top, [](float x, float y) { return fmaxf(x, y); });
+  const float sc = a.scale * kLog2e;
+  float sum[RS];
+#pragma unroll
+  for (int n = 0; n < RS; ++n) sum[n] = 0.f;
+#pragma unroll
+  for (int k = 0; k < kTiles; ++k)
+    if (wave + k * kFewWaves < tiles) {
+#pragma unroll
+      for (int n = 0; n < RS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[k][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][n][r], sc, -top[n] * sc));
+          sum[n] += s[k][n][r];
+        }
+    }
+  over_waves(1, sum, [](float x, float y) { return x + y; });
+#pragma unroll
+  for (int n = 0; n < RS; ++n) sum[n] = 32 * n + (lane & 31) < rows ? 1.f / sum[n] : 0.f;
+  float *w = a.weights + ((u.l * a.B + u.b) * int64_t(a.Hkv) + u.g) * a.C;
+#pragma unroll
+  for (int k = 0; k < kTiles; ++k) {
+    const int j = wave + k * kFewWaves;
+    if (j < tiles) {
+      float x[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = s[k][0][r] * sum[0];
+        if (RS == 2) x[r] = __builtin_fmaf(s[k][RS - 1][r], sum[RS - 1], x[r]);
+      }
+      store_mass(a, w, 32 * j + product_row(lane, lane & 15), cols, u.P, sum_of_lanes(x, lane), lane);
+    }
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void few_rows_kernel(WeightArgs a, WeightLayers L) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Unit u = unit_of(a, blockIdx.x);
+  if (!u.valid || u.N == 0) return;
+  const int blocks = few_rows<T, D>(a.rep * int64_t(u.N), u.P + u.N);
+  if (blocks == 1) few_rows_body<T, D, 1>(a, L, u, lds);
+  else if (blocks == 2) few_rows_body<T, D, 2>(a, L, u, lds);
 }
 
 int layers_at_once(int32_t n) { return n < kMaxAttnLayers ? n : kMaxAttnLayers; }
@@ -408,28 +574,36 @@ template <typename T, int D>
 int32_t launch(WeightArgs a, const WeightLayers &L, hipStream_t st) {
   constexpr int kMost = D * sizeof(T) == 512 ? 1 : 2;  // (512-byte rows: 64 registers a block)
   constexpr int kRing = kStages * Tile<T, D>::kBytes, kLds = kRing + kLogs * int(sizeof(float));
-  static std::atomic<uint64_t> done[4];
-  auto start = [&](auto kernel, std::atomic<uint64_t> &mark, int ns, int64_t length, int bytes, int parts, auto... more) -> int32_t {
+  static std::atomic<uint64_t> done[5];
+  auto start = [&](auto kernel, std::atomic<uint64_t> &mark, int threads, int64_t tiles, int bytes, int parts, auto... more) -> int32_t {
     const int32_t rc = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), bytes, mark, "lsp_attn_key_weights");
     if (rc != LSP_OK) return rc;
-    a.tiles = int((length + 32 * ns * kWaves - 1) / (32 * ns * kWaves));
+    a.tiles = int(tiles);
     const int64_t grid = place_grid(a);
     if (grid > (int64_t(1) << 23)) {
       set_error("lsp_attn_key_weights: %lld workgroups are too many", (long long)grid);
       return LSP_ERR_UNSUPPORTED;
     }
-    kernel<<<dim3(unsigned(grid), parts), kThreads, bytes, st>>>(a, L, more...);
+    kernel<<<dim3(unsigned(grid), parts), threads, bytes, st>>>(a, L, more...);
     LSP_CHECK_LAUNCH("lsp_attn_key_weights: launch");
     return LSP_OK;
   };
-  // two blocks of 32 to a wave where that leaves two workgroups to a compute unit
   const int64_t rows = int64_t(a.rep) * a.S, cols = a.C;
-  const bool two_rows = kMost == 2 && a.units * ((rows + 255) / 256) >= kEnough, two_cols = kMost == 2 && a.units * ((cols + 255) / 256) >= kEnough;
-  const int log_rows = 32 * kWaves * (two_rows ? 2 : 1);
-  const int32_t rc = two_rows ? start(row_log_kernel<T, D, kMost>, done[0], 2, rows, kRing, a.max_parts)
-                              : start(row_log_kernel<T, D, 1>, done[1], 1, rows, kRing, a.max_parts);
+  if constexpr (kHasFew<T, D>) {
+    constexpr int kBytes = kFewWaves * kFewStages<T, D> * Tile<T, D>::kBytes;
+    const int32_t rc = start(few_rows_kernel<T, D>, done[4], kFewWaves * kWave, 1, kBytes, 1);
+    if (rc != LSP_OK) return rc;
+    if (few_rows<T, D>(rows, cols + a.S)) return LSP_OK;  // whatever the lengths
+  }
+  // two blocks of 32 to a wave where that leaves two workgroups to a compute unit
+  auto groups = [](int64_t n, int ns) { return (n + 32 * ns * kWaves - 1) / (32 * ns * kWaves); };
+  const int row_blocks = kMost == 2 && a.units * groups(rows, 2) >= kEnough ? 2 : 1, col_blocks = kMost == 2 && a.units * groups(cols, 2) >= kEnough ? 2 : 1;
+  const int log_rows = 32 * kWaves * row_blocks;
+  const int32_t rc = row_blocks == 2 ? start(row_log_kernel<T, D, kMost>, done[0], kThreads, groups(rows, 2), kRing, a.max_parts)
+                                     : start(row_log_kernel<T, D, 1>, done[1], kThreads, groups(rows, 1), kRing, a.max_parts);
   if (rc != LSP_OK) return rc;
-  return two_cols ? start(key_sum_kernel<T, D, kMost>, done[2], 2, cols, kLds, 1, log_rows) : start(key_sum_kernel<T, D, 1>, done[3], 1, cols, kLds, 1, log_rows);
+  return col_blocks == 2 ? start(key_sum_kernel<T, D, kMost>, done[2], kThreads, groups(cols, 2), kLds, 1, log_rows)
+                         : start(key_sum_kernel<T, D, 1>, done[3], kThreads, groups(cols, 1), kLds, 1, log_rows);
 }
 
 }  // namespace
