@@ -14,6 +14,8 @@
 // Everything is summed in fp32, in an order that sizes alone decide.
 #include <math.h>
 
+#include <type_traits>
+
 #include "lsp_attn.h"
 
 namespace lsp {
@@ -27,7 +29,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-constexpr int kStages = 4;           // of the ring: the tile in use, two that are on their way or there, one that is being asked for
+constexpr int kStages = 4;           // of the ring
 constexpr int kLogs = 4096;          // rows whose L are in LDS at a time
 constexpr int kMaxParts = 16;        // of the keys, where rows are few
 constexpr int kPartKeys = 128;       // a part has at least
@@ -112,6 +114,9 @@ __device__ __forceinline__ float sum_of_lanes(float (&x)[16], int lane) {
   fold<0xb1, 1>(x, lane);   // quad_perm [1,0,3,2]
   return x[0] + __shfl_xor(x[0], 16);
 }
+
+// The compiler may not put off what makes x to behind a later branch, away from the matrix instructions it is meant to run beside.
+__device__ __forceinline__ void stays_here(float &x) { asm volatile("" : "+v"(x)); }
 
 struct Unit {
   int l, b, g, w, N, P;
@@ -202,21 +207,102 @@ __device__ __forceinline__ void load_row(u32x4 (&f)[F], const char *row, int lan
   for (int c = 0; c < F; ++c) f[c] = *reinterpret_cast<const u32x4 *>(row + 32 * c + 16 * (lane >> 5));
 }
 
-// tile j of the stream is in stage j % kStages; body(stage, j) for all of [first, end), with the next ones asked for meanwhile
-template <typename T, int D, typename F, typename Body>
-__device__ __forceinline__ void run_ring(Ring<T, D> &ring, int first, int end, F ask, Body body) {
+// The wave's NS blocks (`own`) times each of the tiles [first, end) of the stream, one product behind the other: while the matrix cores make one,
+// the vector units use the one before.  Tile j + 1 is read from the ring at the start of tile j's last product, so that its barrier is also the one
+// behind which tile j's stage is free.
+// begin(parity of a tile, tile) comes before a tile's first product.  Of a product, with its block and its tile, the next one's first half goes by
+// ready() (READY) and its second half, or all of it, by use(product, block, parity, first, end): numbers [first, end) of 16.
+// STREAM_ROWS: the products' rows are the stream's (its columns otherwise).
+template <bool STREAM_ROWS, bool READY, typename T, int D, int NS, typename Ask, typename Begin, typename Ready, typename Use>
+__device__ __forceinline__ void run_pipeline(Ring<T, D> &ring, int first, int end, const int (&at)[Tile<T, D>::kFrags], bool live,
+                                             const u32x4 (&own)[NS][Tile<T, D>::kFrags], float nothing, Ask ask, Begin begin, Ready ready, Use use) {
+  typedef Tile<T, D> G;
+  constexpr int F = G::kFrags;
   // (tiles beyond the end are asked for again as the last one, so that as many loads are under way everywhere)
 #pragma unroll
-  for (int k = 0; k < kStages - 1; ++k) ask(min(first + k, end - 1), k);
-  Ring<T, D>::template wait<kStages - 2>();
-  int stage = 0;
-  for (int j = first; j < end; ++j) {
-    const int free = stage == 0 ? kStages - 1 : stage - 1;
-    ask(min(j + kStages - 1, end - 1), free);
-    body(stage, j);
+  for (int k = 0; k < kStages; ++k) ask(min(first + k, end - 1), k);
+  Ring<T, D>::template wait<kStages - 1>();
+  auto next = [&](int j, int stage) {  // tile j + 1 is there, tile j's stage takes tile j + kStages
     Ring<T, D>::template wait<kStages - 2>();
-    stage = stage == kStages - 1 ? 0 : stage + 1;
+    ask(min(j + kStages, end - 1), stage);
+  };
+  if (!live) {
+    for (int j = first, stage = 0; j < end; ++j, stage = (stage + 1) % kStages) next(j, stage);
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    return;
   }
+  constexpr bool kAhead = G::kRowBytes < 512;  // (there are no registers for two tiles of these)
+  u32x4 x[kAhead ? 2 : 1][F];
+  f32x16 s[2];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[1][r] = nothing;
+  ring.read(x[0], 0, at);
+  auto tile = [&](int j, auto place) {
+    constexpr int kStage = decltype(place)::value, P = kStage & 1;
+    begin(P, j);
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      if (kAhead && n == NS - 1) {
+        next(j, kStage);
+        ring.read(x[1 - P], (kStage + 1) % kStages, at);
+      }
+      // (the product before: block `before` of this tile or the one before)
+      const int cur = NS == 2 ? n : P, before = NS == 2 ? 1 - n : 0, its_parity = NS == 2 && n == 1 ? P : 1 - P;
+      f32x16 &now = s[cur], &old = s[1 - cur];
+      auto make = [&](int c) {
+        if (STREAM_ROWS) step(now, x[kAhead ? P : 0][c], own[n][c], static_cast<const T *>(nullptr));
+        else step(now, own[n][c], x[kAhead ? P : 0][c], static_cast<const T *>(nullptr));
+      };
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) now[r] = 0.f;
+      constexpr int kFrom = READY ? F / 2 : 0, kEach = 16 / (F - kFrom), kMatrix = sizeof(T) == 2 ? 1 : 4;
+#pragma unroll
+      for (int c = 0; c < kFrom; ++c) make(c);
+      if (READY) ready(old, before, NS == 2 && n == 1 ? j : j - 1);
+#pragma unroll
+      for (int c = kFrom; c < F; ++c) {
+        make(c);
+        use(old, before, its_parity, (c - kFrom) * kEach, (c - kFrom + 1) * kEach);
+      }
+      // matrix, vector and exponential instructions in turn
+#pragma unroll
+      for (int c = kFrom; c < F; ++c) {
+        __builtin_amdgcn_sched_group_barrier(0x008, kMatrix, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, kEach + 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, kEach, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, kEach, 0);
+      }
+    }
+    if (!kAhead) {
+      next(j, kStage);
+      ring.read(x[0], (kStage + 1) % kStages, at);
+    }
+  };
+  static_assert(kStages == 4, "a round of the loop");
+  for (int j = first;; j += kStages) {
+    tile(j, std::integral_constant<int, 0>());
+    if (j + 1 == end) break;
+    tile(j + 1, std::integral_constant<int, 1>());
+    if (j + 2 == end) break;
+    tile(j + 2, std::integral_constant<int, 2>());
+    if (j + 3 == end) break;
+    tile(j + 3, std::integral_constant<int, 3>());
+    if (j + 4 == end) break;
+  }
+  const bool last_is_even = (end - first) & 1;
+  // the last product
+  auto finish = [&](f32x16 &last, int parity) {
+    if (READY) ready(last, NS - 1, end - 1);
+    use(last, NS - 1, parity, 0, 16);
+  };
+  if (NS == 2) {
+    if (last_is_even) finish(s[1], 0); else finish(s[1], 1);
+  } else {
+    if (last_is_even) finish(s[0], 0); else finish(s[1], 1);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // nothing is still on its way into LDS
 }
 
 template <typename T, int D, int NS>
@@ -265,53 +351,41 @@ __global__ __launch_bounds__(kThreads, 2) void row_log_kernel(WeightArgs a, Weig
     }
   };
   const float sc = a.scale * kLog2e;
-  float ref[NS], sum[NS];
+  float ref[NS], sum[NS], sum2[NS];  // (two chains of additions)
 #pragma unroll
-  for (int n = 0; n < NS; ++n) ref[n] = kFarBelow, sum[n] = 0.f;
+  for (int n = 0; n < NS; ++n) ref[n] = kFarBelow, sum[n] = sum2[n] = 0.f;
   const int tiles = (keys + 31) / 32;
-  const bool live = e1 < rows;
-  run_ring(ring, int(int64_t(tiles) * part / parts), int(int64_t(tiles) * (part + 1) / parts), ask, [&](int stage, int j) {
-    if (!live) return;
-    u32x4 kf[G::kFrags];
-    ring.read(kf, stage, at);
-    f32x16 s[NS];
+  run_pipeline<true, true, T, D, NS>(
+      ring, int(int64_t(tiles) * part / parts), int(int64_t(tiles) * (part + 1) / parts), at, e1 < rows, qf, -INFINITY, ask, [](int, int) {},
+      [&](f32x16 &s, int n, int j) {
+        if (32 * j + 32 > keys) {
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
+          for (int r = 0; r < 16; ++r) s[r] = 32 * j + product_row(lane, r) < keys ? s[r] : -INFINITY;
+        }
+        float top = max3(s[0], s[1], s[2]);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+        for (int r = 3; r < 15; r += 2) top = max3(top, s[r], s[r + 1]);
+        top = fmaxf(top, s[15]) * sc;
+        if (__any(top > ref[n] + 8.f)) {  // (seldom: sums of 2^8 at most for each key are far from the end of fp32's range)
+          const float to = fmaxf(top, ref[n]);
+          const float f = __builtin_amdgcn_exp2f(ref[n] - to);
+          sum[n] *= f;
+          sum2[n] *= f;
+          ref[n] = to;
+        }
+      },
+      [&](const f32x16 &s, int n, int, int r0, int r1) {
 #pragma unroll
-      for (int c = 0; c < G::kFrags; ++c) step(s[n], kf[c], qf[n][c], static_cast<const T *>(nullptr));
-    }
-    if (32 * j + 32 > keys) {
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] = 32 * j + product_row(lane, r) < keys ? s[n][r] : -INFINITY;
-    }
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      float top = max3(s[n][0], s[n][1], s[n][2]);
-#pragma unroll
-      for (int r = 3; r < 15; r += 2) top = max3(top, s[n][r], s[n][r + 1]);
-      top = fmaxf(top, s[n][15]) * sc;
-      if (top > ref[n] + 8.f) {  // (seldom: sums of 2^8 at most for each key are far from the end of fp32's range)
-        sum[n] *= __builtin_amdgcn_exp2f(ref[n] - top);
-        ref[n] = top;
-      }
-      float p = 0.f, p2 = 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        p += __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], sc, -ref[n]));
-        p2 += __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r + 1], sc, -ref[n]));
-      }
-      sum[n] += p + p2;
-    }
-  });
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // nothing is still on its way into LDS
+        for (int r = r0; r < r1; ++r) {
+          float &to = r & 1 ? sum[n] : sum2[n];
+          to += __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -ref[n]));
+          stays_here(to);
+        }
+      });
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
     const float other = __shfl_xor(ref[n], 32), top = fmaxf(ref[n], other);
-    float all = sum[n] * __builtin_amdgcn_exp2f(ref[n] - top);
+    float all = (sum[n] + sum2[n]) * __builtin_amdgcn_exp2f(ref[n] - top);
     all += __shfl_xor(all, 32);
     const int e = e1 + 32 * n + (lane & 31);
     if (lane < 32 && e < rows)
@@ -352,15 +426,17 @@ __global__ __launch_bounds__(kThreads, 2) void key_sum_kernel(WeightArgs a, Weig
   for (int c = 0; c < G::kFrags; ++c) at[c] = G::frag_at(lane, c);
   const float sc = a.scale * kLog2e;
   const bool live = t1 < cols;
-  f32x16 mass[NS];
+  float mass[NS][16];
 #pragma unroll
   for (int n = 0; n < NS; ++n)
 #pragma unroll
     for (int r = 0; r < 16; ++r) mass[n][r] = 0.f;
 
   Ring<T, D> ring(lds);
-  // entry e + 32 is `down` rows and `over` heads on from entry e, or one head more and N rows less
-  const int over = 32 / u.N, down = 32 - over * u.N;
+  int in_tile[G::kLoads];  // within a tile of one head, from its first row
+#pragma unroll
+  for (int k = 0; k < G::kLoads; ++k) in_tile[k] = ring.row[k] * int(a.qs[1]) + ring.byte[k];
+  const bool near = a.qs[1] <= 1 << 25;  // (a tile's bytes fit 32 bits)
   for (int chunk = 0; chunk < rows; chunk += kLogs) {
     const int here = min(rows - chunk, kLogs), padded = (here + 31) & ~31;
     if (chunk > 0) __syncthreads();
@@ -377,56 +453,49 @@ __global__ __launch_bounds__(kThreads, 2) void key_sum_kernel(WeightArgs a, Weig
       }
       logs[e] = x;
     }
-    int head[G::kLoads], pos[G::kLoads];  // of the entries that this lane asks for
-#pragma unroll
-    for (int k = 0; k < G::kLoads; ++k) {
-      head[k] = (chunk + ring.row[k]) / u.N;
-      pos[k] = chunk + ring.row[k] - head[k] * u.N;
-    }
     const int tiles = padded / 32;
-    int asked = 0;
+    // row and address of the first entry of the next tile to be asked for
+    int pos, asked = 0;
+    const char *base;
+    auto to_entry = [&](int e) {
+      const int h = e / u.N;
+      pos = e - h * u.N;
+      base = q + pos * a.qs[1] + h * a.qs[2];
+    };
+    to_entry(chunk);
     auto ask = [&](int j, int stage) {
-      ring.ask(stage, [&](int k, int, int byte) {
-        const bool there = head[k] < a.rep;  // (an entry behind the last one: some row)
-        return q + (there ? pos[k] : 0) * a.qs[1] + (there ? head[k] : 0) * a.qs[2] + byte;
-      });
-      if (j == asked) {  // (uniform: not where the last tile is asked for again)
-        ++asked;
-#pragma unroll
-        for (int k = 0; k < G::kLoads; ++k) {
-          pos[k] += down;
-          head[k] += over;
-          if (pos[k] >= u.N) pos[k] -= u.N, ++head[k];
-        }
+      if (j < asked) return ring.ask(stage, [&](int, int, int byte) { return q + byte; });  // (behind the last one: any row)
+      ++asked;
+      if (pos + 32 <= u.N && near) {
+        ring.ask(stage, [&](int k, int, int) { return base + in_tile[k]; });
+        pos += 32;
+        base += 32 * a.qs[1];
+        if (pos < u.N) return;
+      } else {
+        ring.ask(stage, [&](int, int row, int byte) {
+          const int e = min(chunk + 32 * j + row, rows - 1), h = e / u.N;
+          return q + (e - h * u.N) * a.qs[1] + h * a.qs[2] + byte;
+        });
       }
+      to_entry(chunk + 32 * (j + 1));
     };
     __syncthreads();  // (the logarithms are there)
-    run_ring(ring, 0, tiles, ask, [&](int stage, int j) {
-      if (!live) return;
-      u32x4 qf[G::kFrags];
-      ring.read(qf, stage, at);
-      const float log = logs[32 * j + (lane & 31)];
+    float log[2] = {INFINITY, INFINITY};
+    run_pipeline<false, false, T, D, NS>(
+        ring, 0, tiles, at, live, kf, 0.f, ask, [&](int parity, int j) { log[parity] = logs[32 * j + (lane & 31)]; }, [](f32x16 &, int, int) {},
+        [&](const f32x16 &s, int n, int parity, int r0, int r1) {
 #pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        f32x16 s;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-        for (int c = 0; c < G::kFrags; ++c) step(s, kf[n][c], qf[c], static_cast<const T *>(nullptr));
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mass[n][r] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -log));
-      }
-    });
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // nothing is still on its way into LDS
+          for (int r = r0; r < r1; ++r) {
+            mass[n][r] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -log[parity]));
+            stays_here(mass[n][r]);
+          }
+        });
   }
   // over the 32 lanes that hold the same keys
   float *w = a.weights + ((u.l * a.B + u.b) * int64_t(a.Hkv) + u.g) * a.C;
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
-    float x[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = mass[n][r];
-    store_mass(a, w, t1 + 32 * n + product_row(lane, lane & 15), cols, u.P, sum_of_lanes(x, lane), lane);
+    store_mass(a, w, t1 + 32 * n + product_row(lane, lane & 15), cols, u.P, sum_of_lanes(mass[n], lane), lane);
   }
 }
 
