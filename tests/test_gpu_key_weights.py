@@ -44,6 +44,10 @@ CASES = [   # B, S, Hq, Hkv, D, C, prefix, suffix
     (3, 70, 8, 2, 128, 300, [129, 0, 300], [70, 33, 1]), (2, 33, 7, 1, 128, 100, [31, 64], [32, 33]), (1, 200, 2, 2, 64, 700, [513], [200]),
     (4, 17, 28, 4, 128, 90, [63, 65, 1, 32], [17, 0, 16, 1]), (1, 129, 3, 3, 128, 1300, [1025], [129]), (1, 5, 2, 1, 128, 5000, [4999], [5]),
     (2, 257, 4, 4, 128, 400, [255, 397], [257, 256]), (1, 20, 6, 2, 64, 2100, [2080], [20]), (16, 21, 4, 4, 128, 130, [100 + b for b in range(16)], [1 + b for b in range(16)]),
+    # each side of what the kernels divide by: 32 and 64 rows on 1024 and 2048 keys, and more of either
+    (4, 32, 1, 1, 128, 2100, [2016, 2017, 992, 2100], [32, 32, 32, 1]), (4, 64, 1, 1, 64, 2100, [960, 961, 1015, 2080], [64, 64, 33, 20]),
+    (3, 65, 2, 1, 128, 1200, [1000, 959, 1200], [32, 33, 65]), (2, 9, 7, 1, 64, 3000, [2900, 950], [9, 9]), (1, 2, 28, 4, 128, 4500, [4400], [2]),
+    (1, 600, 7, 1, 64, 300, [200], [600]), (2, 700, 3, 1, 128, 900, [130, 0], [700, 699]), (1, 1400, 4, 1, 64, 64, [40], [1399]),
 ]
 
 
@@ -173,3 +177,29 @@ def test_native_and_general_path_agree(lsp, monkeypatch):
     assert torch.equal(a, x) and torch.equal(b, y) and torch.equal(x, y[0])
     with pytest.raises(lsp.LspError, match="decay"):
         lsp.attn_key_weights(q, k, c, P, N, w, decay=-0.1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_more_units_than_one_pass_of_the_grid(lsp, dtype):
+    """Several units to a workgroup, ragged, some without rows, some with more rows than the others' kernel takes."""
+    B, S, Hq, Hkv, D, C = 40, 70, 8, 8, 64, 150
+    q, k, c, w = _operands(B, S, Hq, Hkv, D, C, dtype, seed=9)
+    P = torch.tensor([(37 * b) % 151 for b in range(B)], dtype=torch.int32)
+    N = torch.tensor([(29 * b) % 71 for b in range(B)], dtype=torch.int32)
+    got = lsp.attn_key_weights(q[0].cuda(), k[0].cuda(), c[0].cuda(), P.cuda(), N.cuda(), w[0].cuda(), decay=0.5)
+    _close(got, serving.key_weights(q[0], k[0], c[0], P, N, w[0], 0.5), w[0], P, N, C)
+
+
+def test_a_second_launch_of_few_layers(lsp):
+    """33 layers are a launch of 32 and one of 1, whose units are few enough to be divided further; the workspace is that of the first."""
+    B, S, Hq, Hkv, D, C, L = 10, 70, 2, 2, 64, 600, 33
+    q, k, c, w = _operands(B, S, Hq, Hkv, D, C, torch.bfloat16, layers=L, seed=10)
+    P, N = torch.tensor([500 + b for b in range(B)], dtype=torch.int32), torch.full((B,), 70, dtype=torch.int32)
+    dq, dk, dc = (list(t.cuda().unbind(0)) for t in (q, k, c))
+    table = lsp.AttnLayerTable(dq, dk, dk, dc, dc, [torch.zeros_like(t) for t in dq])
+    need = lsp.attn_key_weights_workspace_bytes(lsp.LSP_BF16, B, S, Hq, Hkv, D, C, L)
+    ws = torch.full((need + 4096,), 7, dtype=torch.uint8, device="cuda")
+    got = lsp.attn_key_weights_layers(table, P.cuda(), N.cuda(), w.cuda(), workspace=ws[:need])
+    assert (ws[need:] == 7).all()
+    for l in (0, 31, 32):
+        _close(got[l], serving.key_weights(q[l], k[l], c[l], P, N, w[l]), w[l], P, N, C)
