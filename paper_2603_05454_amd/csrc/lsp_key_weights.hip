@@ -35,6 +35,9 @@ constexpr int kMaxParts = 16;        // of the keys, for the logarithms of few r
 constexpr int kPartKeys = 128;       // a part has at least
 constexpr int kPartRows = 128;       // a part of the rows, for the sums of few keys, has at least
 constexpr int kGroups = 512;         // workgroups that a launch is divided into where it can be: two to a compute unit
+// Keys of more bytes than this (as many as the attention's K/V, which are twice that) are loaded with the non-temporal hint: 8 layers of 32 heads, 16 x 21
+// rows on 1536 keys, 1.6 GB, 343 -> 332 us.
+constexpr int64_t kOnceBytes = int64_t(160) << 20;
 constexpr float kFarBelow = -1.7e38f;  // a reference below all scores
 
 struct WeightArgs {
@@ -79,6 +82,10 @@ struct Tile {
       row = line / kLines;
       byte = 256 * (line % kLines) + 16 * (x ^ (row & 15));
     }
+  }
+  // byte that belongs to place 64 k + y, from place y's, y < 64 (its row: 1024 / kRowBytes k on)
+  static __device__ __forceinline__ int byte_of(int byte, int k) {
+    return byte ^ 16 * (kRowBytes == 128 ? 4 * k & 4 : kRowBytes == 256 ? 4 * k & 12 : 2 * k & 14);
   }
 };
 
@@ -176,7 +183,7 @@ template <typename T, int D>
 constexpr int kFewRowsOf = Tile<T, D>::kRowBytes == 512 ? 32 : kFewRows;  // (as many as there are registers for)
 constexpr int kFewWaves = 8;
 template <int RS>
-constexpr int kFewTiles = RS == 1 ? 8 : 4;  // a wave's: 128 registers of scores
+constexpr int kFewTiles = RS == 1 ? 8 : 3;  // a wave's: 128 or 96 registers of scores
 template <typename T, int D>
 __host__ __device__ constexpr bool keeps_scores(int64_t rows, int64_t keys) {
   return Tile<T, D>::kRowBytes <= 256 && rows <= kFewRows && keys <= kFewWaves * 32 * (rows <= 32 ? kFewTiles<1> : kFewTiles<2>);
@@ -400,7 +407,7 @@ __device__ __forceinline__ void mask_keys(f32x16 &s, int first, int keys, int la
 
 // ---- few rows ----------------------------------------------------------------------
 // The rows (32 RS of them at most) are every wave's; the waves share the keys, in tiles of 32 that each fetches for itself.
-template <typename T, int D>
+template <typename T, int D, bool ONCE = false>  // ONCE: non-temporal loads
 struct OwnTiles {
   typedef Tile<T, D> G;
   static constexpr int kLoads = G::kBytes / 1024, kDepth = 2;  // tiles ahead
@@ -410,12 +417,24 @@ struct OwnTiles {
   __device__ __forceinline__ void ask(const WeightArgs &a, const Unit &u, const Operands &o, int j, int stage) const {
     int own_lane = lane;
     asm volatile("" : "+v"(own_lane));  // (places are computed anew for every tile: kept, they take the registers of scores)
+    // Load k takes the rows kRows k on from the first one's, with pieces exchanged by k alone (Tile::place).
+    constexpr int kRows = 1024 / G::kRowBytes;
+    int row, byte;
+    G::place(own_lane, row, byte);
+    const int t = 32 * j;
+    auto load = [&](int k, const char *at) {
+      __builtin_amdgcn_global_load_lds(at, (__attribute__((address_space(3))) void *)(lds + stage * G::kBytes + k * 1024), 16, 0, ONCE ? 2 : 0);
+    };
+    auto whole = [&](const char *base, int64_t stride) {  // (per load three vector instructions; 25 where rows are looked up one by one)
+      const uint32_t first = uint32_t(row) * uint32_t(stride);
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      int row, byte;
-      G::place(k * kWave + own_lane, row, byte);
-      __builtin_amdgcn_global_load_lds(o.key(a, u, min(32 * j + row, u.keys - 1)) + byte,
-                                       (__attribute__((address_space(3))) void *)(lds + stage * G::kBytes + k * 1024), 16, 0, 0);
+      for (int k = 0; k < kLoads; ++k) load(k, base + k * kRows * stride + (first + uint32_t(G::byte_of(byte, k))));
+    };
+    if (t + 32 <= u.P) whole(o.kc + t * a.cs[1], a.cs[1]);
+    else if (t >= u.P && t + 32 <= u.keys) whole(o.ks + (t - u.P) * a.ks[1], a.ks[1]);
+    else {
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) load(k, o.key(a, u, min(t + row + k * kRows, u.keys - 1)) + G::byte_of(byte, k));
     }
   }
   // The tile in `stage`, which may be written again then; `newer`: one asked for later may be under way.
@@ -444,15 +463,16 @@ __device__ __forceinline__ void multiply(f32x16 &s, const u32x4 (&kf)[F], const 
 }
 
 // All of the unit's scores are kept in registers, so that K is read once and every score and exponential computed once.  Maxima and sums of the
-// rows meet in LDS.  The first tiles have been asked for; when these are done with, before_end() is called.
-template <typename T, int D, int RS, typename BeforeEnd>
-__device__ __forceinline__ void few_rows_body(const WeightArgs &a, const Unit &u, const Operands &o, const OwnTiles<T, D> &own, int wave, float *s_row,
-                                              BeforeEnd before_end) {
+// rows meet in LDS.  first_tiles() asks for the first ones, if that has not been done (`asked`); when the last are done with, before_end() is called.
+template <typename T, int D, int RS, bool ONCE, typename FirstTiles, typename BeforeEnd>
+__device__ __forceinline__ void few_rows_body(const WeightArgs &a, const Unit &u, const Operands &o, const OwnTiles<T, D, ONCE> &own, int wave, float *s_row,
+                                              bool asked, FirstTiles first_tiles, BeforeEnd before_end) {
   typedef Tile<T, D> G;
   constexpr int kTiles = kFewTiles<RS>, kDepth = OwnTiles<T, D>::kDepth;
   const int lane = own.lane, tiles = (u.keys + 31) / 32, cols = min(u.keys, a.C);
   u32x4 qf[RS][G::kFrags];
   load_rows(qf, a, u, o, lane);
+  if (!asked) first_tiles();
   f32x16 s[kTiles][RS];
   float top[RS], sum[RS];
 #pragma unroll
@@ -462,7 +482,7 @@ __device__ __forceinline__ void few_rows_body(const WeightArgs &a, const Unit &u
     const int j = wave + k * kFewWaves;
     if (j < tiles) {
       u32x4 kf[G::kFrags];
-      own.read(kf, k % kDepth, j + kFewWaves < tiles && k > 0);  // (the rows are newer than the first two)
+      own.read(kf, k % kDepth, j + kFewWaves < tiles && !(k == 0 && asked));  // (the rows may be newer than the first two)
       if (j + kDepth * kFewWaves < tiles) own.ask(a, u, o, j + kDepth * kFewWaves, k % kDepth);
 #pragma unroll
       for (int n = 0; n < RS; ++n) {
@@ -535,37 +555,43 @@ __device__ __forceinline__ void few_rows_body(const WeightArgs &a, const Unit &u
 
 // One workgroup to a compute unit (128 KB of tiles on their way), which goes on to the units that are left; the next one's first tiles are fetched
 // while this one's sums are formed.
-template <typename T, int D>
-__global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void few_rows_kernel(WeightArgs a, WeightLayers L) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  __shared__ float s_row[2 * kFewWaves * kFewRows];
+template <typename T, int D, bool ONCE, typename NextOf>
+__device__ __forceinline__ void few_rows_units(const WeightArgs &a, const WeightLayers &L, Unit u, char *lds, float *s_row, NextOf next_of) {
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const OwnTiles<T, D> own(lds, wave, lane);
-  auto next_of = [&](int n) {
-    Unit u;
-    for (;; n += gridDim.x) {
-      u = unit_at(a, n);
-      if (!u.valid || (u.N > 0 && keeps_scores<T, D>(u.rows, u.keys))) return u;
-    }
-  };
+  const OwnTiles<T, D, ONCE> own(lds, wave, lane);
   auto fetch = [&](const Unit &u) {
     const Operands o(a, L, u);
 #pragma unroll
     for (int k = 0; k < OwnTiles<T, D>::kDepth; ++k)
       if (32 * (wave + k * kFewWaves) < u.keys) own.ask(a, u, o, wave + k * kFewWaves, k);
   };
-  Unit u = next_of(blockIdx.x);
-  if (u.valid) fetch(u);
-  while (u.valid) {
+  for (bool asked = false; u.valid; asked = true) {
     const Unit next = next_of(u.n + gridDim.x);
     const Operands o(a, L, u);
+    auto first_tiles = [&]() { fetch(u); };
     auto before_end = [&]() {
       if (next.valid) fetch(next);
     };
-    if (u.rows <= 32) few_rows_body<T, D, 1>(a, u, o, own, wave, s_row, before_end);
-    else few_rows_body<T, D, 2>(a, u, o, own, wave, s_row, before_end);
+    if (u.rows <= 32) few_rows_body<T, D, 1, ONCE>(a, u, o, own, wave, s_row, asked, first_tiles, before_end);
+    else few_rows_body<T, D, 2, ONCE>(a, u, o, own, wave, s_row, asked, first_tiles, before_end);
     u = next;
   }
+}
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void few_rows_kernel(WeightArgs a, WeightLayers L) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ float s_row[2 * kFewWaves * kFewRows];
+  auto next_of = [&](int n) {
+    for (;; n += gridDim.x) {
+      const Unit u = unit_at(a, n);
+      if (!u.valid || (u.N > 0 && keeps_scores<T, D>(u.rows, u.keys))) return u;
+    }
+  };
+  const Unit u = next_of(blockIdx.x);
+  if (!u.valid) return;
+  // (by the first unit's keys: the others' are about as many)
+  if (int64_t(a.units) * u.keys * Tile<T, D>::kRowBytes > kOnceBytes) few_rows_units<T, D, true>(a, L, u, lds, s_row, next_of);
+  else few_rows_units<T, D, false>(a, L, u, lds, s_row, next_of);
 }
 
 // More keys than that: what the waves have of a part of them is streamed, for the rows' logarithms (SUMS = false) and then for the sums.

@@ -44,8 +44,8 @@ CASES = [   # B, S, Hq, Hkv, D, C, prefix, suffix
     (3, 70, 8, 2, 128, 300, [129, 0, 300], [70, 33, 1]), (2, 33, 7, 1, 128, 100, [31, 64], [32, 33]), (1, 200, 2, 2, 64, 700, [513], [200]),
     (4, 17, 28, 4, 128, 90, [63, 65, 1, 32], [17, 0, 16, 1]), (1, 129, 3, 3, 128, 1300, [1025], [129]), (1, 5, 2, 1, 128, 5000, [4999], [5]),
     (2, 257, 4, 4, 128, 400, [255, 397], [257, 256]), (1, 20, 6, 2, 64, 2100, [2080], [20]), (16, 21, 4, 4, 128, 130, [100 + b for b in range(16)], [1 + b for b in range(16)]),
-    # each side of what the kernels divide by: 32 and 64 rows on 1024 and 2048 keys, and more of either
-    (4, 32, 1, 1, 128, 2100, [2016, 2017, 992, 2100], [32, 32, 32, 1]), (4, 64, 1, 1, 64, 2100, [960, 961, 1015, 2080], [64, 64, 33, 20]),
+    # each side of what the kernels divide by: 32 and 64 rows on 768 and 2048 keys, and more of either
+    (4, 32, 1, 1, 128, 2100, [2016, 2017, 992, 2100], [32, 32, 32, 1]), (4, 64, 1, 1, 64, 2100, [704, 705, 735, 2080], [64, 64, 33, 20]),
     (3, 65, 2, 1, 128, 1200, [1000, 959, 1200], [32, 33, 65]), (2, 9, 7, 1, 64, 3000, [2900, 950], [9, 9]), (1, 2, 28, 4, 128, 4500, [4400], [2]),
     (1, 600, 7, 1, 64, 300, [200], [600]), (2, 700, 3, 1, 128, 900, [130, 0], [700, 699]), (1, 1400, 4, 1, 64, 64, [40], [1399]),
 ]
