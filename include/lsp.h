@@ -474,6 +474,7 @@ typedef struct {
   int64_t cache_batch_stride; /* elements between sequences; 0 = C*Hkv*D */
 } lsp_evict_desc;
 
+/* Bytes of the workspace; 0 for a call that needs none, and for a descriptor that is refused. */
 size_t lsp_kv_evict_workspace_bytes(const lsp_evict_desc *desc);
 
 /*
@@ -482,8 +483,9 @@ size_t lsp_kv_evict_workspace_bytes(const lsp_evict_desc *desc);
  * 16-byte aligned; rows move inside these buffers.  new_weights: device, shape of weights,
  * may be weights itself.  new_len: device int32[B], may be prefix_len itself.
  * kept_index: device int32 [num_layers, B, Hkv, keep], or NULL.  workspace: device,
- * 16-byte aligned, lsp_kv_evict_workspace_bytes(desc) bytes of any content, for this call
- * alone until it has run.  Limits: B, Hkv <= 65535.
+ * 16-byte aligned, lsp_kv_evict_workspace_bytes(desc) bytes (0: none is needed) of any
+ * content, for this call alone until it has run.  Limits: B, Hkv <= 65535, D <= 65536,
+ * C < 2^30, B * Hkv * min(num_layers, 32) < 2^23.
  */
 int32_t lsp_kv_evict(const lsp_evict_desc *desc, const float *weights, const int32_t *prefix_len,
                      void *const *k_cache_layers, void *const *v_cache_layers, float *new_weights,

@@ -1,22 +1,35 @@
 // lsp_kv_evict: cuts the cache of a sequence back to `keep` rows, those of most accumulated attention weight, for every layer
 // and KV head by itself.
 //
-// Which rows stay: the first `first`, the last `recent`, and of the others the largest weights (equal ones: the lower row).  A
-// radix select over the weights' bits, mapped to whole numbers of the same order, finds the smallest weight that stays, 8
-// bits a pass.
+// Which rows stay: the first `first`, the last `recent`, and of the others the largest weights (equal ones: the lower row).  The weights'
+// bits, mapped to whole numbers of the same order, are in registers (16 a thread, which is 8192 rows); the smallest that stays is
+// found by halving the interval between the least and the largest, a count over the workgroup each time, until as many are at or above the
+// middle as there are places.  (A histogram of their leading bits, which accumulated weights share, is a queue for few counters in LDS.)
+// With ties at the end, the row up to which the equal ones stay is found in the same way.
 //
 // Where they go: keys carry their positions and the attention has no mask, so the order of cached rows means nothing.  Rows
 // below `keep` that stay do not move; each row from `keep` on that stays goes into the place of one below that leaves (the n-th of
 // one to the n-th of the other).  That moves at most P - keep rows, where closing the gaps in order moves every row behind the first
 // one.  Sources are all at or above `keep` and destinations below, so nothing that is read is written.
-#include "lsp_common.h"
+//
+// What bounds it: HBM, for the rows that move (8 layers, 8 x about 4860 rows of 32 heads cut to 4096: 1.4 GB), and where they are few
+// the selection's chain of counts.  Few units (layer, sequence, KV head) with many rows to move take several workgroups each, which all find
+// the same rows and move a part of them.
+#include "lsp_attn.h"
 
 namespace lsp {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kKeys = 16;                     // of a thread
+constexpr int kBlock = kThreads * kKeys;      // rows whose weights are in registers at a time
+constexpr int kWindow = 2048;                 // moves that are listed in LDS at a time
+constexpr int kMaxParts = 16;                 // workgroups of a unit
+constexpr int64_t kPartBytes = 256 << 10;     // to be moved, a workgroup's at least
+constexpr int kEnough = 512;                  // workgroups
 constexpr int kMaxLayersPerLaunch = 32;
 struct CachePtrs {
   char *at[2 * kMaxLayersPerLaunch];  // K then V per layer
@@ -27,118 +40,256 @@ struct EvictArgs {
   float *new_weights;
   int32_t *kept_index;  // [layers, B, Hkv, keep] or null
   const int32_t *prefix_len;
-  int32_t *moves;  // per unit (layer, sequence, KV head): count, then `room` destinations, then `room` sources
-  int32_t B, Hkv, C, keep, high, first, recent, room;
+  // per unit, where another kernel writes weights and index (`later`): P, moves (-1: nothing leaves), `room` destinations, `room` sources
+  int32_t *moves;
+  int32_t B, Hkv, C, keep, high, first, recent, room, parts, later;
+  int32_t row_bytes;
+  Div by_pieces;  // 16-byte pieces of a K row and a V row
+  int64_t cache_row_bytes, cache_batch_bytes;
 };
 
-// Whole numbers in the order of the weights: -0 as 0, NaN below everything.
+// Whole numbers from 1 on in the order of the weights: -0 as 0, NaN below everything.
 __device__ __forceinline__ uint32_t order_of(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 1;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sum over the workgroup of the flags of the threads before this one; `all`: of all of them.
-__device__ __forceinline__ int place_in_group(bool flag, int *s_wave, int &all) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const unsigned long long m = __ballot(flag);
-  if (lane == 0) s_wave[wave] = __popcll(m);
-  __syncthreads();
-  int before = __popcll(m & ((1ull << lane) - 1));
-  all = 0;
-  for (int w = 0; w < kThreads / kWave; ++w) {
-    if (w < wave) before += s_wave[w];
-    all += s_wave[w];
+// Numbers of all waves, of which each has one (in every lane).
+struct Meeting {
+  int *s;  // [2][kWaves]: two, so that one barrier is enough
+  int turn = 0;
+  __device__ __forceinline__ int *put(int x) {
+    int *at = s + turn * kWaves;
+    turn ^= 1;
+    if ((threadIdx.x & (kWave - 1)) == 0) at[threadIdx.x / kWave] = x;
+    __syncthreads();
+    return at;
   }
-  __syncthreads();
-  return before;
-}
+  __device__ __forceinline__ int sum(int x) {
+    const int *at = put(x);
+    int r = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) r += at[w];
+    return r;
+  }
+  __device__ __forceinline__ uint32_t most(uint32_t x) {
+    const int *at = put(int(x));
+    uint32_t r = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) r = max(r, uint32_t(at[w]));
+    return r;
+  }
+};
 
-__global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ int s_count[256], s_wave[kThreads / kWave], s_digit, s_left;
-  const int tid = threadIdx.x, b = blockIdx.y, unit = (blockIdx.z * a.B + b) * a.Hkv + blockIdx.x;
+// ONE: a unit's rows are one block, whose weights are read once.
+template <bool ONE>
+__global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a, CachePtrs p) {
+  __shared__ int s_meet[2 * kWaves], s_places[2][kKeys * kWaves], s_total[2], s_dst[kWindow], s_src[kWindow];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int g = blockIdx.x, b = blockIdx.y, l = blockIdx.z / a.parts, part = blockIdx.z - l * a.parts, unit = (l * a.B + b) * a.Hkv + g;
   const int P = min(max(a.prefix_len[b], 0), a.C);
   const float *w = a.weights + int64_t(unit) * a.C;
   float *nw = a.new_weights + int64_t(unit) * a.C;
   int32_t *kept = a.kept_index == nullptr ? nullptr : a.kept_index + int64_t(unit) * a.keep;
-  int32_t *moves = a.moves + int64_t(unit) * (1 + 2 * a.room), *holes = moves + 1, *sources = moves + 1 + a.room;
+  int32_t *list = a.later ? a.moves + int64_t(unit) * (2 + 2 * int64_t(a.room)) : nullptr;
   if (P <= a.high) {  // nothing leaves
-    for (int t = tid; t < P; t += kThreads) nw[t] = w[t];
+    if (part > 0) return;
+    if (a.later) {
+      if (tid == 0) list[0] = P, list[1] = -1;
+      return;
+    }
+    if (nw != w)
+      for (int t = tid; t < P; t += kThreads) nw[t] = w[t];
     if (kept != nullptr)
       for (int t = tid; t < a.keep; t += kThreads) kept[t] = t < P ? t : -1;
-    if (tid == 0) moves[0] = 0;
     return;
   }
-  // rows [first, end) compete for `left` places
-  const int end = P - a.recent;
-  int left = a.keep - a.first - a.recent;
-  uint32_t found = 0, mask = 0;  // the digits found so far
-  for (int shift = 24; shift >= 0 && left > 0; shift -= 8) {
-    s_count[tid] = 0;
-    __syncthreads();
-    for (int t = a.first + tid; t < end; t += kThreads) {
-      const uint32_t u = order_of(w[t]);
-      if ((u & mask) == found) atomicAdd(&s_count[u >> shift & 255], 1);
+  // rows [first, end) compete for `places` places; the others' key is 0
+  const int end = P - a.recent, places = a.keep - a.first - a.recent, blocks = ONE ? 1 : (P + kBlock - 1) / kBlock;
+  uint32_t key[kKeys];
+  auto load = [&](int blk) {
+#pragma unroll
+    for (int r = 0; r < kKeys; ++r) {
+      const int t = blk * kBlock + r * kThreads + tid;
+      key[r] = t >= a.first && t < end ? order_of(w[t]) : 0;
+    }
+  };
+  if (ONE) load(0);
+  Meeting meet = {s_meet};
+  auto count = [&](auto in) {  // rows for which in(key, row)
+    int n = 0;
+    for (int blk = 0; blk < blocks; ++blk) {
+      if (!ONE) load(blk);
+#pragma unroll
+      for (int r = 0; r < kKeys; ++r)
+        if (blk * kBlock + r * kThreads < P) n += __popcll(__ballot(in(key[r], blk * kBlock + r * kThreads + tid)));
+    }
+    return meet.sum(n);
+  };
+  uint32_t least = 0xffffffffu;  // what stays is above, or equal and up to row `upto`
+  int upto = -1;
+  if (places > 0) {
+    uint32_t top = 0, low = 0;  // (low: of the complements)
+    for (int blk = 0; blk < blocks; ++blk) {
+      if (!ONE) load(blk);
+#pragma unroll
+      for (int r = 0; r < kKeys; ++r) {
+        top = max(top, key[r]);
+        low = max(low, key[r] == 0 ? 0u : ~key[r]);
+      }
+    }
+#pragma unroll
+    for (int m = 1; m < kWave; m <<= 1) {
+      top = max(top, uint32_t(__shfl_xor(int(top), m)));
+      low = max(low, uint32_t(__shfl_xor(int(low), m)));
+    }
+    // at least `places` are at or above lo, fewer at or above hi
+    uint32_t lo = ~meet.most(low), hi = meet.most(top) + 1;
+    int above = 0;
+    bool exact = false;
+    while (hi - lo > 1) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      const int n = count([&](uint32_t k, int) { return k >= mid; });
+      if (n >= places) lo = mid;
+      else hi = mid, above = n;
+      if (n == places) {
+        exact = true;
+        break;
+      }
+    }
+    least = lo;
+    upto = P;
+    if (!exact) {  // the largest row with fewer than as many equal ones before it as there are places left
+      const int equal = places - above;
+      upto = 0;
+      int bit = 1;
+      while (bit <= P / 2) bit *= 2;
+      for (; bit > 0; bit >>= 1)
+        if ((upto | bit) <= P && count([&](uint32_t k, int t) { return k == least && t < (upto | bit); }) < equal) upto |= bit;
+    }
+  }
+  auto stays = [&](uint32_t k, int t) { return t < P && (k == 0 || k > least || (k == least && t <= upto)); };
+
+  // The n-th row below `keep` that leaves is the place of the n-th one from there on that stays.
+  int moves = kWindow;  // (known after the first round)
+  for (int window = 0; window < moves; window += kWindow) {
+    int nh = 0, ns = 0;  // in the blocks before
+    for (int blk = 0; blk < blocks; ++blk) {
+      if (!ONE) load(blk);
+      uint32_t hole = 0, moved = 0;  // bit r: row r of the thread
+#pragma unroll
+      for (int r = 0; r < kKeys; ++r) {
+        const int t = blk * kBlock + r * kThreads + tid;
+        const bool s = stays(key[r], t);
+        hole |= uint32_t(t < a.keep && !s) << r;
+        moved |= uint32_t(t >= a.keep && s) << r;
+        const int h = __popcll(__ballot(hole >> r & 1)), m = __popcll(__ballot(moved >> r & 1));
+        if (lane == 0) {
+          s_places[0][r * kWaves + wave] = h;
+          s_places[1][r * kWaves + wave] = m;
+        }
+      }
+      __syncthreads();
+      if (wave < 2) {  // the numbers before each: two per lane
+        int *at = s_places[wave];
+        static_assert(kKeys * kWaves == 2 * kWave, "two per lane");
+        const int x = at[2 * lane], y = at[2 * lane + 1];
+        int before = x + y;
+#pragma unroll
+        for (int m = 1; m < kWave; m <<= 1) {
+          const int from = __shfl_up(before, m);
+          if (lane >= m) before += from;
+        }
+        if (lane == kWave - 1) s_total[wave] = before;
+        at[2 * lane] = before - x - y;
+        at[2 * lane + 1] = before - y;
+      }
+      __syncthreads();
+      const unsigned long long earlier = (1ull << lane) - 1;
+#pragma unroll
+      for (int r = 0; r < kKeys; ++r) {
+        const int t = blk * kBlock + r * kThreads + tid;
+        const bool is_hole = hole >> r & 1, is_moved = moved >> r & 1;
+        const unsigned long long holes = __ballot(is_hole), all_moved = __ballot(is_moved);
+        if (is_hole) {
+          const int n = nh + s_places[0][r * kWaves + wave] + __popcll(holes & earlier) - window;
+          if (n >= 0 && n < kWindow) s_dst[n] = t;
+        }
+        if (is_moved) {
+          const int n = ns + s_places[1][r * kWaves + wave] + __popcll(all_moved & earlier) - window;
+          if (n >= 0 && n < kWindow) s_src[n] = t;
+        }
+        if (!a.later && window == 0 && t < a.keep && !is_hole) {
+          if (nw != w) nw[t] = w[t];
+          if (kept != nullptr) kept[t] = t;
+        }
+      }
+      nh += s_total[0];
+      ns += s_total[1];
+      __syncthreads();
+    }
+    moves = nh;  // (= ns: `keep` rows stay)
+    const int here = min(moves - window, kWindow);
+    if (a.later && part == 0) {
+      if (window == 0 && tid == 0) list[0] = P, list[1] = moves;
+      for (int n = tid; n < here; n += kThreads) {
+        list[2 + window + n] = s_dst[n];
+        list[2 + a.room + window + n] = s_src[n];
+      }
+    }
+    if (!a.later)  // (weights in registers: what is written here is not read again)
+      for (int n = tid; n < here; n += kThreads) {
+        nw[s_dst[n]] = w[s_src[n]];
+        if (kept != nullptr) kept[s_dst[n]] = s_src[n];
+      }
+    // the rows, K and V, 16 bytes a thread, four loads under way
+    char *k_base = p.at[2 * l] + int64_t(b) * a.cache_batch_bytes + int64_t(g) * a.row_bytes;
+    char *v_base = p.at[2 * l + 1] + int64_t(b) * a.cache_batch_bytes + int64_t(g) * a.row_bytes;
+    constexpr int kAhead = 4;
+    const int pieces = a.row_bytes / 8, items = here * pieces, step = kThreads * a.parts;
+    for (int i0 = part * kThreads + tid; i0 < items; i0 += kAhead * step) {
+      u32x4 x[kAhead];
+      char *to[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = min(i0 + k * step, items - 1), n = quotient(i, a.by_pieces), at = (i - n * pieces) * 16;
+        char *base = at < a.row_bytes ? k_base + at : v_base + (at - a.row_bytes);
+        to[k] = base + s_dst[n] * a.cache_row_bytes;
+        x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + s_src[n] * a.cache_row_bytes));
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + k * step < items) __builtin_nontemporal_store(x[k], reinterpret_cast<u32x4 *>(to[k]));
     }
     __syncthreads();
-    if (tid == 0) {
-      int d = 255, above = 0;
-      for (; d > 0 && above + s_count[d] < left; --d) above += s_count[d];
-      s_digit = d;
-      s_left = left - above;
-    }
-    __syncthreads();
-    found |= uint32_t(s_digit) << shift;
-    mask |= 255u << shift;
-    left = s_left;
-    __syncthreads();
   }
-  // `left` of the rows equal to `found` stay, the lowest ones; with no place for any, none does
-  const bool none = a.keep == a.first + a.recent;
-  int equal_before = 0, nh = 0, ns = 0;
-  for (int t0 = 0; t0 < P; t0 += kThreads) {
-    const int t = t0 + tid;
-    const uint32_t u = t >= a.first && t < end ? order_of(w[t]) : 0;
-    const bool in = t >= a.first && t < end, equal = in && !none && u == found;
-    int all;
-    const int e = equal_before + place_in_group(equal, s_wave, all);
-    equal_before += all;
-    const bool stays = t < P && (!in || (!none && (u > found || (equal && e < left))));
-    const bool hole = t < a.keep && !stays, moved = t >= a.keep && stays;
-    const int h = nh + place_in_group(hole, s_wave, all);
-    nh += all;
-    const int s = ns + place_in_group(moved, s_wave, all);
-    ns += all;
-    if (hole) holes[h] = t;
-    if (moved) sources[s] = t;
-    if (stays && t < a.keep) {
-      nw[t] = w[t];
-      if (kept != nullptr) kept[t] = t;
-    }
-  }
-  __syncthreads();  // (holes and sources are as many: `keep` rows stay)
-  for (int k = tid; k < nh; k += kThreads) {
-    nw[holes[k]] = w[sources[k]];
-    if (kept != nullptr) kept[holes[k]] = sources[k];
-  }
-  if (tid == 0) moves[0] = nh;
 }
 
-// One moved row of a unit, K and V, per workgroup and round.
-__global__ __launch_bounds__(kWave) void evict_move_kernel(EvictArgs a, CachePtrs p, int row_bytes, int64_t cache_row_bytes, int64_t cache_batch_bytes) {
-  const int unit = blockIdx.x, b = unit / a.Hkv % a.B, g = unit % a.Hkv, l = unit / a.Hkv / a.B;
-  const int32_t *moves = a.moves + int64_t(unit) * (1 + 2 * a.room);
-  const int n = moves[0];
-  char *base = p.at[2 * l + blockIdx.z] + int64_t(b) * cache_batch_bytes + int64_t(g) * row_bytes;
-  for (int k = blockIdx.y; k < n; k += gridDim.y) {
-    const int dst = moves[1 + k], src = moves[1 + a.room + k];
-    for (int o = threadIdx.x * 16; o < row_bytes; o += kWave * 16)
-      *reinterpret_cast<u32x4 *>(base + dst * cache_row_bytes + o) = *reinterpret_cast<const u32x4 *>(base + src * cache_row_bytes + o);
+// Weights and index of a unit whose workgroups, or whose blocks of rows, were several: they are read by all until the end.
+constexpr int kLaterThreads = 256;
+__global__ __launch_bounds__(kLaterThreads) void evict_weights_kernel(EvictArgs a, int32_t *new_len) {
+  const int tid = threadIdx.x, unit = blockIdx.x, b = unit / a.Hkv % a.B;
+  const float *w = a.weights + int64_t(unit) * a.C;
+  float *nw = a.new_weights + int64_t(unit) * a.C;
+  int32_t *kept = a.kept_index == nullptr ? nullptr : a.kept_index + int64_t(unit) * a.keep;
+  const int32_t *list = a.moves + int64_t(unit) * (2 + 2 * int64_t(a.room));
+  const int P = list[0], moves = list[1], rows = moves < 0 ? P : a.keep;
+  if (nw != w)
+    for (int t = tid; t < rows; t += kLaterThreads) nw[t] = w[t];
+  if (kept != nullptr)
+    for (int t = tid; t < a.keep; t += kLaterThreads) kept[t] = t < P ? t : -1;
+  __syncthreads();
+  for (int n = tid; n < moves; n += kLaterThreads) {
+    const int dst = list[2 + n], src = list[2 + a.room + n];
+    nw[dst] = w[src];
+    if (kept != nullptr) kept[dst] = src;
   }
+  if (new_len != nullptr && unit == b * a.Hkv && tid == 0) new_len[b] = rows;
 }
 
 __global__ void evict_length_kernel(int B, int C, int keep, int high, const int32_t *prefix_len, int32_t *new_len) {
-  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  const int b = blockIdx.x * 256 + threadIdx.x;
   if (b >= B) return;
   const int P = min(max(prefix_len[b], 0), C);
   new_len[b] = P > high ? keep : P;
@@ -147,16 +298,24 @@ __global__ void evict_length_kernel(int B, int C, int keep, int high, const int3
 // rows that can move at most
 int32_t room_of(const lsp_evict_desc *d) { return d->keep < d->C - d->keep ? d->keep : d->C - d->keep; }
 int32_t layers_at_once(int32_t n) { return n < kMaxLayersPerLaunch ? n : kMaxLayersPerLaunch; }
+// workgroups of a unit
+int32_t parts_of(const lsp_evict_desc *d, int32_t layers) {
+  const int64_t units = int64_t(layers) * d->B * d->Hkv, bytes = int64_t(room_of(d)) * d->D * int64_t(elem_size(d->kv_dtype)) * 2;
+  const int64_t most = kEnough / units < kMaxParts ? kEnough / units : kMaxParts, n = bytes / kPartBytes < most ? bytes / kPartBytes : most;
+  return n > 1 ? int32_t(n) : 1;
+}
+bool weights_later(const lsp_evict_desc *d, int32_t layers) { return d->C > kBlock || parts_of(d, layers) > 1; }
 
 int32_t check(const lsp_evict_desc *d) {
   LSP_CHECK_ARG(d != nullptr, "lsp_kv_evict: null descriptor");
   LSP_CHECK_ARG(d->kv_dtype == LSP_F32 || d->kv_dtype == LSP_BF16, "lsp_kv_evict: unknown kv_dtype %d", d->kv_dtype);
   LSP_CHECK_ARG(d->B > 0 && d->B <= 65535 && d->Hkv > 0 && d->Hkv <= 65535 && d->D > 0 && d->C > 0 && d->num_layers > 0, "lsp_kv_evict: bad dimension");
+  LSP_CHECK_ARG(d->D <= 65536 && d->C < 1 << 30, "lsp_kv_evict: D must be <= 65536 and C below 2^30");
   LSP_CHECK_ARG(d->keep > 0 && d->keep <= d->C, "lsp_kv_evict: keep must be 1..C (got %d, C = %d)", d->keep, d->C);
   LSP_CHECK_ARG(d->high >= d->keep, "lsp_kv_evict: high = %d is below keep = %d", d->high, d->keep);
   LSP_CHECK_ARG(d->first >= 0 && d->recent >= 0 && int64_t(d->first) + d->recent <= d->keep,
                 "lsp_kv_evict: first + recent must be 0..keep (got %d + %d of %d)", d->first, d->recent, d->keep);
-  LSP_CHECK_ARG(int64_t(d->B) * d->Hkv * layers_at_once(d->num_layers) < int64_t(1) << 31, "lsp_kv_evict: too many heads");
+  LSP_CHECK_ARG(int64_t(d->B) * d->Hkv * layers_at_once(d->num_layers) < int64_t(1) << 23, "lsp_kv_evict: too many heads");
   return LSP_OK;
 }
 
@@ -165,7 +324,14 @@ int32_t check(const lsp_evict_desc *d) {
 
 extern "C" size_t lsp_kv_evict_workspace_bytes(const lsp_evict_desc *d) {
   if (lsp::check(d) != LSP_OK) return 0;
-  return size_t(lsp::layers_at_once(d->num_layers)) * d->B * d->Hkv * (1 + 2 * size_t(lsp::room_of(d))) * sizeof(int32_t);
+  // a launch for the last layers, of fewer units, may divide them further
+  size_t most = 0;
+  const int32_t rest = d->num_layers % lsp::kMaxLayersPerLaunch, sizes[2] = {lsp::layers_at_once(d->num_layers), rest};
+  for (int32_t n : sizes) {
+    const size_t bytes = n > 0 && lsp::weights_later(d, n) ? size_t(n) * d->B * d->Hkv * (2 + 2 * size_t(lsp::room_of(d))) * sizeof(int32_t) : 0;
+    if (bytes > most) most = bytes;
+  }
+  return most;
 }
 
 extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, const int32_t *prefix_len, void *const *k_cache_layers,
@@ -184,30 +350,45 @@ extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, c
     LSP_CHECK_ARG(aligned16(k_cache_layers[l]) && aligned16(v_cache_layers[l]), "lsp_kv_evict: K/V pointer of layer %d is not 16-byte aligned", l);
   }
   const size_t need = lsp_kv_evict_workspace_bytes(d);
-  if (workspace == nullptr || workspace_bytes < need || !aligned16(workspace)) {
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) {
     set_error("lsp_kv_evict: workspace of %zu bytes (16-byte aligned) required, got %zu", need, workspace_bytes);
     return LSP_ERR_WORKSPACE;
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
   EvictArgs a = {weights, new_weights, kept_index, prefix_len, static_cast<int32_t *>(workspace), d->B, d->Hkv, d->C, d->keep, d->high, d->first, d->recent, room_of(d)};
+  a.row_bytes = int32_t(row_bytes);
+  a.by_pieces = div_by(row_bytes / 8);
+  a.cache_row_bytes = cache_row_bytes;
+  a.cache_batch_bytes = cache_bb;
+  bool lengths_left = true;
   for (int l0 = 0; l0 < d->num_layers; l0 += kMaxLayersPerLaunch) {
     const int nl = layers_at_once(d->num_layers - l0);
     const int64_t units = int64_t(l0) * d->B * d->Hkv;
     a.weights = weights + units * d->C;
     a.new_weights = new_weights + units * d->C;
     a.kept_index = kept_index == nullptr ? nullptr : kept_index + units * d->keep;
+    a.parts = parts_of(d, nl);
+    a.later = weights_later(d, nl);
     CachePtrs p;
     for (int l = 0; l < kMaxLayersPerLaunch; ++l) {
       const int s = l < nl ? l0 + l : l0;
       p.at[2 * l] = static_cast<char *>(k_cache_layers[s]);
       p.at[2 * l + 1] = static_cast<char *>(v_cache_layers[s]);
     }
-    evict_select_kernel<<<dim3(d->Hkv, d->B, nl), kThreads, 0, st>>>(a);
-    LSP_CHECK_LAUNCH("lsp_kv_evict: selection launch");
-    evict_move_kernel<<<dim3(nl * d->B * d->Hkv, 16, 2), kWave, 0, st>>>(a, p, int(row_bytes), cache_row_bytes, cache_bb);
-    LSP_CHECK_LAUNCH("lsp_kv_evict: copy launch");
+    const dim3 grid(d->Hkv, d->B, nl * a.parts);
+    if (d->C <= kBlock) evict_kernel<true><<<grid, kThreads, 0, st>>>(a, p);
+    else evict_kernel<false><<<grid, kThreads, 0, st>>>(a, p);
+    LSP_CHECK_LAUNCH("lsp_kv_evict: launch");
+    if (a.later) {
+      const bool last = l0 + nl == d->num_layers;  // (every layer goes by the lengths)
+      evict_weights_kernel<<<nl * d->B * d->Hkv, kLaterThreads, 0, st>>>(a, last ? new_len : nullptr);
+      LSP_CHECK_LAUNCH("lsp_kv_evict: weights launch");
+      if (last) lengths_left = false;
+    }
   }
-  evict_length_kernel<<<(d->B + 255) / 256, 256, 0, st>>>(d->B, d->C, d->keep, d->high, prefix_len, new_len);
-  LSP_CHECK_LAUNCH("lsp_kv_evict: length launch");
+  if (lengths_left) {
+    evict_length_kernel<<<(d->B + 255) / 256, 256, 0, st>>>(d->B, d->C, d->keep, d->high, prefix_len, new_len);
+    LSP_CHECK_LAUNCH("lsp_kv_evict: length launch");
+  }
   return LSP_OK;
 }

@@ -54,6 +54,9 @@ CASES = [   # L, B, Hkv, D, C, P, keep, high, first, recent
     (1, 1, 2, 64, 900, [900], 100, None, 40, 60), (2, 2, 1, 64, 513, [513, 0], 1, None, 0, 1), (1, 4, 2, 64, 200, [100, 120, 121, 200], 80, 120, 3, 9),
     (1, 1, 1, 128, 9000, [8999], 4100, None, 4, 256), (1, 2, 1, 64, 20000, [19999, 18001], 12000, None, 0, 1000), (35, 1, 2, 64, 50, [50], 30, None, 0, 4),
     (1, 2, 2, 64, 60, [60, 60], 60, None, 0, 0), (1, 1, 1, 64, 70001, [70001], 35000, None, 4, 100),
+    # blocks of 8192 rows, lists of 2048 moves, several workgroups of a unit
+    (1, 1, 1, 64, 8192, [8192], 4096, None, 0, 0), (1, 1, 1, 64, 8193, [8193], 4097, None, 0, 0), (2, 2, 2, 128, 8192, [8192, 7000], 4090, None, 3, 2000),
+    (1, 3, 1, 128, 16400, [16400, 9000, 4000], 5000, None, 1, 9), (33, 4, 2, 128, 6000, [6000, 100, 3001, 5000], 3000, None, 4, 0),
 ]
 
 

@@ -55,7 +55,8 @@ def test_evict_entry_point():
                          (dict(first=10, recent=11), -1, b"first"), (dict(first=2 ** 31 - 1, recent=2 ** 31 - 1), -1, b"first"), (dict(D=4), -1, b"multiple of 16"),
                          (dict(cache_batch_stride=100), -1, b"stride"), (dict(w=None), -1, b"null"), (dict(nl=None), -1, b"null"),
                          (dict(kc=(ctypes.c_void_p * 1)(0)), -1, b"layer 0"), (dict(vc=(ctypes.c_void_p * 1)(p.value + 8)), -1, b"aligned"),
-                         (dict(ws=None), -3, b"workspace"), (dict(wsb=8), -3, b"workspace")):
+                         (dict(C=9000, ws=None), -3, b"workspace"), (dict(C=9000, wsb=8), -3, b"workspace"), (dict(D=1 << 17), -1, b"65536"),
+                         (dict(C=1 << 30), -1, b"2^30"), (dict(B=65535, Hkv=65535), -1, b"many heads")):
         assert call(**kw) == rc and word in L.lsp_last_error(), (kw, L.lsp_last_error())
     assert L.lsp_kv_evict_workspace_bytes(None) == 0
 
