@@ -84,7 +84,7 @@ struct Meeting {
 
 // ONE: a unit's rows are one block, whose weights are read once.
 template <bool ONE>
-__global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a, CachePtrs p) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 8 : 1))) void evict_kernel(EvictArgs a, CachePtrs p) {
   __shared__ int s_meet[2 * kWaves], s_places[2][kKeys * kWaves], s_total[2], s_dst[kWindow], s_src[kWindow];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int g = blockIdx.x, b = blockIdx.y, l = blockIdx.z / a.parts, part = blockIdx.z - l * a.parts, unit = (l * a.B + b) * a.Hkv + g;
@@ -108,10 +108,18 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a, CachePtrs 
   // rows [first, end) compete for `places` places; the others' key is 0
   const int end = P - a.recent, places = a.keep - a.first - a.recent, blocks = ONE ? 1 : (P + kBlock - 1) / kBlock;
   uint32_t key[kKeys];
+  // (a thread's number that the compiler takes for a new one: it would keep sixteen rows' numbers, addresses and flags from loop to loop, in
+  // registers that would leave one workgroup to a compute unit)
+  auto here_tid = [&]() {
+    int x = tid;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
   auto load = [&](int blk) {
+    const int own = here_tid();
 #pragma unroll
     for (int r = 0; r < kKeys; ++r) {
-      const int t = blk * kBlock + r * kThreads + tid;
+      const int t = blk * kBlock + r * kThreads + own;
       key[r] = t >= a.first && t < end ? order_of(w[t]) : 0;
     }
   };
@@ -121,9 +129,10 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a, CachePtrs 
     int n = 0;
     for (int blk = 0; blk < blocks; ++blk) {
       if (!ONE) load(blk);
+      const int own = here_tid();
 #pragma unroll
       for (int r = 0; r < kKeys; ++r)
-        if (blk * kBlock + r * kThreads < P) n += __popcll(__ballot(in(key[r], blk * kBlock + r * kThreads + tid)));
+        if (blk * kBlock + r * kThreads < P) n += __popcll(__ballot(in(key[r], blk * kBlock + r * kThreads + own)));
     }
     return meet.sum(n);
   };
@@ -178,9 +187,10 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a, CachePtrs 
     for (int blk = 0; blk < blocks; ++blk) {
       if (!ONE) load(blk);
       uint32_t hole = 0, moved = 0;  // bit r: row r of the thread
+      const int own = here_tid();
 #pragma unroll
       for (int r = 0; r < kKeys; ++r) {
-        const int t = blk * kBlock + r * kThreads + tid;
+        const int t = blk * kBlock + r * kThreads + own;
         const bool s = stays(key[r], t);
         hole |= uint32_t(t < a.keep && !s) << r;
         moved |= uint32_t(t >= a.keep && s) << r;
@@ -207,9 +217,11 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a, CachePtrs 
       }
       __syncthreads();
       const unsigned long long earlier = (1ull << lane) - 1;
+      const int own2 = here_tid();
 #pragma unroll
       for (int r = 0; r < kKeys; ++r) {
-        const int t = blk * kBlock + r * kThreads + tid;
+        if (blk * kBlock + r * kThreads >= P) break;
+        const int t = blk * kBlock + r * kThreads + own2;
         const bool is_hole = hole >> r & 1, is_moved = moved >> r & 1;
         const unsigned long long holes = __ballot(is_hole), all_moved = __ballot(is_moved);
         if (is_hole) {
