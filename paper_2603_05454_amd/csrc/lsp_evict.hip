@@ -42,6 +42,7 @@ struct EvictArgs {
   const int32_t *prefix_len;
   // per unit, where another kernel writes weights and index (`later`): P, moves (-1: nothing leaves), `room` destinations, `room` sources
   int32_t *moves;
+  int32_t *new_len;  // where they are written by the first launch (not over the lengths that all of them read), or null
   int32_t B, Hkv, C, keep, high, first, recent, room, parts, later;
   int32_t row_bytes;
   Div by_pieces;  // 16-byte pieces of a K row and a V row
@@ -93,6 +94,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
   float *nw = a.new_weights + int64_t(unit) * a.C;
   int32_t *kept = a.kept_index == nullptr ? nullptr : a.kept_index + int64_t(unit) * a.keep;
   int32_t *list = a.later ? a.moves + int64_t(unit) * (2 + 2 * int64_t(a.room)) : nullptr;
+  if (a.new_len != nullptr && tid == 0 && g == 0 && l == 0 && part == 0) a.new_len[b] = P > a.high ? a.keep : P;
   if (P <= a.high) {  // nothing leaves
     if (part > 0) return;
     if (a.later) {
@@ -367,12 +369,12 @@ extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, c
     return LSP_ERR_WORKSPACE;
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
-  EvictArgs a = {weights, new_weights, kept_index, prefix_len, static_cast<int32_t *>(workspace), d->B, d->Hkv, d->C, d->keep, d->high, d->first, d->recent, room_of(d)};
+  EvictArgs a = {weights, new_weights, kept_index, prefix_len, static_cast<int32_t *>(workspace), new_len == prefix_len ? nullptr : new_len, d->B, d->Hkv, d->C, d->keep, d->high, d->first, d->recent, room_of(d)};
   a.row_bytes = int32_t(row_bytes);
   a.by_pieces = div_by(row_bytes / 8);
   a.cache_row_bytes = cache_row_bytes;
   a.cache_batch_bytes = cache_bb;
-  bool lengths_left = true;
+  bool lengths_left = new_len == prefix_len;
   for (int l0 = 0; l0 < d->num_layers; l0 += kMaxLayersPerLaunch) {
     const int nl = layers_at_once(d->num_layers - l0);
     const int64_t units = int64_t(l0) * d->B * d->Hkv;
@@ -391,8 +393,9 @@ extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, c
     if (d->C <= kBlock) evict_kernel<true><<<grid, kThreads, 0, st>>>(a, p);
     else evict_kernel<false><<<grid, kThreads, 0, st>>>(a, p);
     LSP_CHECK_LAUNCH("lsp_kv_evict: launch");
+    a.new_len = nullptr;
     if (a.later) {
-      const bool last = l0 + nl == d->num_layers;  // (every layer goes by the lengths)
+      const bool last = lengths_left && l0 + nl == d->num_layers;  // (every layer goes by the lengths)
       evict_weights_kernel<<<nl * d->B * d->Hkv, kLaterThreads, 0, st>>>(a, last ? new_len : nullptr);
       LSP_CHECK_LAUNCH("lsp_kv_evict: weights launch");
       if (last) lengths_left = false;

@@ -38,6 +38,7 @@ constexpr float kLagOctaves = 8.0f;
 // that holds one, or a row of nothing else, takes a way of its own.
 constexpr float kLow = -1e37f;
 constexpr int kMaxAlt = 32;
+constexpr int kRankStep = 8;    // entries that are read at a time
 constexpr int kMinCut = 16384;  // rows of at most this many entries are not cut
 
 template <typename T>
@@ -152,7 +153,7 @@ template <typename T, int NT, bool ALT>
 inline size_t dynamic_lds(int64_t elements) {
   const int64_t group = 2 * NT, vectors = (elements / Vec<T>::N + group - 1) / group * group;
   const int64_t maxima = (vectors < tile_vectors<T, NT>() ? vectors : tile_vectors<T, NT>()) * int64_t(sizeof(T));
-  const int64_t entries = (NT * Vec<T>::N + kMaxAlt + 16) * 8, merged = ((3 + 2 * kMaxAlt) * 8 + 17 * kMaxAlt) * 8;
+  const int64_t entries = (NT * Vec<T>::N + kMaxAlt + 16 + kRankStep) * 8, merged = ((3 + 2 * kMaxAlt) * 8 + 17 * kMaxAlt + kRankStep) * 8;
   const int64_t least = elements > kMinCut && merged > entries ? merged : entries;  // (only rows that are cut meet)
   return !ALT ? size_t(merged) : size_t(maxima > least ? maxima : least);
 }
@@ -171,11 +172,13 @@ __device__ __forceinline__ int group_sum(Shared<NT> &sh, int n) {
   return all;
 }
 
-// The best K of `n` entries in LDS and of sh.best go to sh.best.  Every thread calls it, after a barrier.
+// The best K of `n` entries in LDS and of sh.best go to sh.best.  Every thread calls it, after a barrier; there is room for K + kRankStep entries more.
+// Eight are read at a time: one by one the trip to LDS is waited for at each (8 rows of 82 303 entries, cut into 16 segments, 20 alternatives: 19.2 us).
 template <int NT>
 __device__ __forceinline__ void rank_entries(Shared<NT> &sh, uint64_t *entries, int n, int K) {
+  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
   const int tid = threadIdx.x;
-  if (tid < K) entries[n + tid] = sh.best[tid];
+  if (tid < K + kRankStep) entries[n + tid] = tid < K ? sh.best[tid] : 0;
   n += K;
   __syncthreads();
   if (tid < K) sh.best[tid] = 0;
@@ -183,7 +186,13 @@ __device__ __forceinline__ void rank_entries(Shared<NT> &sh, uint64_t *entries, 
   for (int e = tid; e < n; e += NT) {
     const uint64_t mine = entries[e];
     int before = 0;
-    for (int k = 0; k < n; ++k) before += entries[k] > mine;
+    for (int k = 0; k < n; k += kRankStep) {
+      u64x2 x[kRankStep / 2];
+#pragma unroll
+      for (int i = 0; i < kRankStep / 2; ++i) x[i] = *reinterpret_cast<const u64x2 *>(entries + k + 2 * i);
+#pragma unroll
+      for (int i = 0; i < kRankStep / 2; ++i) before += (x[i].x > mine) + (x[i].y > mine);
+    }
     if (before < K && mine != 0) sh.best[before] = mine;
   }
   __syncthreads();
@@ -539,7 +548,7 @@ __global__ __launch_bounds__(NT) void token_scores_split_kernel(const T *__restr
     if (lane < 1 << k) part = {__uint_as_float(got[lane * words]), __uint_as_float(got[lane * words + 1]), __uint_as_float(got[lane * words + 2])};
     st = merge_stats(part);
     if (ALT) {
-      uint64_t *entries = reinterpret_cast<uint64_t *>(lds) + ((all + 1) >> 1);
+      uint64_t *entries = reinterpret_cast<uint64_t *>(lds) + ((all + 3) >> 2) * 2;  // (16-byte aligned)
       for (int j = tid; j < a.K << k; j += NT) {
         const int s = j / a.K, e = j - s * a.K;
         entries[j] = uint64_t(got[s * words + 3 + 2 * e]) << 32 | got[s * words + 4 + 2 * e];
