@@ -14,6 +14,7 @@ argument by argument, raises, or allocates what is missing.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import warnings
 
@@ -22,7 +23,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblsp.so")
 _lib = None
-_nat_addresses = None
+_nat_addresses = _nat_attn_table = _nat_layer_table = None
 _nat = None     # the native marshalling module, bound to the loaded library (None: not loaded, or not built)
 
 LSP_F32, LSP_BF16 = 0, 1
@@ -75,7 +76,7 @@ NATIVE_ENTRIES = ("lsp_attn_workspace_bytes", "lsp_attn_step", "lsp_attn_step_la
 
 def lib() -> ctypes.CDLL:
     """The loaded C-ABI library; raises LspError when it has not been built."""
-    global _lib, _nat, _nat_addresses
+    global _lib, _nat, _nat_addresses, _nat_attn_table, _nat_layer_table
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise LspError(f"{LIB_PATH} is missing: run `python -m paper_2603_05454_amd.build` "
@@ -98,7 +99,8 @@ def lib() -> ctypes.CDLL:
         else:
             _binding.bind(*[ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in NATIVE_ENTRIES])
             _nat = _binding
-            _nat_addresses = _binding.addresses     # (not a call of a step: serves the tables, which are built beforehand)
+            # (no calls of a step: they serve the tables, which are built beforehand)
+            _nat_addresses, _nat_attn_table, _nat_layer_table = _binding.addresses, _binding.attn_table, _binding.layer_table
         _lib = L
     return _lib
 
@@ -244,6 +246,12 @@ def _addresses(tensors):
     return None if b is None else (ctypes.c_void_p * len(tensors)).from_buffer_copy(b)
 
 
+@functools.lru_cache(maxsize=64)
+def _pointers(n):
+    """The ctypes type of n addresses."""
+    return ctypes.c_void_p * n
+
+
 class AttnLayerTable:
     """Host arrays of per-layer device pointers for lsp_attn_step_layers, built once and
     reused (all layers must share shape, dtype and strides)."""
@@ -252,6 +260,13 @@ class AttnLayerTable:
         n = len(q)
         if not (len(k_suf) == len(v_suf) == len(k_cache) == len(v_cache) == len(out) == n > 0):
             raise LspError("AttnLayerTable: one tensor of each kind per layer, at least one layer")
+        made = _nat_attn_table(q, k_suf, v_suf, k_cache, v_cache, out) if _nat_attn_table is not None else None
+        if made is not None:
+            Arr = _pointers(n)
+            self.n, self.out, self.keep = n, out, (q, k_suf, v_suf, k_cache, v_cache, out)
+            self.desc = AttnDesc.from_buffer_copy(made[0])
+            self.arrays = [Arr.from_buffer_copy(b) for b in made[1:]]
+            return
         arrays = [_addresses(lst) for lst in (q, k_suf, v_suf, k_cache, v_cache, out)]
         for lst, array in zip((q, k_suf, v_suf, k_cache, v_cache, out), arrays):
             for t in lst if array is None else lst[:1]:
@@ -406,6 +421,13 @@ class LayerTable:
         n = len(k_suf)
         if not (len(v_suf) == len(k_cache) == len(v_cache) == n > 0):
             raise LspError("LayerTable: one tensor of each kind per layer, at least one layer")
+        made = _nat_layer_table(k_suf, v_suf, k_cache, v_cache) if _nat_layer_table is not None else None
+        if made is not None:
+            Arr = _pointers(n)
+            self.n, self.keep = n, (k_suf, v_suf, k_cache, v_cache)
+            self.kv_dtype, self.B, self.S, self.Hkv, self.D, self.C, self.suf_bs, self.cache_bs = made[0]
+            self.arrays = [Arr.from_buffer_copy(b) for b in made[1:]]
+            return
         arrays = [_addresses(lst) for lst in (k_suf, v_suf, k_cache, v_cache)]
         for lst, array in zip((k_suf, v_suf, k_cache, v_cache), arrays):
             for t in lst if array is None else lst[:1]:
@@ -655,8 +677,14 @@ def _here(*ts):
 
 
 def _table_here(t):
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
+    """A table's first tensor; with one device there is no other to be on."""
+    if _devices() > 1:
         _here(t)
+
+
+@functools.lru_cache(maxsize=1)
+def _devices() -> int:
+    return torch.cuda.device_count()
 
 
 def _call_workspace(given, need, device):

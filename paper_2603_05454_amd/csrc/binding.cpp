@@ -8,6 +8,7 @@
 // Why: through ctypes a call cost 9-18 us on the host (attribute reads, checks and
 // conversions of up to 20 arguments in the interpreter), more than many of
 // the kernels behind it take; here it is 4-10 us, most of it the launch itself.
+#define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <hip/hip_runtime_api.h>
 
@@ -582,6 +583,68 @@ PyObject *addresses(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return bytes.o;
 }
 
+// What a table is made of: N lists of as many tensors, each list's of one device, element type (the first one's), shape and strides; their addresses as
+// bytes.  false: the constructor in Python looks at them, and raises or takes them.
+template <int N>
+bool lists(PyObject *const *a, const at::Tensor *(&first)[N], Object *(&bytes)[N]) {
+  const Py_ssize_t count = PyList_Check(a[0]) ? PyList_GET_SIZE(a[0]) : 0;
+  if (count == 0) return false;
+  for (int k = 0; k < N; ++k) {
+    if (!PyList_Check(a[k]) || PyList_GET_SIZE(a[k]) != count) return false;
+    bytes[k] = new Object(PyBytes_FromStringAndSize(nullptr, count * Py_ssize_t(sizeof(void *))));
+    if (!bytes[k]->o) return false;
+    auto *out = reinterpret_cast<void **>(PyBytes_AS_STRING(bytes[k]->o));
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const at::Tensor *t = device_tensor(PyList_GET_ITEM(a[k], i));
+      if (!t) return false;
+      if (i == 0) first[k] = t;
+      if (t->device() != first[0]->device() || t->scalar_type() != first[0]->scalar_type() || t->sizes() != first[k]->sizes() || t->strides() != first[k]->strides()) return false;
+      out[i] = t->mutable_data_ptr();
+    }
+  }
+  return true;
+}
+template <int N>
+struct Lists {
+  const at::Tensor *first[N] = {};
+  Object *bytes[N] = {};
+  bool of(PyObject *const *a) { return lists<N>(a, first, bytes); }
+  ~Lists() {
+    for (Object *o : bytes) delete o;
+  }
+};
+// (q, k_suf, v_suf, k_cache, v_cache, out) -> (descriptor as bytes, six lists of addresses as bytes)
+PyObject *attn_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(6);
+  Lists<6> l;
+  ORDINARY(l.of(a));
+  const at::Tensor &q = *l.first[0], &ks = *l.first[1], &vs = *l.first[2], &kc = *l.first[3], &vc = *l.first[4], &out = *l.first[5];
+  ORDINARY(q.dim() == 4 && ks.dim() == 4 && kc.dim() == 4);
+  const int64_t B = q.size(0), S = q.size(1), Hq = q.size(2), D = q.size(3), Hkv = ks.size(2), C = kc.size(1);
+  ORDINARY(shape4(ks, B, S, Hkv, D) && shape4(vs, B, S, Hkv, D) && shape4(kc, B, C, Hkv, D) && shape4(vc, B, C, Hkv, D) && shape4(out, B, S, Hq, D) &&
+           same_strides(ks, vs) && same_strides(kc, vc));
+  lsp_attn_desc d = {};
+  ORDINARY(element_type(q, d.dtype) && strides3(q, d.q_stride) && strides3(ks, d.kv_suf_stride) && strides3(kc, d.cache_stride) && strides3(out, d.o_stride));
+  d.B = int32_t(B); d.S = int32_t(S); d.Hq = int32_t(Hq); d.Hkv = int32_t(Hkv); d.D = int32_t(D); d.C = int32_t(C);
+  return Py_BuildValue("(y#OOOOOO)", reinterpret_cast<const char *>(&d), Py_ssize_t(sizeof d), l.bytes[0]->o, l.bytes[1]->o, l.bytes[2]->o, l.bytes[3]->o,
+                       l.bytes[4]->o, l.bytes[5]->o);
+}
+// (k_suf, v_suf, k_cache, v_cache) -> ((kv_dtype, B, S, Hkv, D, C, suf_bs, cache_bs), four lists of addresses as bytes)
+PyObject *layer_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(4);
+  Lists<4> l;
+  ORDINARY(l.of(a));
+  int32_t type;
+  ORDINARY(element_type(*l.first[0], type));
+  for (const at::Tensor *t : l.first)
+    ORDINARY(t->dim() == 4 && t->stride(3) == 1 && t->stride(2) == t->size(3) && t->stride(1) == t->size(2) * t->size(3));
+  const at::Tensor &ks = *l.first[0], &vs = *l.first[1], &kc = *l.first[2], &vc = *l.first[3];
+  ORDINARY(vs.sizes() == ks.sizes() && vc.sizes() == kc.sizes() && same_strides(ks, vs) && same_strides(kc, vc) && kc.size(0) == ks.size(0) &&
+           kc.size(2) == ks.size(2) && kc.size(3) == ks.size(3));
+  return Py_BuildValue("((iLLLLLLL)OOOO)", type, (long long)ks.size(0), (long long)ks.size(1), (long long)ks.size(2), (long long)ks.size(3),
+                       (long long)kc.size(1), (long long)ks.stride(0), (long long)kc.stride(0), l.bytes[0]->o, l.bytes[1]->o, l.bytes[2]->o, l.bytes[3]->o);
+}
+
 // No C++ exception may reach the interpreter: torch throws where a tensor has no strides or no
 // storage (sparse, batched by vmap), there is no device or a subclass written in Python raises (the error is then
 // set as well), and the general path meets the same and raises it.
@@ -603,7 +666,8 @@ PyMethodDef methods[] = {fast<bind>("bind"), fast<attn_step>("attn_step"), fast<
                          fast<flip_update>("flip_update"), fast<poll_lengths>("poll_lengths"),
                          fast<poll_start>("poll_start"), fast<poll_wait>("poll_wait"), fast<addresses>("addresses"),
                          fast<token_scores>("token_scores"), fast<attn_key_weights>("attn_key_weights"),
-                         fast<attn_key_weights_layers>("attn_key_weights_layers"), fast<kv_evict>("kv_evict"), {nullptr, nullptr, 0, nullptr}};
+                         fast<attn_key_weights_layers>("attn_key_weights_layers"), fast<kv_evict>("kv_evict"), fast<attn_table>("attn_table"),
+                         fast<layer_table>("layer_table"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

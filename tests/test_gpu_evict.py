@@ -147,3 +147,28 @@ def test_native_and_general_path_agree(lsp, monkeypatch):
             lsp.kv_evict(w, p, table, 30, high=40, first=1, recent=5)
         made.append((k, v, w, p))
     assert all(torch.equal(a, b) for a, b in zip(*made))
+
+
+def test_tables_made_natively_and_in_python_are_the_same(lsp, monkeypatch):
+    """Of tensors in one buffer, with a batch stride; lists that do not belong together are refused as before."""
+    big = torch.randn((3, 2, 20, 4, 64), device="cuda")
+    suf, cache = [t[:, :6] for t in big.unbind(0)], [t[:, 6:] for t in big.unbind(0)]
+    q = [torch.randn((2, 6, 8, 64), device="cuda") for _ in range(3)]
+    lsp.lib()
+    native = lsp.AttnLayerTable(q, suf, suf, cache, cache, q), lsp.LayerTable(suf, suf, cache, cache)
+    with monkeypatch.context() as m:
+        m.setattr(lsp, "_nat_attn_table", None)
+        m.setattr(lsp, "_nat_layer_table", None)
+        general = lsp.AttnLayerTable(q, suf, suf, cache, cache, q), lsp.LayerTable(suf, suf, cache, cache)
+    assert bytes(native[0].desc) == bytes(general[0].desc) and native[0].n == general[0].n and native[0].out is general[0].out
+    for a, b in zip(native, general):
+        assert [bytes(x) for x in a.arrays] == [bytes(x) for x in b.arrays] and len(a.keep) == len(b.keep)
+    for name in ("n", "kv_dtype", "B", "S", "Hkv", "D", "C", "suf_bs", "cache_bs"):
+        assert getattr(native[1], name) == getattr(general[1], name), name
+    for bad in ((suf, suf, cache, [t.double() for t in cache]), (suf, suf, cache[:2], cache), ([t.cpu() for t in suf], suf, cache, cache),
+                (suf, suf, [t[:1] for t in cache], cache), ([t.transpose(1, 2) for t in suf], suf, cache, cache), (suf[:2] + [suf[2][:, :5]], suf, cache, cache)):
+        with pytest.raises(lsp.LspError):
+            lsp.LayerTable(*bad)
+    for bad in ((q, suf, suf, cache, cache, [t.bfloat16() for t in q]), (q, suf, suf, cache, cache, q[:1]), (q[:2] + [q[2][:, :5]], suf, suf, cache, cache, q)):
+        with pytest.raises(lsp.LspError):
+            lsp.AttnLayerTable(*bad)

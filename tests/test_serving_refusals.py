@@ -67,7 +67,8 @@ def test_the_binding_refuses_wrong_tensors(monkeypatch):
     monkeypatch.setattr(m, "_dev", lambda *ts: None)
     monkeypatch.setattr(m, "lib", lambda: pytest.fail("the call reached the library"))
     monkeypatch.setattr(m, "_nat", None)
-    monkeypatch.setattr(m, "_nat_addresses", None)
+    for name in ("_nat_addresses", "_nat_attn_table", "_nat_layer_table"):
+        monkeypatch.setattr(m, name, None)
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32)     # noqa: E731
     f32 = lambda *s: torch.zeros(s)                        # noqa: E731
     z = f32(2, 4, 64)
