@@ -10,14 +10,96 @@ from __future__ import annotations
 
 import torch
 
-from . import (AttnLayerTable, LayerTable, LspError, ProgressPoll, _commit_out, attn_step_layers, commit_step, confidence,
-               confidence_workspace_bytes, lm_head_confidence, lm_head_confidence_workspace_bytes)
+from . import (AttnLayerTable, LayerTable, LspError, ProgressPoll, _commit_out, _need, attn_key_weights_layers, attn_key_weights_workspace_bytes,
+               attn_step_layers, commit_step, confidence, confidence_workspace_bytes, kv_evict, kv_evict_workspace_bytes, kv_gather_append,
+               lm_head_confidence, lm_head_confidence_workspace_bytes, token_scores, token_scores_workspace_bytes)
+
+
+class _Scores:
+    """What the committed tokens' positions are told about them: buffers of one entry per token of the caller's, filled as `tokens` is."""
+
+    def __init__(self, buffers, tokens, V):
+        B, T = tokens.shape
+        unknown = set(buffers) - {"logprob", "entropy", "alt_id", "alt_logprob"}
+        if unknown or not buffers:
+            raise LspError(f"decode_loop: scores are logprob, entropy, alt_id and alt_logprob, got {sorted(buffers)}")
+        if ("alt_id" in buffers) != ("alt_logprob" in buffers):
+            raise LspError("decode_loop: alt_id and alt_logprob come together")
+        self.K = buffers["alt_id"].shape[-1] if "alt_id" in buffers else 0
+        if "alt_id" in buffers and not 1 <= self.K <= 32:
+            raise LspError(f"decode_loop: 1 to 32 alternatives, got {self.K}")
+        for k, t in buffers.items():
+            _need(f"scores['{k}']", t, torch.int32 if k == "alt_id" else torch.float32, (B, T, self.K) if k.startswith("alt") else (B, T))
+        self.buffers, self.out, self.workspace = buffers, None, None
+        self.place = torch.arange(T, device=tokens.device)
+
+    def look(self, z, top1_id, suffix_len):
+        if self.out is None:
+            f = dict(dtype=torch.float32, device=z.device)
+            B, S = top1_id.shape
+            # (zeros: what lies behind the active rows is gathered, though not kept)
+            self.out = (torch.zeros((B, S), **f), torch.zeros((B, S), **f), *((torch.zeros((B, S, self.K), dtype=torch.int32, device=z.device),
+                        torch.zeros((B, S, self.K), **f)) if self.K else (None, None)))
+            self.workspace = torch.empty(max(16, token_scores_workspace_bytes(*z.shape, self.K)), dtype=torch.uint8, device=z.device)
+        token_scores(z, top1_id, suffix_len, num_alt=self.K, out=self.out, workspace=self.workspace)
+
+    def keep(self, prefix_len, commit_len):
+        """Of the tokens just committed, which are the last commit_len[b] before prefix_len[b]."""
+        row = self.place - (prefix_len - commit_len).unsqueeze(1)
+        new = (row >= 0) & (row < commit_len.unsqueeze(1))
+        row = row.clamp(0, self.out[0].shape[1] - 1)
+        for k, src in zip(("logprob", "entropy", "alt_id", "alt_logprob"), self.out):
+            to = self.buffers.get(k)
+            if to is not None and to.dim() == 2:
+                to.copy_(torch.where(new, torch.gather(src, 1, row), to))
+            elif to is not None:
+                to.copy_(torch.where(new.unsqueeze(2), torch.gather(src, 1, row.unsqueeze(2).expand(to.shape)), to))
+
+
+class _Budget:
+    """Caches that are cut back by accumulated attention weight.  Their rows are no longer the sequence's positions: cache_len counts them."""
+
+    def __init__(self, keep, high=None, first=0, recent=0, decay=1.0, cache_len=None, weights=None):
+        self.kw = dict(keep=int(keep), high=int(keep if high is None else high), first=int(first), recent=int(recent))
+        self.decay, self.cache_len, self.weights, self.ready = float(decay), cache_len, weights, False
+
+    def start(self, table, prefix_len, suffix_len):
+        if self.cache_len is None:
+            self.cache_len = prefix_len.clone()
+        k = self.kw
+        if not (0 < k["keep"] <= min(k["high"], table.C) and min(k["first"], k["recent"]) >= 0 and k["first"] + k["recent"] <= k["keep"] and 0 <= self.decay <= 1):
+            raise LspError(f"decode_loop: cache_budget needs 0 < keep <= high, first + recent <= keep and 0 <= decay <= 1, got {k}, decay {self.decay}")
+        shape = (table.n, table.B, table.Hkv, table.C)
+        if self.weights is None:
+            self.weights = torch.zeros(shape, device=prefix_len.device)
+        _need("cache_len", self.cache_len, torch.int32, (table.B,))
+        _need("weights", self.weights, torch.float32, shape)
+        left, rows = torch.stack([suffix_len.max(), (suffix_len + self.cache_len).max()]).tolist()
+        if max(rows, left + self.kw["high"]) > table.C:
+            raise LspError(f"decode_loop: a cache of {table.C} rows has no room for {left} more positions on {self.kw['high']} rows (high), or on those there are")
+
+    def weigh(self, attn, suffix_len):
+        d = attn.desc
+        if not self.ready:
+            self.workspace = torch.empty(max(16, attn_key_weights_workspace_bytes(d.dtype, d.B, d.S, d.Hq, d.Hkv, d.D, d.C, attn.n)), dtype=torch.uint8,
+                                         device=suffix_len.device)
+        attn_key_weights_layers(attn, self.cache_len, suffix_len, self.weights, decay=self.decay, workspace=self.workspace)
+
+    def append(self, table, commit_len):
+        if not self.ready:
+            dev = commit_len.device
+            self.rows = torch.arange(table.S, dtype=torch.int32, device=dev).expand(table.B, table.S).contiguous()
+            self.appended = torch.empty(table.B, dtype=torch.int32, device=dev)
+            self.evict_workspace = torch.empty(max(16, kv_evict_workspace_bytes(table, **self.kw)), dtype=torch.uint8, device=dev)
+            self.ready = True
+        kv_gather_append(self.rows, commit_len, self.cache_len, table, appended=self.appended)
+        kv_evict(self.weights, self.cache_len, table, workspace=self.evict_workspace, **self.kw)
 
 
 def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
                 prefix_len, suffix_len, tokens, kv_layers=None, gen_len=None, run_attention=False,
                 poll=1, max_steps=100000, stop_after=None, observer=None, timed=False, commit_kw=None,
-                graph=False, lm_head_weight=None, flip_window=None, flip_trace=False, state=None):
+                graph=False, lm_head_weight=None, flip_window=None, flip_trace=False, state=None, scores=None, cache_budget=None):
     """logits_fn(step, prefix_len) -> device logits [B,S,V].  prefix_len,
     suffix_len, tokens and the caches in kv_layers (list of dicts q?, k_suf,
     v_suf, k_cache, v_cache) are updated in place.
@@ -45,10 +127,20 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
     same generation start, last-seen ids and flip counters, step numbers going on from
     where it stopped - so that stopping and resuming walks exactly like one uninterrupted
     call.  The sequence state itself (lengths, tokens, caches) is the caller's as always.
+    scores: dict of buffers that take, for every committed token at its place in `tokens`, what the logits it was chosen from
+    say about it (lsp_token_scores): "logprob", "entropy" (fp32 [B,T]), "alt_id", "alt_logprob" (int32 and fp32 [B,T,K], K up
+    to 32); any of them.  Needs the logits, so not together with lm_head_weight.
+    cache_budget: dict(keep[, high, first, recent, decay, cache_len, weights]): caches of bounded length (run_attention and
+    kv_layers needed).  After every step, sequences with more than `high` (default: keep) cached rows are cut back to the `keep`
+    that received most attention, per layer and KV head, beside the first `first` and the last `recent` (lsp_attn_key_weights,
+    lsp_kv_evict); decay: what is left of a weight at the next step (default 1).  The caches' lengths are then cache_len (int32 [B],
+    updated in place; default: a copy of prefix_len), and prefix_len counts tokens alone; weights fp32 [layers,B,Hkv,C] are those that
+    the prompt's rows begin with (default 0).  A cache has to have room for `high` rows and all that is to be generated.  state
+    carries both on.
     A sequence that still has active positions but commits nothing (min_commit = 0, or its
     cache / token buffer is full) would never finish: the loop raises LspError instead.
     Returns dict(steps, flips, flip_denominator, window_flips, window_denominator, committed,
-    state[, flip_trace: int32 [steps,B,2]][, lsp_ms, lsp_ms_steps]); steps, the flip counts
+    state[, flip_trace: int32 [steps,B,2]][, lsp_ms, lsp_ms_steps][, cache_len]); steps, the flip counts
     and committed are totals since the generation began (earlier calls included)."""
     dev = prefix_len.device
     B = prefix_len.shape[0]
@@ -72,6 +164,16 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
     if min_commit < 1 and stop_after is None:
         raise LspError("decode_loop needs min_commit >= 1 (Section 3.2: at least one token per iteration) "
                        "unless stop_after bounds the number of steps")
+    said = budget = None
+    if scores is not None:
+        if lm_head_weight is not None:
+            raise LspError("decode_loop: scores need the logits, which the fused output head does not store")
+        said = _Scores(scores, tokens, V)
+    if cache_budget is not None:
+        if not run_attention or kv_layers is None:
+            raise LspError("decode_loop: a cache budget goes by the attention of kv_layers (run_attention)")
+        kept = {} if state is None else {k: state[k] for k in ("cache_len", "weights") if k in state}
+        budget = _Budget(**{**kept, **cache_budget})
     # Lengths of another type or place are no error with nothing to do.
     ordinary = all(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() for t in (prefix_len, suffix_len, base)) and counters.is_contiguous()
     progress = None
@@ -81,6 +183,9 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
     table = None
     if kv_layers is not None:       # (built while the first test is under way)
         table = LayerTable(*[[L[k] for L in kv_layers] for k in ("k_suf", "v_suf", "k_cache", "v_cache")])
+    if budget is not None:
+        budget.start(table, prefix_len, suffix_len)
+    cached = prefix_len if budget is None else budget.cache_len
     out = conf = None
     attn_out = None
     events = []
@@ -96,7 +201,9 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
                 outs = torch.empty((len(kv_layers), *q.shape), dtype=q.dtype, device=q.device)
                 attn_out = AttnLayerTable(*[[L[k] for L in kv_layers] for k in ("q", "k_suf", "v_suf", "k_cache", "v_cache")],
                                           list(outs.unbind(0)))
-            attn_step_layers(attn_out, prefix_len, suffix_len)     # every layer in one launch
+            attn_step_layers(attn_out, cached, suffix_len)     # every layer in one launch
+            if budget is not None:
+                budget.weigh(attn_out, suffix_len)
         if lm_head_weight is None:
             if ws is None:
                 ws = torch.empty(confidence_workspace_bytes(*z.shape), dtype=torch.uint8, device=dev)
@@ -105,11 +212,17 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
             if ws is None:
                 ws = torch.empty(lm_head_confidence_workspace_bytes(z.shape[0], z.shape[1], V), dtype=torch.uint8, device=dev)
             conf = lm_head_confidence(z, lm_head_weight, suffix_len, out=conf, workspace=ws)
+        if said is not None:
+            said.look(z, conf[0], suffix_len)
         if out is None:
             out = _commit_out(*conf[0].shape, dev)
         commit_step(conf[2], conf[0], bitmap, V, tau, window, min_commit, snap_enabled, prefix_len, suffix_len,
-                    base, last_id, counters, flip_window, step_counts, tokens=tokens, layers=table, C=tokens.shape[1], out=out,
+                    base, last_id, counters, flip_window, step_counts, tokens=tokens, layers=table if budget is None else None, C=tokens.shape[1], out=out,
                     **(commit_kw or {}))
+        if said is not None:
+            said.keep(prefix_len, out["commit_len"])
+        if budget is not None:
+            budget.append(table, out["commit_len"])
 
     while True:
         if (steps - first) % poll == 0:
@@ -160,6 +273,9 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
         committed, *c = totals
     res = dict(steps=steps, flips=c[0], flip_denominator=c[1], window_flips=c[2], window_denominator=c[3],
                committed=committed, state=dict(base=base, last_id=last_id, counters=counters, steps=steps))
+    if budget is not None:
+        res["cache_len"] = budget.cache_len
+        res["state"].update(cache_len=budget.cache_len, weights=budget.weights)
     if flip_trace:
         res["flip_trace"] = torch.stack(trace).cpu() if trace else torch.zeros((0, B, 2), dtype=torch.int32)
     if timed:
