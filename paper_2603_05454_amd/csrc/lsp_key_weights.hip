@@ -101,11 +101,8 @@ __device__ __forceinline__ void step(f32x16 &s, const u32x4 &a, const u32x4 &b, 
 // row of the product that register r of a lane holds (its column: lane % 32)
 __device__ __forceinline__ int product_row(int lane, int r) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-  return d;
-}
+// v_maximum3_f32.  (Not in asm: the compiler has to see that it reads what a matrix instruction wrote, and wait for that.)
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
 // Sum over lane % 32 of 16 numbers: lane l gets the one with number l % 16.  Every step halves what a lane has to send: the partner is the
 // mirror image within 16, 8, 4 and 2 lanes, so that it agrees in the bits that earlier steps went by (46 instructions, 80 for each by itself).
@@ -374,7 +371,7 @@ struct LogSum {
     float top = max3(s[0], s[1], s[2]);
 #pragma unroll
     for (int r = 3; r < 15; r += 2) top = max3(top, s[r], s[r + 1]);
-    top = fmaxf(top, s[15]) * sc;
+    top = max3(top, s[15], s[15]) * sc;
     if (__any(top > ref + 8.f)) {
       const float to = fmaxf(top, ref), f = __builtin_amdgcn_exp2f(ref - to);
       sum *= f;

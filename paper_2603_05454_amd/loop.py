@@ -73,6 +73,8 @@ class _Budget:
         if self.weights is None:
             self.weights = torch.zeros(shape, device=prefix_len.device)
         _need("cache_len", self.cache_len, torch.int32, (table.B,))
+        if self.cache_len.data_ptr() in (prefix_len.data_ptr(), suffix_len.data_ptr()):
+            raise LspError("decode_loop: cache_len is a buffer of its own")
         _need("weights", self.weights, torch.float32, shape)
         left, rows = torch.stack([suffix_len.max(), (suffix_len + self.cache_len).max()]).tolist()
         if max(rows, left + self.kw["high"]) > table.C:

@@ -149,7 +149,8 @@ def test_refusals(lsp):
     s = _start(w)
     f = torch.zeros((3, w.C), device="cuda")
     for kw, text in ((dict(cache_budget=dict(keep=w.C - 10)), "no room"), (dict(cache_budget=dict(keep=44, weights=f)), "weights must"),
-                     (dict(cache_budget=dict(keep=44, cache_len=s["prefix_len"].long())), "cache_len must"), (dict(scores=dict(margin=f)), "scores are"),
+                     (dict(cache_budget=dict(keep=44, cache_len=s["prefix_len"].long())), "cache_len must"),
+                     (dict(cache_budget=dict(keep=44, cache_len=s["prefix_len"])), "buffer of its own"), (dict(scores=dict(margin=f)), "scores are"),
                      (dict(scores={}), "scores are"), (dict(scores=dict(logprob=f[:, 1:])), "must have shape"), (dict(scores=dict(alt_id=f)), "come together"),
                      (dict(scores=dict(logprob=f), lm_head_weight=f), "logits"), (dict(cache_budget=dict(keep=44, first=40, recent=5)), "first"),
                      (dict(cache_budget=dict(keep=44, decay=2)), "decay"), (dict(cache_budget=dict(keep=44, high=43)), "high")):
