@@ -2,16 +2,26 @@
 //
 // With c = scale log2(e) and L[h,i] the base-2 logarithm of the sum over all keys of 2^(c q.k):
 //   mass[g,t] = sum over heads h of group g and rows i < N of 2^(c q[i,h].k[t,g] - L[h,i])
-// Two kernels: row_log_kernel computes L of every row, key_sum_kernel the sums down the columns, each from its own product of queries
-// and keys.  (The products kept instead would be 1.3e9 numbers a layer at 8 x 1024 rows of 32 heads on 4096.)
 //
-// Both are the same loop with the operands exchanged.  A wave holds NS blocks of 32 rows of one operand as matrix fragments in registers (queries for
+// Units are (layer, sequence, KV head); the rows of all heads of a group are one list (entry e: row e % N of head e / N), since they meet the same
+// keys.  Three kernels, each of which takes the units whose lengths, known on the device alone, are its own:
+//   few_rows_kernel   up to 64 rows and as many keys as eight waves have registers for scores of (2048 with 32 rows, 768 with 64): one product, one
+//                     exponential a score.  Bound by the bytes of the keys: 8 layers of 32 heads, 16 x 21 rows on 1536 keys, 1.7 GB, 324 us = 5.2 TB/s.
+//   row_log_kernel    L of every other row, and
+//   key_sum_kernel    the sums down the columns, each from its own product of queries and keys.  (The products kept between them would be 1.3e9 numbers a layer
+//                     at 8 x 1024 rows of 32 heads on 5120 keys.)  Bound by instructions and power: there 376 and 388 us, 0.92 PFLOP/s, with vector
+//                     instructions in 55-64 % of the cycles, matrix instructions in 43-45 %, at 1.95 GHz.  The two do not overlap further in any order that
+//                     was tried (all of the one, then all of the other; halves; exponents, powers and additions a step apart: 753-774 us
+//                     in all for 735), and the attention of the same products, by hand and with half the exponentials, takes 595 us, at the power limit.
+// More rows than there are keys for, or fewer: both of the latter divide what is long, rows or keys, among workgroups that the others leave free
+// (kGroups); one layer of 4 x 497 rows of 28 heads on 4 KV heads and 1500 keys 80 -> 55 us.
+//
+// The last two are the same loop with the operands exchanged.  A wave holds NS blocks of 32 rows of one operand as matrix fragments in registers (queries for
 // the logarithms, keys for the sums) and all four waves of the workgroup read the other one from LDS, 32 rows at a time, from a ring that
 // is filled by loads that go straight to LDS.  Scores come out transposed, keys x queries (v_mfma_f32_32x32x16_bf16, or 32x32x2 in fp32),
 // so a lane's 16 scores are of ONE query: its reference and sum, or its L, are per-lane numbers, and nothing crosses lanes in the loop:
 // the logarithm joins two lanes at the end, the sums of a key stay one register for each of the wave's 32 x NS keys and are reduced over
-// 32 lanes once.  The rows of all heads of a group are one list (entry e: row e % N of head e / N), since they meet the same keys.
-// Everything is summed in fp32, in an order that sizes alone decide.
+// 32 lanes once.  Scores, exponentials and sums are fp32, in an order that sizes alone decide.
 #include <math.h>
 
 #include <type_traits>
@@ -35,14 +45,14 @@ constexpr int kMaxParts = 16;        // of the keys, for the logarithms of few r
 constexpr int kPartKeys = 128;       // a part has at least
 constexpr int kPartRows = 128;       // a part of the rows, for the sums of few keys, has at least
 constexpr int kGroups = 512;         // workgroups that a launch is divided into where it can be: two to a compute unit
-// Keys of more bytes than this (as many as the attention's K/V, which are twice that) are loaded with the non-temporal hint: 8 layers of 32 heads, 16 x 21
-// rows on 1536 keys, 1.6 GB, 343 -> 332 us.
+// Keys of more bytes than this (as many as the attention's K/V, which are twice that) are loaded with the non-temporal hint: in the case above
+// 343 -> 332 us.
 constexpr int64_t kOnceBytes = int64_t(160) << 20;
 constexpr float kFarBelow = -1.7e38f;  // a reference below all scores
 
 struct WeightArgs {
   const int32_t *prefix_len, *suffix_len;
-  int32_t B, S, Hq, Hkv, D, C, rep, layers;
+  int32_t B, S, Hkv, C, rep;
   int32_t units, groups, spread, max_parts;  // (layer, sequence, KV head)s; workgroups of one; each unit in 2^spread pieces
   int32_t log_rows;  // rows of a workgroup of row_log_kernel
   uint32_t tag;      // of the call, beside numbers that workgroups hand over
@@ -928,7 +938,7 @@ extern "C" int32_t lsp_attn_key_weights(const lsp_attn_desc *d, int32_t num_laye
   }
   WeightArgs a = {};
   a.prefix_len = prefix_len; a.suffix_len = suffix_len;
-  a.B = at.B; a.S = at.S; a.Hq = at.Hq; a.Hkv = at.Hkv; a.D = at.D; a.C = at.C; a.rep = at.Hq / at.Hkv;
+  a.B = at.B; a.S = at.S; a.Hkv = at.Hkv; a.C = at.C; a.rep = at.Hq / at.Hkv;
   a.scale = at.scale; a.decay = decay;
   const int64_t es = int64_t(elem_size(d->dtype));
   for (int k = 0; k < 3; ++k) a.qs[k] = at.qs[k] * es, a.ks[k] = at.ks[k] * es, a.cs[k] = at.cs[k] * es;
@@ -937,12 +947,12 @@ extern "C" int32_t lsp_attn_key_weights(const lsp_attn_desc *d, int32_t num_laye
   a.max_parts = max_parts(d, num_layers);
   hipStream_t st = static_cast<hipStream_t>(stream);
   for (int l0 = 0; l0 < num_layers; l0 += kMaxAttnLayers) {
-    a.layers = layers_at_once(num_layers - l0);
-    a.units = a.layers * a.B * a.Hkv;
+    const int layers = layers_at_once(num_layers - l0);
+    a.units = layers * a.B * a.Hkv;
     a.tag = call_tag();
     WeightLayers L;
     for (int l = 0; l < kMaxAttnLayers; ++l) {
-      const int s = l < a.layers ? l0 + l : l0;  // unused slots repeat a valid layer
+      const int s = l < layers ? l0 + l : l0;  // unused slots repeat a valid layer
       L.q[l] = static_cast<const char *>(q_layers[s]);
       L.k_suf[l] = static_cast<const char *>(k_suf_layers[s]);
       L.k_cache[l] = static_cast<const char *>(k_cache_layers[s]);
