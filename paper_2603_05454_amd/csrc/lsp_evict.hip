@@ -4,7 +4,7 @@
 // Which rows stay: the first `first`, the last `recent`, and of the others the largest weights (equal ones: the lower row).  The weights'
 // bits, mapped to whole numbers of the same order, are in registers (16 a thread, which is 8192 rows); the smallest that stays is
 // found by halving the interval between the least and the largest, a count over the workgroup each time, until as many are at or above the
-// middle as there are places.  (A histogram of their leading bits, which accumulated weights share, is a queue for few counters in LDS.)
+// middle as there are places, or until those between are at most 64, which are ranked by counting.  (A histogram of their leading bits, which accumulated weights share, is a queue for few counters in LDS.)
 // With ties at the end, the row up to which the equal ones stay is found in the same way.
 //
 // Where they go: keys carry their positions and the attention has no mask, so the order of cached rows means nothing.  Rows
@@ -12,9 +12,9 @@
 // one to the n-th of the other).  That moves at most P - keep rows, where closing the gaps in order moves every row behind the first
 // one.  Sources are all at or above `keep` and destinations below, so nothing that is read is written.
 //
-// What bounds it: HBM, for the rows that move (8 layers, 8 x about 4860 rows of 32 heads cut to 4096: 1.6 GB read and written in 341 us, a large copy's
-// 4.8 TB/s), and where they are few the selection's chain of counts, each a trip to LDS and a barrier (one layer of four heads, 700 rows cut to 512:
-// 12 us; 32 layers of 32 heads, 1280 rows cut to 1024: 62 us for 0.25 GB).  Few units (layer, sequence, KV head) with many rows to
+// What bounds it: HBM, for the rows that move (8 layers, 8 x about 4860 rows of 32 heads cut to 4096: 1.6 GB read and written in 341-361 us, 0.93-0.98 of a
+// large copy's rate), and where they are few the selection's chain of counts, each a trip to LDS and a barrier (loops end at the last row: sixteen branches not taken are as much; one layer of four heads, 700 rows cut to 512:
+// 9.2 us; 32 layers of 32 heads, 1280 rows cut to 1024: 59 us for 0.25 GB).  Few units (layer, sequence, KV head) with many rows to
 // move take several workgroups each, which all find the same rows and move a part of them.
 #include "lsp_attn.h"
 
@@ -22,11 +22,13 @@ namespace lsp {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kKeys = 16;                     // of a thread (with them 60 registers: four workgroups share a compute unit)
 constexpr int kBlock = kThreads * kKeys;      // rows whose weights are in registers at a time
+constexpr int kFew = kWave;                   // rows that are ranked by counting
 constexpr int kWindow = 2048;                 // moves that are listed in LDS at a time
 constexpr int kMaxParts = 16;                 // workgroups of a unit
 constexpr int64_t kPartBytes = 256 << 10;     // to be moved, a workgroup's at least
@@ -55,6 +57,29 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
   if ((u & 0x7fffffffu) > 0x7f800000u) return 1;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Over a wave on the DPP network: the maximum, in every lane, and the sum up to and with the lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#define LSP_DPP(x, ctrl, rows) uint32_t(__builtin_amdgcn_update_dpp(0, int(x), ctrl, rows, 0xf, false))
+  v = max(v, LSP_DPP(v, 0x111, 0xf));  // row_shr:1
+  v = max(v, LSP_DPP(v, 0x112, 0xf));  // row_shr:2
+  v = max(v, LSP_DPP(v, 0x114, 0xf));  // row_shr:4
+  v = max(v, LSP_DPP(v, 0x118, 0xf));  // row_shr:8
+  v = max(v, LSP_DPP(v, 0x142, 0xa));  // row_bcast:15 into rows 1 and 3
+  v = max(v, LSP_DPP(v, 0x143, 0xc));  // row_bcast:31 into rows 2 and 3
+  return uint32_t(__builtin_amdgcn_readlane(int(v), kWave - 1));
+}
+__device__ __forceinline__ int sum_upto(int n) {
+  uint32_t v = uint32_t(n);
+  v += LSP_DPP(v, 0x111, 0xf);
+  v += LSP_DPP(v, 0x112, 0xf);
+  v += LSP_DPP(v, 0x114, 0xf);
+  v += LSP_DPP(v, 0x118, 0xf);
+  v += LSP_DPP(v, 0x142, 0xa);
+  v += LSP_DPP(v, 0x143, 0xc);
+#undef LSP_DPP
+  return int(v);
 }
 
 // Numbers of all waves, of which each has one (in every lane).
@@ -87,7 +112,9 @@ struct Meeting {
 // ONE: a unit's rows are one block, whose weights are read once.
 template <bool ONE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 8 : 1))) void evict_kernel(EvictArgs a, CachePtrs p) {
-  __shared__ int s_meet[2 * kWaves], s_places[2][kKeys * kWaves], s_total[2], s_dst[kWindow], s_src[kWindow];
+  __shared__ __attribute__((aligned(16))) int s_meet[2 * kWaves];
+  __shared__ int s_places[2][kKeys * kWaves], s_total[2], s_src[kWindow];
+  __shared__ __attribute__((aligned(16))) int s_dst[kWindow];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int g = blockIdx.x, b = blockIdx.y, l = blockIdx.z / a.parts, part = blockIdx.z - l * a.parts, unit = (l * a.B + b) * a.Hkv + g;
   const int P = min(max(a.prefix_len[b], 0), a.C);
@@ -122,6 +149,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
     const int own = here_tid();
 #pragma unroll
     for (int r = 0; r < kKeys; ++r) {
+      if (blk * kBlock + r * kThreads >= P) break;
       const int t = blk * kBlock + r * kThreads + own;
       key[r] = t >= a.first && t < end ? order_of(w[t]) : 0;
     }
@@ -134,8 +162,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
       if (!ONE) load(blk);
       const int own = here_tid();
 #pragma unroll
-      for (int r = 0; r < kKeys; ++r)
-        if (blk * kBlock + r * kThreads < P) n += __popcll(__ballot(in(key[r], blk * kBlock + r * kThreads + own)));
+      for (int r = 0; r < kKeys; ++r) {
+        if (blk * kBlock + r * kThreads >= P) break;
+        n += __popcll(__ballot(in(key[r], blk * kBlock + r * kThreads + own)));
+      }
     }
     return meet.sum(n);
   };
@@ -147,32 +177,52 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
       if (!ONE) load(blk);
 #pragma unroll
       for (int r = 0; r < kKeys; ++r) {
+        if (blk * kBlock + r * kThreads >= P) break;
         top = max(top, key[r]);
         low = max(low, key[r] == 0 ? 0u : ~key[r]);
       }
     }
-#pragma unroll
-    for (int m = 1; m < kWave; m <<= 1) {
-      top = max(top, uint32_t(__shfl_xor(int(top), m)));
-      low = max(low, uint32_t(__shfl_xor(int(low), m)));
-    }
     // at least `places` are at or above lo, fewer at or above hi
-    uint32_t lo = ~meet.most(low), hi = meet.most(top) + 1;
-    int above = 0;
-    bool exact = false;
-    while (hi - lo > 1) {
+    uint32_t lo = ~meet.most(wave_max(low)), hi = meet.most(wave_max(top)) + 1;
+    int from_lo = end - a.first, above = 0;  // how many
+    while (hi - lo > 1 && from_lo != places && from_lo - above > kFew) {
       const uint32_t mid = lo + (hi - lo) / 2;
       const int n = count([&](uint32_t k, int) { return k >= mid; });
-      if (n >= places) lo = mid;
+      if (n >= places) lo = mid, from_lo = n;
       else hi = mid, above = n;
-      if (n == places) {
-        exact = true;
-        break;
-      }
     }
     least = lo;
     upto = P;
-    if (!exact) {  // the largest row with fewer than as many equal ones before it as there are places left
+    if (from_lo != places && from_lo - above <= kFew) {  // those between are ranked
+      uint64_t *few = reinterpret_cast<uint64_t *>(s_dst);
+      if (tid < kFew) few[tid] = 0;
+      if (tid == 0) s_total[0] = 0;
+      __syncthreads();
+      for (int blk = 0; blk < blocks; ++blk) {
+        if (!ONE) load(blk);
+        const int own = here_tid();
+#pragma unroll
+        for (int r = 0; r < kKeys; ++r) {
+          if (blk * kBlock + r * kThreads >= P) break;
+          if (key[r] >= lo && key[r] < hi) few[atomicAdd(&s_total[0], 1)] = uint64_t(key[r]) << 32 | uint32_t(~(blk * kBlock + r * kThreads + own));
+        }
+      }
+      __syncthreads();
+      if (tid < kFew) {
+        const uint64_t mine = few[tid];
+        int before = 0;
+#pragma unroll 4
+        for (int k = 0; k < kFew; k += 2) {
+          const u64x2 x = *reinterpret_cast<const u64x2 *>(few + k);
+          before += (x.x > mine) + (x.y > mine);
+        }
+        if (before == places - above - 1) s_total[0] = int(mine >> 32), s_total[1] = ~int(uint32_t(mine));
+      }
+      __syncthreads();
+      least = uint32_t(s_total[0]);
+      upto = s_total[1];
+      __syncthreads();
+    } else if (from_lo != places) {  // equal ones: the largest row with fewer than as many equal ones before it as there are places left
       const int equal = places - above;
       upto = 0;
       int bit = 1;
@@ -193,6 +243,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
       const int own = here_tid();
 #pragma unroll
       for (int r = 0; r < kKeys; ++r) {
+        if (blk * kBlock + r * kThreads >= P) break;
         const int t = blk * kBlock + r * kThreads + own;
         const bool s = stays(key[r], t);
         hole |= uint32_t(t < a.keep && !s) << r;
@@ -207,13 +258,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
       if (wave < 2) {  // the numbers before each: two per lane
         int *at = s_places[wave];
         static_assert(kKeys * kWaves == 2 * kWave, "two per lane");
-        const int x = at[2 * lane], y = at[2 * lane + 1];
-        int before = x + y;
-#pragma unroll
-        for (int m = 1; m < kWave; m <<= 1) {
-          const int from = __shfl_up(before, m);
-          if (lane >= m) before += from;
-        }
+        const bool there = blk * kBlock + lane / (kWaves / 2) * kThreads < P;  // (those of the same r)
+        const int x = there ? at[2 * lane] : 0, y = there ? at[2 * lane + 1] : 0, before = sum_upto(x + y);
         if (lane == kWave - 1) s_total[wave] = before;
         at[2 * lane] = before - x - y;
         at[2 * lane + 1] = before - y;
