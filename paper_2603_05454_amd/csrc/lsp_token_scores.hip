@@ -41,7 +41,7 @@ constexpr float kLagOctaves = 8.0f;
 // that holds one, or a row of nothing else, takes a way of its own.
 constexpr float kLow = -1e37f;
 constexpr int kMaxAlt = 32;
-constexpr int kRankStep = 8;    // entries that are read at a time
+constexpr int kRankStep = 16;   // entries that are read at a time
 constexpr int kMinCut = 16384;  // rows of at most this many entries are not cut
 
 template <typename T>
@@ -176,7 +176,8 @@ __device__ __forceinline__ int group_sum(Shared<NT> &sh, int n) {
 }
 
 // The best K of `n` entries in LDS and of sh.best go to sh.best.  Every thread calls it, after a barrier; there is room for K + kRankStep entries more.
-// Eight are read at a time: one by one the trip to LDS is waited for at each (8 rows of 82 303 entries, cut into 16 segments, 20 alternatives: 19.2 us).
+// Sixteen are read at a time: one by one the trip to LDS is waited for at each (8 rows of 82 303 entries, cut into 16 segments, 20 alternatives, eight at a
+// time: 19.2 -> 15.0 us).
 template <int NT>
 __device__ __forceinline__ void rank_entries(Shared<NT> &sh, uint64_t *entries, int n, int K) {
   typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
@@ -243,6 +244,19 @@ __device__ __forceinline__ Stat scan_segment(const T *row, int c0, int c1, int K
   if (has_head) one(at_head = Vec<T>::scalar(row + c0 + tid));
   if (has_tail) one(at_tail = Vec<T>::scalar(row + tail0 + tid));
 
+  auto statistics = [&]() {  // lanes, then waves
+    Stat own = a;
+    const float top = wave_max(a.m);
+    take_to(own, a.m == -INFINITY ? -INFINITY : __builtin_fmaf(-top, kLog2e, r));  // (the product unrounded inside the fma)
+    Stat of_wave = {top, wave_sum(own.s), wave_sum(own.t)};
+    if (NT == kWave) return of_wave;
+    if (lane == 0) sh.stat[wave] = of_wave;
+    __syncthreads();
+    Stat w = {-INFINITY, 0.f, 0.f};
+    if (lane < NT / kWave) w = sh.stat[lane];
+    return merge_stats(w);
+  };
+  Stat all;
   const std::false_type full;
   const std::true_type maybe_partial;
   // Lanes past the end of a last, partial group read the last vector again, with -inf in the place of its values.
@@ -370,17 +384,20 @@ __device__ __forceinline__ Stat scan_segment(const T *row, int c0, int c1, int K
       __syncthreads();
       left = sh.count;
     }
+    const int again = v0 + (tid < left ? sh.vectors[tid] : 0);
+    u32x4 entered = {};
+    if (tid < left) entered = vp[again];
+    if (v1 == nvec) all = statistics();  // (while they come)
     // (the maxima's place becomes the entries')
     auto enter = [&](float x, int index) {
       const uint32_t k = key_of(x);
       if (k >= least) entries[atomicAdd(&sh.entries, 1)] = entry_of(k, index);
     };
     if (tid < left) {
-      const int v = v0 + sh.vectors[tid];
       float x[N];
-      Vec<T>::unpack(vp[v], x);
+      Vec<T>::unpack(entered, x);
 #pragma unroll
-      for (int k = 0; k < N; ++k) enter(x[k], vbase + v * N + k);
+      for (int k = 0; k < N; ++k) enter(x[k], vbase + again * N + k);
     }
     if (v0 == 0 && has_head) enter(at_head, c0 + tid);
     if (v1 == nvec && has_tail) enter(at_tail, tail0 + tid);
@@ -388,18 +405,7 @@ __device__ __forceinline__ Stat scan_segment(const T *row, int c0, int c1, int K
     rank_entries<NT>(sh, entries, sh.entries, K);
   }
 
-  // lanes, then waves
-  Stat own = a;
-  const float top = wave_max(a.m);
-  take_to(own, a.m == -INFINITY ? -INFINITY : __builtin_fmaf(-top, kLog2e, r));  // (the product unrounded inside the fma)
-  Stat all = {top, wave_sum(own.s), wave_sum(own.t)};
-  if (NT > kWave) {
-    if (lane == 0) sh.stat[wave] = all;
-    __syncthreads();
-    Stat w = {-INFINITY, 0.f, 0.f};
-    if (lane < NT / kWave) w = sh.stat[lane];
-    all = merge_stats(w);
-  }
+  if (!ALT) all = statistics();
   if (all.m < kLow && all.m > -INFINITY) {  // (uniform) a row of nothing but lowest values: differences first
     __syncthreads();
     Stat w = {all.m, 0.f, 0.f};
