@@ -204,7 +204,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
 #pragma unroll
         for (int r = 0; r < kKeys; ++r) {
           if (blk * kBlock + r * kThreads >= P) break;
-          if (key[r] >= lo && key[r] < hi) few[atomicAdd(&s_total[0], 1)] = uint64_t(key[r]) << 32 | uint32_t(~(blk * kBlock + r * kThreads + own));
+          if (key[r] >= lo && key[r] < hi) {
+            const int at = atomicAdd(&s_total[0], 1);
+            if (at < kFew) few[at] = uint64_t(key[r]) << 32 | uint32_t(~(blk * kBlock + r * kThreads + own));
+          }
         }
       }
       __syncthreads();

@@ -138,7 +138,7 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
     lsp_kv_evict); decay: what is left of a weight at the next step (default 1).  The caches' lengths are then cache_len (int32 [B],
     updated in place; default: a copy of prefix_len), and prefix_len counts tokens alone; weights fp32 [layers,B,Hkv,C] are those that
     the prompt's rows begin with (default 0).  A cache has to have room for `high` rows and all that is to be generated.  state
-    carries both on.
+    carries both on (those of cache_budget are not looked at then).
     A sequence that still has active positions but commits nothing (min_commit = 0, or its
     cache / token buffer is full) would never finish: the loop raises LspError instead.
     Returns dict(steps, flips, flip_denominator, window_flips, window_denominator, committed,
@@ -175,7 +175,9 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
         if not run_attention or kv_layers is None:
             raise LspError("decode_loop: a cache budget goes by the attention of kv_layers (run_attention)")
         kept = {} if state is None else {k: state[k] for k in ("cache_len", "weights") if k in state}
-        budget = _Budget(**{**kept, **cache_budget})
+        budget = _Budget(**{**cache_budget, **kept})
+    elif kv_layers is not None and state is not None and "cache_len" in state:
+        raise LspError("decode_loop: this state's caches were cut back (cache_len): it goes on with a cache_budget")
     # Lengths of another type or place are no error with nothing to do.
     ordinary = all(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() for t in (prefix_len, suffix_len, base)) and counters.is_contiguous()
     progress = None

@@ -130,6 +130,8 @@ def test_stopping_and_resuming_a_bounded_loop(lsp, graph):
     while parts["suffix_len"].max() > 0:
         b = _loop(w, parts, graph=graph, cache_budget=BUDGET, stop_after=3, state=None if b is None else b["state"])
         calls += 1
+        with pytest.raises(lsp.LspError, match="cut back"):
+            _loop(w, parts, graph=graph, state=b["state"])
     assert calls > 2 and a["steps"] == b["steps"] and torch.equal(a["cache_len"], b["cache_len"])
     assert torch.equal(a["state"]["weights"], b["state"]["weights"]) and all(torch.equal(x, y) for x, y in zip(_state(whole), _state(parts)))
 
@@ -159,3 +161,16 @@ def test_refusals(lsp):
     with pytest.raises(lsp.LspError, match="run_attention"):
         from paper_2603_05454_amd.loop import decode_loop
         decode_loop(None, s["bitmap"], w.V, 0.9, 16, 1, 1, s["prefix_len"], s["suffix_len"], s["tokens"], cache_budget=dict(keep=4))
+
+
+def test_a_states_weights_and_lengths_go_before_those_of_the_budget(lsp):
+    """The same dictionary may be handed over at every call, though its tensors are copies that stayed behind."""
+    w = _work()
+    whole, parts = _start(w), _start(w)
+    f = torch.rand((len(whole["kv_layers"]), whole["prefix_len"].shape[0], w.Hkv, w.C), device="cuda")
+    given = lambda s: dict(BUDGET, weights=f.clone(), cache_len=torch.full_like(s["prefix_len"], 30))      # noqa: E731
+    a = _loop(w, whole, cache_budget=given(whole))
+    b = _loop(w, parts, cache_budget=given(parts), stop_after=4)
+    b = _loop(w, parts, cache_budget=given(parts), state=b["state"])
+    assert torch.equal(a["cache_len"], b["cache_len"]) and torch.equal(a["state"]["weights"], b["state"]["weights"])
+    assert all(torch.equal(x, y) for x, y in zip(_state(whole), _state(parts)))
