@@ -172,3 +172,13 @@ def test_tables_made_natively_and_in_python_are_the_same(lsp, monkeypatch):
     for bad in ((q, suf, suf, cache, cache, [t.bfloat16() for t in q]), (q, suf, suf, cache, cache, q[:1]), (q[:2] + [q[2][:, :5]], suf, suf, cache, cache, q)):
         with pytest.raises(lsp.LspError):
             lsp.AttnLayerTable(*bad)
+
+
+@pytest.mark.parametrize("P", [70, 700, 9000])
+@pytest.mark.parametrize("same", [2, 10, 63, 64, 65, 200])
+def test_groups_of_equal_weights_at_the_end(lsp, P, same):
+    """The last place falls inside a group of equal weights, below, at and above the number of rows that are ranked one by one."""
+    w = torch.arange(P).div(same, rounding_mode="floor").float()
+    w = torch.stack([w, w.flip(0), w[torch.randperm(P, generator=torch.Generator().manual_seed(same))]]).reshape(1, 1, 3, P)
+    for keep in (P // 2, P - 1, 3):
+        _run(lsp, 1, 1, 3, 64, P, [P], keep, w=w)
