@@ -4,7 +4,8 @@
 // Which rows stay: the first `first`, the last `recent`, and of the others the largest weights (equal ones: the lower row).  The weights'
 // bits, mapped to whole numbers of the same order, are in registers (16 a thread, which is 8192 rows); the smallest that stays is
 // found by halving the interval between the least and the largest, a count over the workgroup each time, until as many are at or above the
-// middle as there are places, or until those between are at most 64, which are ranked by counting.  (A histogram of their leading bits, which accumulated weights share, is a queue for few counters in LDS.)
+// middle as there are places, or until those between are at most 64, which are ranked by counting.  (A histogram of the weights' leading bits,
+// which accumulated weights share, is a queue for few counters in LDS.)
 // With ties at the end, the row up to which the equal ones stay is found in the same way.
 //
 // Where they go: keys carry their positions and the attention has no mask, so the order of cached rows means nothing.  Rows
@@ -12,10 +13,11 @@
 // one to the n-th of the other).  That moves at most P - keep rows, where closing the gaps in order moves every row behind the first
 // one.  Sources are all at or above `keep` and destinations below, so nothing that is read is written.
 //
-// What bounds it: HBM, for the rows that move (8 layers, 8 x about 4860 rows of 32 heads cut to 4096: 1.6 GB read and written in 341-361 us, 0.93-0.98 of a
-// large copy's rate), and where they are few the selection's chain of counts, each a trip to LDS and a barrier (loops end at the last row: sixteen branches not taken are as much; one layer of four heads, 700 rows cut to 512:
-// 9.2 us; 32 layers of 32 heads, 1280 rows cut to 1024: 59 us for 0.25 GB).  Few units (layer, sequence, KV head) with many rows to
-// move take several workgroups each, which all find the same rows and move a part of them.
+// What bounds it: HBM, for the rows that move (8 layers, 8 x about 4860 rows of 32 heads cut to 4096: 1.6 GB read and written in 310-361 us, about a
+// large copy's rate), and where they are few the selection's chain of counts, each a trip to LDS and a barrier (one layer of four heads, 700 rows cut
+// to 512: 9.2 us; 32 layers of 32 heads, 1280 rows cut to 1024: 59 us for 0.25 GB).  There it counts that loops end at the last row, and that
+// waves add up on the DPP network: together 12.5 -> 9.2 us.  Few units (layer, sequence, KV head) with many rows to move take several workgroups
+// each, which all find the same rows and move a part of them.
 #include "lsp_attn.h"
 
 namespace lsp {

@@ -16,10 +16,10 @@
 // (K / waves)-th largest lane maximum; vectors below T are out, and usually few more than K are left.  If more are left than there are threads
 // (rows of equal entries), a search bit by bit finds the K-th one exactly.
 //
-// What bounds it: HBM with many rows (each byte read once: 8 x 1024 bf16 rows of 152 064 entries with 20 alternatives, 2.5 GB, 395 us = 6.3 TB/s,
+// What bounds it: HBM with many rows (each byte read once: 8 x 1024 bf16 rows of 152 064 entries with 20 alternatives, 2.5 GB, 388 us = 6.4 TB/s,
 // a bare read's rate; 438 us with ordinary instead of non-temporal loads).  With few, latencies: the trip through a row, the
-// vectors read once more, ranks, and the segments' meeting, 1-4 us each (one row of 126 464 entries 9.9 us, 127 of them 16.8, 364 fp32 rows of 30 001
-// 15.5).  Where few rows are active they are cut into segments, whose results meet in the workspace as in confidence_split_kernel
+// vectors read once more, ranks, and the segments' meeting, 1-4 us each (one row of 126 464 entries 9.5 us, 127 of them 16.4, 364 fp32 rows of 30 001
+// 15.1).  Where few rows are active they are cut into segments, whose results meet in the workspace as in confidence_split_kernel
 // (numbers with the call's tag beside them).
 #include <float.h>
 #include <limits.h>
