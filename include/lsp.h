@@ -417,7 +417,8 @@ size_t lsp_token_scores_workspace_bytes(int32_t B, int32_t S, int32_t V, int32_t
  * device fp32 [B,S].  num_alt = K: 0..32; alt_id (int32), alt_logprob (fp32): device
  * [B,S,K], NULL where K = 0.  workspace: device, 16-byte aligned, of any content, for this
  * call alone until it has run; with NULL or fewer bytes than
- * lsp_token_scores_workspace_bytes a row is one workgroup's.
+ * lsp_token_scores_workspace_bytes a row is one workgroup's.  Limits: B, S <= 65535,
+ * V <= 2^30.
  */
 int32_t lsp_token_scores(int32_t dtype, const void *logits, int32_t B, int32_t S, int32_t V, int64_t row_stride,
                          int64_t batch_stride, const int32_t *suffix_len, const int32_t *token_id, int32_t num_alt,
@@ -443,7 +444,8 @@ size_t lsp_attn_key_weights_workspace_bytes(const lsp_attn_desc *desc, int32_t n
  * lsp_attn_step_layers (o_stride is not used; V is not needed).  decay: 0 to 1.
  * weights: device fp32 [num_layers, B, Hkv, C], dense.  workspace: device, 16-byte
  * aligned, lsp_attn_key_weights_workspace_bytes(desc, num_layers) bytes of any
- * content, for this call alone until it has run.  Limit: B * Hq <= 65535.
+ * content, for this call alone until it has run.  Limits: B * Hq <= 65535, C + S and
+ * S * Hq / Hkv <= 2^30.
  */
 int32_t lsp_attn_key_weights(const lsp_attn_desc *desc, int32_t num_layers, const void *const *q_layers,
                              const void *const *k_suf_layers, const void *const *k_cache_layers,

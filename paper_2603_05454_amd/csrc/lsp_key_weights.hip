@@ -922,6 +922,7 @@ extern "C" int32_t lsp_attn_key_weights(const lsp_attn_desc *d, int32_t num_laye
   LSP_CHECK_ARG(q_layers && k_suf_layers && k_cache_layers && prefix_len && suffix_len && weights, "lsp_attn_key_weights: null pointer");
   LSP_CHECK_ARG(decay >= 0.f && decay <= 1.f, "lsp_attn_key_weights: decay must be in [0, 1] (got %g)", double(decay));
   LSP_CHECK_ARG(int64_t(d->B) * d->Hq <= 65535, "lsp_attn_key_weights: B * Hq must be <= 65535");
+  LSP_CHECK_ARG(int64_t(d->C) + d->S <= 1 << 30 && int64_t(d->Hq / d->Hkv) * d->S <= 1 << 30, "lsp_attn_key_weights: C + S and S * Hq / Hkv must be <= 2^30");
   for (int l = 0; l < num_layers; ++l) {
     LSP_CHECK_ARG(q_layers[l] && k_suf_layers[l] && k_cache_layers[l], "lsp_attn_key_weights: null operand in layer %d", l);
     LSP_CHECK_ARG(aligned16(q_layers[l]) && aligned16(k_suf_layers[l]) && aligned16(k_cache_layers[l]),

@@ -620,6 +620,7 @@ extern "C" int32_t lsp_token_scores(int32_t dtype, const void *logits, int32_t B
   LSP_CHECK_ARG(dtype == LSP_F32 || dtype == LSP_BF16, "lsp_token_scores: unknown dtype %d", dtype);
   LSP_CHECK_ARG(B > 0 && S > 0 && V > 0, "lsp_token_scores: need B>0, S>0, V>0 (got %d %d %d)", B, S, V);
   LSP_CHECK_ARG(B <= 65535 && S <= 65535, "lsp_token_scores: B and S must be <= 65535");
+  LSP_CHECK_ARG(V <= 1 << 30, "lsp_token_scores: V must be <= 2^30");
   LSP_CHECK_ARG(num_alt >= 0 && num_alt <= kMaxAlt, "lsp_token_scores: num_alt must be 0..%d (got %d)", kMaxAlt, num_alt);
   LSP_CHECK_ARG(logits && entropy, "lsp_token_scores: null pointer");
   LSP_CHECK_ARG((token_id != nullptr) == (logprob != nullptr), "lsp_token_scores: token_id and logprob come together");

@@ -61,6 +61,17 @@ def test_evict_entry_point():
     assert L.lsp_kv_evict_workspace_bytes(None) == 0
 
 
+def test_sizes_beyond_what_is_counted_in_32_bits():
+    L, p, i64 = m.lib(), _p(BUF), ctypes.c_int64
+    assert L.lsp_token_scores(1, p, 1, 1, (1 << 30) + 1, i64(0), i64(0), None, None, 0, None, p, None, None, None, ctypes.c_size_t(0), None) == -1
+    assert b"2^30" in L.lsp_last_error()
+    one = (ctypes.c_void_p * 1)(p.value)
+    for size in (dict(C=(1 << 30) - 3), dict(S=(1 << 30) - 7), dict(S=1 << 28, Hq=32, Hkv=4), dict(C=2 ** 31 - 1, S=2 ** 31 - 1)):
+        d = m.AttnDesc(**{**dict(dtype=1, B=1, S=4, Hq=4, Hkv=4, D=128, C=8), **size})
+        assert L.lsp_attn_key_weights(ctypes.byref(d), 1, one, one, one, p, p, ctypes.c_float(1), p, p, ctypes.c_size_t(1 << 62), None) == -1, size
+        assert b"2^30" in L.lsp_last_error(), size
+
+
 def test_the_binding_refuses_wrong_tensors(monkeypatch):
     """Host tensors stand in for device tensors: a call that got past the checks would reach the library, which is not there."""
     monkeypatch.setattr(m, "_here", lambda *ts: None)
