@@ -37,9 +37,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // An entropy loses 2^-24 of x s in t + x s: 5e-7 at 8 octaves, 2e-6 at the confidence pass's 32, whose sum has no such term.
 constexpr float kLagOctaves = 8.0f;
-// Entries and maxima below this are kept out of products (-inf, and the lowest values, whose product with log2(e) is): a group of loads
-// that holds one, or a row of nothing else, takes a way of its own.
+// Entries below this are kept out of products (-inf, and the lowest values, whose product with log2(e) is): a group of loads that holds one
+// takes a way of its own.
 constexpr float kLow = -1e37f;
+// Maxima farther from 0 than 2^26: the reference is a rounded product, and the maximum's own exponent its rounding error, up to half a step of it. That is 4 octaves
+// here and 512 at 1e10, where 2^512 is infinite.
+constexpr float kFar = 67108864.f;
 constexpr int kMaxAlt = 32;
 constexpr int kRankStep = 16;   // entries that are read at a time
 constexpr int kMinCut = 16384;  // rows of at most this many entries are not cut
@@ -406,7 +409,7 @@ __device__ __forceinline__ Stat scan_segment(const T *row, int c0, int c1, int K
   }
 
   if (!ALT) all = statistics();
-  if (all.m < kLow && all.m > -INFINITY) {  // (uniform) a row of nothing but lowest values: differences first
+  if (fabsf(all.m) > kFar && all.m > -INFINITY) {  // (uniform) sums that may have overflowed, or be of nothing: differences first
     __syncthreads();
     Stat w = {all.m, 0.f, 0.f};
     for (int c = c0 + tid; c < c1; c += NT) {
