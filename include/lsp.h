@@ -455,12 +455,14 @@ int32_t lsp_attn_key_weights(const lsp_attn_desc *desc, int32_t num_layers, cons
 /* ------------------------------------------------------------------------- *
  * Eviction from a cache by accumulated attention weight.  Every sequence b with
  * P_b > high rows is cut back to `keep` rows, for each layer and KV head g by itself:
- *   rows t < first and t >= P_b - recent stay; of the others those of the largest
- *   weights[b,g,t] (equal weights: the lower row; NaN below everything), `keep` rows in all.
+ *   rows t < first and the last places, t >= P_b - recent, stay; of the others those of the
+ *   largest weights[b,g,t] (equal weights: the lower row; NaN below everything), `keep` rows in all.
  *   Rows below `keep` that stay do not move.  Rows from `keep` on that stay take, in
  *   ascending order, the places below `keep` that have become free, in ascending order.
  * The order of cached rows has no meaning to lsp_attn_step (keys carry their positions,
- * there is no mask); rows appended since the last eviction are behind all others.  Per row
+ * there is no mask); rows appended since the last eviction are behind all others, those that it
+ * moved are not: of a cache that is cut back again and again the last places hold the newest rows
+ * only where at least `recent` were appended in between, and lsp_kv_evict_positions goes by age.  Per row
  * j < min(P_b, keep) kept_index[b,g,j] = the row that is at j now, else -1;
  * new_weights[b,g,j] = its weight; new_len[b] = keep.  Sequences with
  * P_b <= high keep their rows, weights and length.  Rows and weights from new_len[b]
@@ -472,7 +474,7 @@ typedef struct {
   int32_t num_layers;
   int32_t keep;           /* 1..C */
   int32_t high;           /* >= keep: only sequences with more rows than this are cut */
-  int32_t first, recent;  /* rows that stay whatever their weight; first + recent <= keep */
+  int32_t first, recent;  /* rows that stay whatever their weight, at the beginning and at the end; first + recent <= keep */
   int64_t cache_batch_stride; /* elements between sequences; 0 = C*Hkv*D */
 } lsp_evict_desc;
 
@@ -493,6 +495,21 @@ int32_t lsp_kv_evict(const lsp_evict_desc *desc, const float *weights, const int
                      void *const *k_cache_layers, void *const *v_cache_layers, float *new_weights,
                      int32_t *new_len, int32_t *kept_index, void *workspace, size_t workspace_bytes,
                      void *stream);
+
+/*
+ * lsp_kv_evict with `recent` by age: in the place of the last places the rows of the newest `recent` tokens
+ * stay, wherever earlier evictions have put them.  positions: device int32 [num_layers, B, Hkv, C], updated in place: the position
+ * in its sequence of the token that a row is of, or INT32_MIN: the row is where it was appended, so that its position is
+ * token_len[b] - (P_b - t).  A buffer of INT32_MIN is what a cache in order of position begins with; a caller's own positions leave it behind the cached
+ * rows.  Appended rows then need nothing written: of a sequence that is cut, rows below `keep` have their positions afterwards and those from there to P_b INT32_MIN.
+ * token_len: device int32[B], the tokens of the sequence so far (with those that have left the cache); it must not overlap new_len.
+ * Rows t >= first with token_len[b] - position <= recent stay; where they are more than keep - first (which positions of one token each
+ * never are), the last `recent` places do.  Everything else, and the workspace, as for lsp_kv_evict.
+ */
+int32_t lsp_kv_evict_positions(const lsp_evict_desc *desc, const float *weights, int32_t *positions,
+                               const int32_t *token_len, const int32_t *prefix_len, void *const *k_cache_layers,
+                               void *const *v_cache_layers, float *new_weights, int32_t *new_len, int32_t *kept_index,
+                               void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- *
  * Measurement helper (used by the benchmark, not part of the scheduler step):

@@ -47,8 +47,12 @@ def key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay=1.0, s
     return w
 
 
-def evict(weights, prefix_len, keep, high=None, first=0, recent=0, caches=()):
-    """weights [L,B,H,C]; caches: tensors [L,B,C,H,D], rows moved in place.  -> (new weights, new lengths, kept index)."""
+BY_PLACE = -2 ** 31
+
+
+def evict(weights, prefix_len, keep, high=None, first=0, recent=0, caches=(), positions=None, token_len=None):
+    """weights [L,B,H,C]; caches: tensors [L,B,C,H,D], rows moved in place.  -> (new weights, new lengths, kept index).
+    positions [L,B,H,C], updated in place, with token_len [B]: `recent` goes by them, and not by the places."""
     L, B, H, C = weights.shape
     high = keep if high is None else high
     new, length = weights.clone(), prefix_len.clone()
@@ -61,11 +65,19 @@ def evict(weights, prefix_len, keep, high=None, first=0, recent=0, caches=()):
                 at = list(range(min(P, keep)))
                 if P > high:
                     w = weights[l, b, h].tolist()
-                    free = sorted(range(first, P - recent), key=lambda t: (math.isnan(w[t]), -w[t], t))
-                    stay = set(range(first)) | set(range(P - recent, P)) | set(free[:keep - first - recent])
+                    new_rows = set(range(P - recent, P))
+                    if positions is not None:
+                        T = int(token_len[b])
+                        where = [T - (P - t) if p == BY_PLACE else p for t, p in enumerate(positions[l, b, h, :P].tolist())]
+                        young = {t for t in range(first, P) if T - where[t] <= recent}
+                        new_rows = young if len(young) <= keep - first else new_rows
+                    free = sorted(set(range(first, P)) - new_rows, key=lambda t: (math.isnan(w[t]), -w[t], t))
+                    stay = set(range(first)) | new_rows | set(free[:keep - first - len(new_rows)])
                     come = sorted(t for t in stay if t >= keep)
                     for hole, t in zip([t for t in range(keep) if t not in stay], come):
                         at[hole] = t
+                    if positions is not None:
+                        positions[l, b, h, :P] = torch.tensor([where[t] for t in at] + [BY_PLACE] * (P - keep), dtype=torch.int32)
                     for j, t in enumerate(at):
                         if j != t:
                             new[l, b, h, j] = weights[l, b, h, t]

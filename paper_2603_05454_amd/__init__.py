@@ -65,13 +65,13 @@ EXPORTS = ["lsp_version", "lsp_last_error", "lsp_attn_workspace_bytes", "lsp_att
            "lsp_commit", "lsp_commit_step", "lsp_flip_update", "lsp_poll_lengths", "lsp_poll_progress", "lsp_select_scattered", "lsp_kv_gather_append",
            "lsp_attn_step_gather", "lsp_lm_head_confidence_workspace_bytes", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma",
            "lsp_token_scores_workspace_bytes", "lsp_token_scores", "lsp_attn_key_weights_workspace_bytes", "lsp_attn_key_weights",
-           "lsp_kv_evict_workspace_bytes", "lsp_kv_evict"]
+           "lsp_kv_evict_workspace_bytes", "lsp_kv_evict", "lsp_kv_evict_positions"]
 
 # entry points that the native module calls, in the order of its table
 NATIVE_ENTRIES = ("lsp_attn_workspace_bytes", "lsp_attn_step", "lsp_attn_step_layers", "lsp_confidence_workspace_bytes", "lsp_confidence",
                   "lsp_lm_head_confidence_workspace_bytes", "lsp_lm_head_confidence", "lsp_commit", "lsp_flip_update", "lsp_poll_lengths", "lsp_commit_step",
                   "lsp_poll_progress", "lsp_token_scores_workspace_bytes", "lsp_token_scores", "lsp_attn_key_weights_workspace_bytes",
-                  "lsp_attn_key_weights", "lsp_kv_evict_workspace_bytes", "lsp_kv_evict")
+                  "lsp_attn_key_weights", "lsp_kv_evict_workspace_bytes", "lsp_kv_evict", "lsp_kv_evict_positions")
 
 
 def lib() -> ctypes.CDLL:
@@ -89,7 +89,8 @@ def lib() -> ctypes.CDLL:
                   "lsp_attn_key_weights_workspace_bytes", "lsp_kv_evict_workspace_bytes"):
             getattr(L, n).restype = ctypes.c_size_t
         for n in ("lsp_attn_step", "lsp_attn_step_layers", "lsp_confidence", "lsp_confidence_static", "lsp_commit", "lsp_commit_step", "lsp_flip_update", "lsp_poll_lengths", "lsp_select_scattered",
-                  "lsp_kv_gather_append", "lsp_attn_step_gather", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma", "lsp_token_scores", "lsp_attn_key_weights", "lsp_kv_evict"):
+                  "lsp_kv_gather_append", "lsp_attn_step_gather", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma", "lsp_token_scores", "lsp_attn_key_weights", "lsp_kv_evict",
+                  "lsp_kv_evict_positions"):
             getattr(L, n).restype = ctypes.c_int32
         try:
             from . import _binding
@@ -816,12 +817,18 @@ def kv_evict_workspace_bytes(layers: LayerTable, keep, high=None, first=0, recen
     return lib().lsp_kv_evict_workspace_bytes(ctypes.byref(_evict_desc(layers, keep, high, first, recent)))
 
 
+BY_PLACE = -2 ** 31     # a position: the row is where it was appended
+
+
 def kv_evict(weights, prefix_len, layers: LayerTable, keep, high=None, first=0, recent=0, new_weights=None, new_len=None, kept_index=None,
-             workspace=None):
+             workspace=None, positions=None, token_len=None):
     """lsp_kv_evict: sequences of more than `high` (default: keep) cached rows are cut back to `keep`, per layer and KV head those of the
     largest weights [layers,B,Hkv,C] beside the first `first` and the last `recent` ones; rows move inside the caches of `layers`.
     new_weights, new_len: where weights and lengths after it go (default: in place).  kept_index int32 [layers,B,Hkv,keep], when given,
     receives the former row of each.  Returns new_len.
+    positions int32 [layers,B,Hkv,C] and token_len int32 [B] (lsp_kv_evict_positions): for caches that are cut back more than once, where the last
+    places are not the newest rows any more: `recent` goes by the tokens' positions, which are updated in place.  torch.full(..., BY_PLACE)
+    is what a cache in order of position begins with, and what lies behind the cached rows; appended rows need nothing written.  token_len: the tokens so far, in a buffer other than new_len.
     workspace: contiguous device memory of kv_evict_workspace_bytes(...) bytes and any content, aligned to 16 bytes, for this call alone
     until it has run; without one that will do, the call takes its own from torch's allocator."""
     if new_weights is None:
@@ -830,14 +837,19 @@ def kv_evict(weights, prefix_len, layers: LayerTable, keep, high=None, first=0, 
         new_len = prefix_len
     _table_here(layers.keep[2][0])
     if _nat is not None:
-        rc = _nat.kv_evict(weights, prefix_len, layers, (keep, keep if high is None else high, first, recent), new_weights, new_len, kept_index, workspace)
+        rc = _nat.kv_evict(weights, prefix_len, layers, (keep, keep if high is None else high, first, recent), new_weights, new_len, kept_index, workspace,
+                           *(() if positions is None and token_len is None else (positions, token_len)))
         if rc is not None:
             _check(rc, "lsp_kv_evict")
             return new_len
     if layers.cache_bs == 0 and layers.B > 1:
         raise LspError("caches must not be broadcast")
-    _here(weights, prefix_len, new_weights, new_len, kept_index)
+    _here(weights, prefix_len, new_weights, new_len, kept_index, positions, token_len)
     shape = (layers.n, layers.B, layers.Hkv, layers.C)
+    if (positions is None) != (token_len is None):
+        raise LspError("positions and token_len come together")
+    _need("positions", positions, torch.int32, shape, optional=True)
+    _need("token_len", token_len, torch.int32, (layers.B,), optional=True)
     _need("weights", weights, torch.float32, shape)
     _need("new_weights", new_weights, torch.float32, shape)
     _need("prefix_len", prefix_len, torch.int32, (layers.B,))
@@ -846,8 +858,12 @@ def kv_evict(weights, prefix_len, layers: LayerTable, keep, high=None, first=0, 
     _need("kept_index", kept_index, torch.int32, (*shape[:3], d.keep), optional=True)
     need = lib().lsp_kv_evict_workspace_bytes(ctypes.byref(d))
     workspace = _call_workspace(workspace, need, weights.device)
-    rc = lib().lsp_kv_evict(ctypes.byref(d), _ptr(weights), _ptr(prefix_len), layers.arrays[2], layers.arrays[3], _ptr(new_weights), _ptr(new_len),
-                            _ptr(kept_index), _ptr(workspace), ctypes.c_size_t(need), _stream())
+    rest = (_ptr(prefix_len), layers.arrays[2], layers.arrays[3], _ptr(new_weights), _ptr(new_len), _ptr(kept_index), _ptr(workspace), ctypes.c_size_t(need),
+            _stream())
+    if positions is None:
+        rc = lib().lsp_kv_evict(ctypes.byref(d), _ptr(weights), *rest)
+    else:
+        rc = lib().lsp_kv_evict_positions(ctypes.byref(d), _ptr(weights), _ptr(positions), _ptr(token_len), *rest)
     _check(rc, "lsp_kv_evict")
     return new_len
 

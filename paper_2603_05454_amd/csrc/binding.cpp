@@ -45,8 +45,9 @@ struct Entry {
   decltype(&lsp_attn_key_weights) attn_key_weights;
   decltype(&lsp_kv_evict_workspace_bytes) kv_evict_workspace_bytes;
   decltype(&lsp_kv_evict) kv_evict;
+  decltype(&lsp_kv_evict_positions) kv_evict_positions;
 } g;
-constexpr int kEntries = 18;
+constexpr int kEntries = 19;
 
 const at::Tensor *tensor(PyObject *o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
 const at::Tensor *device_tensor(PyObject *o) {
@@ -170,6 +171,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   g.attn_key_weights = reinterpret_cast<decltype(g.attn_key_weights)>(p[15]);
   g.kv_evict_workspace_bytes = reinterpret_cast<decltype(g.kv_evict_workspace_bytes)>(p[16]);
   g.kv_evict = reinterpret_cast<decltype(g.kv_evict)>(p[17]);
+  g.kv_evict_positions = reinterpret_cast<decltype(g.kv_evict_positions)>(p[18]);
   Py_RETURN_NONE;
 }
 
@@ -437,9 +439,10 @@ PyObject *commit(PyObject *, PyObject *const *a, Py_ssize_t n) {
                 data<int32_t>(flags), data<float>(tau), nullptr, 0, stream());
 }
 
-// (weights, prefix_len, layer table, (keep, high, first, recent), new_weights, new_len, kept_index or None, workspace or None)
+// (weights, prefix_len, layer table, (keep, high, first, recent), new_weights, new_len, kept_index or None, workspace or None[, positions, token_len])
 PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  ARGUMENTS(8);
+  const bool aged = n == 10;
+  ARGUMENTS((aged ? 10 : 8));
   long i[4], t[9];
   ORDINARY(PyTuple_Check(a[3]) && PyTuple_GET_SIZE(a[3]) == 4);
   for (int k = 0; k < 4; ++k) ORDINARY(integer(PyTuple_GET_ITEM(a[3], k), i[k]) && i[k] == int32_t(i[k]));
@@ -458,10 +461,14 @@ PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
                    *nw = dense(a[4], at::kFloat, {t[6], t[1], t[3], t[5]}), *nl = dense(a[5], at::kInt, {t[1]}),
                    *kept = a[6] == Py_None ? nullptr : dense(a[6], at::kInt, {t[6], t[1], t[3], i[0]});
   ORDINARY(w && pl && nw && nl && (kept || a[6] == Py_None));
+  const at::Tensor *at = aged ? dense(a[8], at::kInt, {t[6], t[1], t[3], t[5]}) : nullptr, *tl = aged ? dense(a[9], at::kInt, {t[1]}) : nullptr;
+  ORDINARY(!aged || (at && tl));
   const Workspace work(g.kv_evict_workspace_bytes(&d), local_tensor(a[7]));
-  const int32_t rc = unlocked(g.kv_evict, &d, data<float>(w), data<int32_t>(pl), static_cast<void *const *>(tab[2].view.buf),
-                              static_cast<void *const *>(tab[3].view.buf), data<float>(nw), data<int32_t>(nl), data<int32_t>(kept), work.at, work.bytes,
-                              stream());
+  auto *k = static_cast<void *const *>(tab[2].view.buf), *v = static_cast<void *const *>(tab[3].view.buf);
+  const int32_t rc = aged ? unlocked(g.kv_evict_positions, &d, data<float>(w), data<int32_t>(at), data<int32_t>(tl), data<int32_t>(pl), k, v, data<float>(nw),
+                                     data<int32_t>(nl), data<int32_t>(kept), work.at, work.bytes, stream())
+                          : unlocked(g.kv_evict, &d, data<float>(w), data<int32_t>(pl), k, v, data<float>(nw), data<int32_t>(nl), data<int32_t>(kept),
+                                     work.at, work.bytes, stream());
   ORDINARY(rc != LSP_ERR_WORKSPACE);
   return PyLong_FromLong(rc);
 }

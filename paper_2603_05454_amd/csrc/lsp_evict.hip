@@ -8,6 +8,10 @@
 // which accumulated weights share, is a queue for few counters in LDS.)
 // With ties at the end, the row up to which the equal ones stay is found in the same way.
 //
+// Which rows are the last: those at the end, as long as rows are only appended.  An eviction puts rows from the end among the others, so that a cache that is evicted from
+// again needs its rows' positions.  They are kept beside the weights, for rows from `keep` on as "by place" (kByPlace), since those in front of the end were appended in
+// order: a row at t is P - t rows old.  An append has nothing to write then, and an eviction writes the positions below `keep`.
+//
 // Where they go: keys carry their positions and the attention has no mask, so the order of cached rows means nothing.  Rows
 // below `keep` that stay do not move; each row from `keep` on that stays goes into the place of one below that leaves (the n-th of
 // one to the n-th of the other).  That moves at most P - keep rows, where closing the gaps in order moves every row behind the first
@@ -36,6 +40,7 @@ constexpr int kMaxParts = 16;                 // workgroups of a unit
 constexpr int64_t kPartBytes = 256 << 10;     // to be moved, a workgroup's at least
 constexpr int kEnough = 512;                  // workgroups
 constexpr int kMaxLayersPerLaunch = 32;
+constexpr int32_t kByPlace = INT32_MIN;
 struct CachePtrs {
   char *at[2 * kMaxLayersPerLaunch];  // K then V per layer
 };
@@ -44,7 +49,8 @@ struct EvictArgs {
   const float *weights;  // [layers, B, Hkv, C], the launch's first layer
   float *new_weights;
   int32_t *kept_index;  // [layers, B, Hkv, keep] or null
-  const int32_t *prefix_len;
+  int32_t *positions;   // as the weights, or null: then the last places are the last rows
+  const int32_t *token_len, *prefix_len;
   // per unit, where another kernel writes weights and index (`later`): P, moves (-1: nothing leaves), `room` destinations, `room` sources
   int32_t *moves;
   int32_t *new_len;  // where they are written by the first launch (not over the lengths that all of them read), or null
@@ -59,6 +65,14 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
   if ((u & 0x7fffffffu) > 0x7f800000u) return 1;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// How many tokens are at or behind a row's: 1 for the last one.  (Differences that wrap: numbers that make no sense may do any harm but undefined.)
+__device__ __forceinline__ int age_of(int32_t position, int32_t tokens, int rows, int t) {
+  return position == kByPlace ? rows - t : int32_t(uint32_t(tokens) - uint32_t(position));
+}
+__device__ __forceinline__ int32_t position_of(int32_t position, int32_t tokens, int rows, int t) {
+  return position == kByPlace ? int32_t(uint32_t(tokens) - uint32_t(rows - t)) : position;
 }
 
 // Over a wave on the DPP network: the maximum, in every lane, and the sum up to and with the lane.
@@ -111,8 +125,8 @@ struct Meeting {
   }
 };
 
-// ONE: a unit's rows are one block, whose weights are read once.
-template <bool ONE>
+// ONE: a unit's rows are one block, whose weights are read once.  AGED: the last rows go by positions.
+template <bool ONE, bool AGED>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 8 : 1))) void evict_kernel(EvictArgs a, CachePtrs p) {
   __shared__ __attribute__((aligned(16))) int s_meet[2 * kWaves];
   __shared__ int s_places[2][kKeys * kWaves], s_total[2], s_src[kWindow];
@@ -137,8 +151,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
       for (int t = tid; t < a.keep; t += kThreads) kept[t] = t < P ? t : -1;
     return;
   }
-  // rows [first, end) compete for `places` places; the others' key is 0
-  const int end = P - a.recent, places = a.keep - a.first - a.recent, blocks = ONE ? 1 : (P + kBlock - 1) / kBlock;
+  // rows [first, end) compete for `places` places, but those that are young (AGED); the others' key is 0
+  const int blocks = ONE ? 1 : (P + kBlock - 1) / kBlock;
+  int32_t *position = AGED ? a.positions + int64_t(unit) * a.C : nullptr;
+  const int32_t tokens = AGED ? a.token_len[b] : 0;
+  bool by_age = AGED;
+  int end = AGED ? P : P - a.recent, places = a.keep - a.first - (AGED ? 0 : a.recent), rivals = end - a.first;
   uint32_t key[kKeys];
   // (a thread's number that the compiler takes for a new one: it would keep sixteen rows' numbers, addresses and flags from loop to loop, in
   // registers that would leave one workgroup to a compute unit)
@@ -153,7 +171,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
     for (int r = 0; r < kKeys; ++r) {
       if (blk * kBlock + r * kThreads >= P) break;
       const int t = blk * kBlock + r * kThreads + own;
-      key[r] = t >= a.first && t < end ? order_of(w[t]) : 0;
+      key[r] = t >= a.first && t < end && (!AGED || !by_age || age_of(position[t], tokens, P, t) > a.recent) ? order_of(w[t]) : 0;
     }
   };
   if (ONE) load(0);
@@ -171,6 +189,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
     }
     return meet.sum(n);
   };
+  if (AGED) {
+    rivals = count([&](uint32_t k, int) { return k != 0; });
+    places -= P - a.first - rivals;
+    if (places < 0) {  // more rows than there is room for claim to be the last (positions that make no sense): those at the end are
+      by_age = false;
+      end = P - a.recent;
+      places = a.keep - a.first - a.recent;
+      rivals = end - a.first;
+      if (ONE) load(0);
+    }
+  }
   uint32_t least = 0xffffffffu;  // what stays is above, or equal and up to row `upto`
   int upto = -1;
   if (places > 0) {
@@ -186,7 +215,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
     }
     // at least `places` are at or above lo, fewer at or above hi
     uint32_t lo = ~meet.most(wave_max(low)), hi = meet.most(wave_max(top)) + 1;
-    int from_lo = end - a.first, above = 0;  // how many
+    int from_lo = rivals, above = 0;  // how many
     while (hi - lo > 1 && from_lo != places && from_lo - above > kFew) {
       const uint32_t mid = lo + (hi - lo) / 2;
       const int n = count([&](uint32_t k, int) { return k >= mid; });
@@ -289,6 +318,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
         if (!a.later && window == 0 && t < a.keep && !is_hole) {
           if (nw != w) nw[t] = w[t];
           if (kept != nullptr) kept[t] = t;
+          if (AGED && position[t] == kByPlace) position[t] = position_of(kByPlace, tokens, P, t);
         }
       }
       nh += s_total[0];
@@ -308,6 +338,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
       for (int n = tid; n < here; n += kThreads) {
         nw[s_dst[n]] = w[s_src[n]];
         if (kept != nullptr) kept[s_dst[n]] = s_src[n];
+        if (AGED) position[s_dst[n]] = position_of(position[s_src[n]], tokens, P, s_src[n]);
       }
     // the rows, K and V, 16 bytes a thread, four loads under way
     char *k_base = p.at[2 * l] + int64_t(b) * a.cache_batch_bytes + int64_t(g) * a.row_bytes;
@@ -330,9 +361,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 
     }
     __syncthreads();
   }
+  if (AGED && !a.later)  // (all that was there has been read)
+    for (int t = a.keep + tid; t < P; t += kThreads) position[t] = kByPlace;
 }
 
-// Weights and index of a unit whose workgroups, or whose blocks of rows, were several: they are read by all until the end.
+// Weights, index and positions of a unit whose workgroups, or whose blocks of rows, were several: they are read by all until the end.
 constexpr int kLaterThreads = 256;
 __global__ __launch_bounds__(kLaterThreads) void evict_weights_kernel(EvictArgs a, int32_t *new_len) {
   const int tid = threadIdx.x, unit = blockIdx.x, b = unit / a.Hkv % a.B;
@@ -350,6 +383,19 @@ __global__ __launch_bounds__(kLaterThreads) void evict_weights_kernel(EvictArgs 
     const int dst = list[2 + n], src = list[2 + a.room + n];
     nw[dst] = w[src];
     if (kept != nullptr) kept[dst] = src;
+  }
+  if (a.positions != nullptr && moves >= 0) {
+    int32_t *position = a.positions + int64_t(unit) * a.C;
+    const int32_t tokens = a.token_len[b];
+    for (int n = tid; n < moves; n += kLaterThreads) {
+      const int dst = list[2 + n], src = list[2 + a.room + n];
+      position[dst] = position_of(position[src], tokens, P, src);
+    }
+    __syncthreads();
+    for (int t = tid; t < P; t += kLaterThreads) {
+      if (t >= a.keep) position[t] = kByPlace;
+      else if (position[t] == kByPlace) position[t] = position_of(kByPlace, tokens, P, t);
+    }
   }
   if (new_len != nullptr && unit == b * a.Hkv && tid == 0) new_len[b] = rows;
 }
@@ -400,10 +446,11 @@ extern "C" size_t lsp_kv_evict_workspace_bytes(const lsp_evict_desc *d) {
   return most;
 }
 
-extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, const int32_t *prefix_len, void *const *k_cache_layers,
-                                void *const *v_cache_layers, float *new_weights, int32_t *new_len, int32_t *kept_index, void *workspace,
-                                size_t workspace_bytes, void *stream) {
-  using namespace lsp;
+namespace lsp {
+namespace {
+int32_t evict(const lsp_evict_desc *d, const float *weights, int32_t *positions, const int32_t *token_len, const int32_t *prefix_len,
+              void *const *k_cache_layers, void *const *v_cache_layers, float *new_weights, int32_t *new_len, int32_t *kept_index, void *workspace,
+              size_t workspace_bytes, void *stream) {
   const int32_t rc = check(d);
   if (rc != LSP_OK) return rc;
   LSP_CHECK_ARG(weights && prefix_len && k_cache_layers && v_cache_layers && new_weights && new_len, "lsp_kv_evict: null pointer");
@@ -421,7 +468,7 @@ extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, c
     return LSP_ERR_WORKSPACE;
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
-  EvictArgs a = {weights, new_weights, kept_index, prefix_len, static_cast<int32_t *>(workspace), new_len == prefix_len ? nullptr : new_len, d->B, d->Hkv, d->C, d->keep, d->high, d->first, d->recent, room_of(d)};
+  EvictArgs a = {weights, new_weights, kept_index, positions, token_len, prefix_len, static_cast<int32_t *>(workspace), new_len == prefix_len ? nullptr : new_len, d->B, d->Hkv, d->C, d->keep, d->high, d->first, d->recent, room_of(d)};
   a.row_bytes = int32_t(row_bytes);
   a.by_pieces = div_by(row_bytes / 8);
   a.cache_row_bytes = cache_row_bytes;
@@ -433,6 +480,7 @@ extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, c
     a.weights = weights + units * d->C;
     a.new_weights = new_weights + units * d->C;
     a.kept_index = kept_index == nullptr ? nullptr : kept_index + units * d->keep;
+    a.positions = positions == nullptr ? nullptr : positions + units * d->C;
     a.parts = parts_of(d, nl);
     a.later = weights_later(d, nl);
     CachePtrs p;
@@ -442,8 +490,9 @@ extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, c
       p.at[2 * l + 1] = static_cast<char *>(v_cache_layers[s]);
     }
     const dim3 grid(d->Hkv, d->B, nl * a.parts);
-    if (d->C <= kBlock) evict_kernel<true><<<grid, kThreads, 0, st>>>(a, p);
-    else evict_kernel<false><<<grid, kThreads, 0, st>>>(a, p);
+    const auto kernel = d->C <= kBlock ? (positions ? evict_kernel<true, true> : evict_kernel<true, false>)
+                                       : (positions ? evict_kernel<false, true> : evict_kernel<false, false>);
+    kernel<<<grid, kThreads, 0, st>>>(a, p);
     LSP_CHECK_LAUNCH("lsp_kv_evict: launch");
     a.new_len = nullptr;
     if (a.later) {
@@ -458,4 +507,24 @@ extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, c
     LSP_CHECK_LAUNCH("lsp_kv_evict: length launch");
   }
   return LSP_OK;
+}
+}  // namespace
+}  // namespace lsp
+
+extern "C" int32_t lsp_kv_evict(const lsp_evict_desc *d, const float *weights, const int32_t *prefix_len, void *const *k_cache_layers,
+                                void *const *v_cache_layers, float *new_weights, int32_t *new_len, int32_t *kept_index, void *workspace,
+                                size_t workspace_bytes, void *stream) {
+  return lsp::evict(d, weights, nullptr, nullptr, prefix_len, k_cache_layers, v_cache_layers, new_weights, new_len, kept_index, workspace, workspace_bytes,
+                    stream);
+}
+
+extern "C" int32_t lsp_kv_evict_positions(const lsp_evict_desc *d, const float *weights, int32_t *positions, const int32_t *token_len,
+                                          const int32_t *prefix_len, void *const *k_cache_layers, void *const *v_cache_layers, float *new_weights,
+                                          int32_t *new_len, int32_t *kept_index, void *workspace, size_t workspace_bytes, void *stream) {
+  using namespace lsp;
+  LSP_CHECK_ARG(positions && token_len, "lsp_kv_evict_positions: null pointer");
+  const auto tokens = reinterpret_cast<uintptr_t>(token_len), lengths = reinterpret_cast<uintptr_t>(new_len), bytes = uintptr_t(d ? d->B : 0) * sizeof(int32_t);
+  LSP_CHECK_ARG(tokens + bytes <= lengths || lengths + bytes <= tokens, "lsp_kv_evict_positions: token_len must not be new_len");
+  return evict(d, weights, positions, token_len, prefix_len, k_cache_layers, v_cache_layers, new_weights, new_len, kept_index, workspace, workspace_bytes,
+               stream);
 }

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import torch
 
-from . import (AttnLayerTable, LayerTable, LspError, ProgressPoll, _commit_out, _need, attn_key_weights_layers, attn_key_weights_workspace_bytes,
+from . import (BY_PLACE, AttnLayerTable, LayerTable, LspError, ProgressPoll, _commit_out, _need, attn_key_weights_layers, attn_key_weights_workspace_bytes,
                attn_step_layers, commit_step, confidence, confidence_workspace_bytes, kv_evict, kv_evict_workspace_bytes, kv_gather_append,
                lm_head_confidence, lm_head_confidence_workspace_bytes, token_scores, token_scores_workspace_bytes)
 
@@ -59,9 +59,9 @@ class _Scores:
 class _Budget:
     """Caches that are cut back by accumulated attention weight.  Their rows are no longer the sequence's positions: cache_len counts them."""
 
-    def __init__(self, keep, high=None, first=0, recent=0, decay=1.0, cache_len=None, weights=None):
+    def __init__(self, keep, high=None, first=0, recent=0, decay=1.0, cache_len=None, weights=None, positions=None):
         self.kw = dict(keep=int(keep), high=int(keep if high is None else high), first=int(first), recent=int(recent))
-        self.decay, self.cache_len, self.weights, self.ready = float(decay), cache_len, weights, False
+        self.decay, self.cache_len, self.weights, self.positions, self.ready = float(decay), cache_len, weights, positions, False
 
     def start(self, table, prefix_len, suffix_len):
         if self.cache_len is None:
@@ -76,6 +76,9 @@ class _Budget:
         if self.cache_len.data_ptr() in (prefix_len.data_ptr(), suffix_len.data_ptr()):
             raise LspError("decode_loop: cache_len is a buffer of its own")
         _need("weights", self.weights, torch.float32, shape)
+        if self.positions is None and k["recent"] > 0:
+            self.positions = torch.full(shape, BY_PLACE, dtype=torch.int32, device=prefix_len.device)
+        _need("positions", self.positions, torch.int32, shape, optional=True)
         left, rows = torch.stack([suffix_len.max(), (suffix_len + self.cache_len).max()]).tolist()
         if max(rows, left + self.kw["high"]) > table.C:
             raise LspError(f"decode_loop: a cache of {table.C} rows has no room for {left} more positions on {self.kw['high']} rows (high), or on those there are")
@@ -87,7 +90,7 @@ class _Budget:
                                          device=suffix_len.device)
         attn_key_weights_layers(attn, self.cache_len, suffix_len, self.weights, decay=self.decay, workspace=self.workspace)
 
-    def append(self, table, commit_len):
+    def append(self, table, commit_len, prefix_len):
         if not self.ready:
             dev = commit_len.device
             self.rows = torch.arange(table.S, dtype=torch.int32, device=dev).expand(table.B, table.S).contiguous()
@@ -95,7 +98,8 @@ class _Budget:
             self.evict_workspace = torch.empty(max(16, kv_evict_workspace_bytes(table, **self.kw)), dtype=torch.uint8, device=dev)
             self.ready = True
         kv_gather_append(self.rows, commit_len, self.cache_len, table, appended=self.appended)
-        kv_evict(self.weights, self.cache_len, table, workspace=self.evict_workspace, **self.kw)
+        kv_evict(self.weights, self.cache_len, table, workspace=self.evict_workspace, positions=self.positions,
+                 token_len=None if self.positions is None else prefix_len, **self.kw)
 
 
 def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
@@ -132,13 +136,14 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
     scores: dict of buffers that take, for every committed token at its place in `tokens`, what the logits it was chosen from
     say about it (lsp_token_scores): "logprob", "entropy" (fp32 [B,T]), "alt_id", "alt_logprob" (int32 and fp32 [B,T,K], K up
     to 32); any of them.  Needs the logits, so not together with lm_head_weight.
-    cache_budget: dict(keep[, high, first, recent, decay, cache_len, weights]): caches of bounded length (run_attention and
+    cache_budget: dict(keep[, high, first, recent, decay, cache_len, weights, positions]): caches of bounded length (run_attention and
     kv_layers needed).  After every step, sequences with more than `high` (default: keep) cached rows are cut back to the `keep`
-    that received most attention, per layer and KV head, beside the first `first` and the last `recent` (lsp_attn_key_weights,
-    lsp_kv_evict); decay: what is left of a weight at the next step (default 1).  The caches' lengths are then cache_len (int32 [B],
+    that received most attention, per layer and KV head, beside the first `first` rows and those of the newest `recent` tokens (lsp_attn_key_weights,
+    lsp_kv_evict_positions); decay: what is left of a weight at the next step (default 1).  The caches' lengths are then cache_len (int32 [B],
     updated in place; default: a copy of prefix_len), and prefix_len counts tokens alone; weights fp32 [layers,B,Hkv,C] are those that
-    the prompt's rows begin with (default 0).  A cache has to have room for `high` rows and all that is to be generated.  state
-    carries both on (those of cache_budget are not looked at then).
+    the prompt's rows begin with (default 0), positions int32 of that shape the cached rows' tokens, which `recent` goes by (default: BY_PLACE, the
+    cached rows are in order and end with the newest token, which is also what is to be behind the cached rows).  A cache has to have room for `high` rows and all that is to be generated.  state
+    carries these on (those of cache_budget are not looked at then).
     A sequence that still has active positions but commits nothing (min_commit = 0, or its
     cache / token buffer is full) would never finish: the loop raises LspError instead.
     Returns dict(steps, flips, flip_denominator, window_flips, window_denominator, committed,
@@ -174,8 +179,10 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
     if cache_budget is not None:
         if not run_attention or kv_layers is None:
             raise LspError("decode_loop: a cache budget goes by the attention of kv_layers (run_attention)")
-        kept = {} if state is None else {k: state[k] for k in ("cache_len", "weights") if k in state}
+        kept = {} if state is None or "cache_len" not in state else {k: state.get(k) for k in ("cache_len", "weights", "positions")}
         budget = _Budget(**{**cache_budget, **kept})
+        if kept and budget.positions is None and budget.kw["recent"] > 0:
+            raise LspError("decode_loop: this state's caches were cut back without positions (recent = 0): nothing says which of their rows are recent")
     elif kv_layers is not None and state is not None and "cache_len" in state:
         raise LspError("decode_loop: this state's caches were cut back (cache_len): it goes on with a cache_budget")
     # Lengths of another type or place are no error with nothing to do.
@@ -226,7 +233,7 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
         if said is not None:
             said.keep(prefix_len, out["commit_len"])
         if budget is not None:
-            budget.append(table, out["commit_len"])
+            budget.append(table, out["commit_len"], prefix_len)
 
     while True:
         if (steps - first) % poll == 0:
@@ -280,6 +287,8 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
     if budget is not None:
         res["cache_len"] = budget.cache_len
         res["state"].update(cache_len=budget.cache_len, weights=budget.weights)
+        if budget.positions is not None:
+            res["state"]["positions"] = budget.positions
     if flip_trace:
         res["flip_trace"] = torch.stack(trace).cpu() if trace else torch.zeros((0, B, 2), dtype=torch.int32)
     if timed:
