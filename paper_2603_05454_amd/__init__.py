@@ -176,6 +176,8 @@ def version() -> str:
 def _strides3(t):
     if t.dim() != 4 or t.stride(3) != 1:
         raise LspError("attention operands are [batch, row, head, D] with a contiguous innermost dimension")
+    if t.stride(2) == 0:        # (three strides of 0 stand for a dense tensor)
+        raise LspError("attention operands must not be broadcast over heads")
     return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
@@ -786,8 +788,6 @@ def attn_key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay=1
     for name, t, shape in (("k_suf", k_suf, (B, S, Hkv, D)), ("k_cache", k_cache, (B, C, Hkv, D))):
         if t.dtype != q.dtype or tuple(t.shape) != shape:
             raise LspError(f"{name} must be {q.dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-    if 0 in (q.stride(2), k_suf.stride(2), k_cache.stride(2)):      # (strides of 0 stand for a dense tensor)
-        raise LspError("attention operands must not be broadcast over heads")
     d = AttnDesc(dtype=_dtype(q), B=B, S=S, Hq=Hq, Hkv=Hkv, D=D, C=C)
     d.q_stride, d.kv_suf_stride, d.cache_stride = _strides3(q), _strides3(k_suf), _strides3(k_cache)
     one = ctypes.c_void_p * 1

@@ -78,7 +78,7 @@ bool shape4(const at::Tensor &t, int64_t a, int64_t b, int64_t c, int64_t d) {
   return t.dim() == 4 && t.size(0) == a && t.size(1) == b && t.size(2) == c && t.size(3) == d;
 }
 bool strides3(const at::Tensor &t, int64_t (&s)[3]) {
-  if (t.stride(3) != 1) return false;
+  if (t.stride(3) != 1 || t.stride(2) == 0) return false;  // (three strides of 0 stand for a dense tensor)
   for (int k = 0; k < 3; ++k) s[k] = t.stride(k);
   return true;
 }
@@ -325,7 +325,6 @@ PyObject *attn_key_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {
   ORDINARY(ks->scalar_type() == q->scalar_type() && kc->scalar_type() == q->scalar_type() && shape4(*ks, B, S, Hkv, D) && shape4(*kc, B, C, Hkv, D));
   lsp_attn_desc d = {};
   ORDINARY(element_type(*q, d.dtype) && strides3(*q, d.q_stride) && strides3(*ks, d.kv_suf_stride) && strides3(*kc, d.cache_stride));
-  ORDINARY(d.q_stride[2] > 0 && d.kv_suf_stride[2] > 0 && d.cache_stride[2] > 0);  // (strides of 0 stand for a dense tensor)
   d.B = int32_t(B); d.S = int32_t(S); d.Hq = int32_t(Hq); d.Hkv = int32_t(Hkv); d.D = int32_t(D); d.C = int32_t(C);
   const void *at[3] = {q->const_data_ptr(), ks->const_data_ptr(), kc->const_data_ptr()};
   return key_weights(d, 1, &at[0], &at[1], &at[2], dense(a[3], at::kInt, {B}), dense(a[4], at::kInt, {B}), dense(a[5], at::kFloat, {B, Hkv, C}), a[6],

@@ -1,0 +1,55 @@
+"""Strides of 0 stand for a dense tensor in the C calls, so a tensor that is broadcast in the dimensions they are of would be read, or written, past its end:
+the binding refuses it (no GPU needed: nothing is launched)."""
+import pytest
+import torch
+
+import paper_2603_05454_amd as m
+
+
+@pytest.fixture
+def host(monkeypatch):
+    """Host tensors stand in for device tensors: a call that got past the checks would reach the library, which is not there."""
+    monkeypatch.setattr(m, "_here", lambda *ts: None)
+    monkeypatch.setattr(m, "_dev", lambda *ts: None)
+    monkeypatch.setattr(m, "lib", lambda: pytest.fail("the call reached the library"))
+    monkeypatch.setattr(m, "_attn_workspace", lambda d, given: (None, 0))
+    for name in ("_nat", "_nat_addresses", "_nat_attn_table", "_nat_layer_table"):
+        monkeypatch.setattr(m, name, None)
+
+
+def _row(n, heads, dim=64):
+    """[2, n, heads, dim] of one row of one head."""
+    return torch.zeros(dim).expand(2, n, heads, dim)
+
+
+@pytest.mark.parametrize("which", ["q", "suffix", "cache", "out"])
+def test_attention_operands(host, which):
+    q, k, c = torch.zeros(2, 4, 4, 64), torch.zeros(2, 4, 2, 64), torch.zeros(2, 16, 2, 64)
+    out, i = q.clone(), torch.zeros(2, dtype=torch.int32)
+    if which == "q":
+        q = _row(4, 4)
+    elif which == "suffix":
+        k = _row(4, 2)
+    elif which == "cache":
+        c = _row(16, 2)
+    else:
+        out = _row(4, 4)
+    for call in (lambda: m.AttnLayerTable([q], [k], [k], [c], [c], [out]), lambda: m.attn_step(q, k, k, c, c, i, i, out=out),
+                 lambda: m.attn_step(q, k, k, c, c, i, i, out=out, cache_row_index=torch.zeros((2, 16), dtype=torch.int32))):
+        with pytest.raises(m.LspError, match="broadcast"):
+            call()
+
+
+@pytest.mark.gpu
+def test_the_native_path_refuses_them_too():
+    q, k, c = torch.zeros(2, 4, 4, 64).cuda(), torch.zeros(2, 4, 2, 64).cuda(), torch.zeros(2, 16, 2, 64).cuda()
+    i = torch.zeros(2, dtype=torch.int32).cuda()
+    m.lib()
+    assert m._nat is not None
+    for bad in (dict(q=q.new_zeros(64).expand(2, 4, 4, 64)), dict(k=k.new_zeros(64).expand(2, 4, 2, 64)),
+                dict(c=c.new_zeros(64).expand(2, 16, 2, 64)), dict(out=q.new_zeros(64).expand(2, 4, 4, 64))):
+        a = {**dict(q=q, k=k, c=c, out=q.clone()), **bad}
+        with pytest.raises(m.LspError, match="broadcast"):
+            m.AttnLayerTable([a["q"]], [a["k"]], [a["k"]], [a["c"]], [a["c"]], [a["out"]])
+        with pytest.raises(m.LspError, match="broadcast"):
+            m.attn_step(a["q"], a["k"], a["k"], a["c"], a["c"], i, i, out=a["out"])
