@@ -440,6 +440,8 @@ class LayerTable:
                 if not (t.is_contiguous() or (t.stride(3) == 1 and t.stride(2) == t.shape[3]
                                               and t.stride(1) == t.shape[2] * t.shape[3])):
                     raise LspError("LayerTable: the rows of a sequence must be dense (only the batch stride is free)")
+                if t.stride(0) == 0 and t.shape[0] > 1:     # (a stride of 0 stands for dense sequences)
+                    raise LspError("LayerTable: suffix buffers and caches must not be broadcast over sequences")
         if k_cache[0].shape[0] != k_suf[0].shape[0] or k_cache[0].shape[2:] != k_suf[0].shape[2:]:
             raise LspError("LayerTable: caches and suffix buffers disagree on batch, heads or head size")
         Arr = ctypes.c_void_p * n
@@ -842,8 +844,6 @@ def kv_evict(weights, prefix_len, layers: LayerTable, keep, high=None, first=0, 
         if rc is not None:
             _check(rc, "lsp_kv_evict")
             return new_len
-    if layers.cache_bs == 0 and layers.B > 1:
-        raise LspError("caches must not be broadcast")
     _here(weights, prefix_len, new_weights, new_len, kept_index, positions, token_len)
     shape = (layers.n, layers.B, layers.Hkv, layers.C)
     if (positions is None) != (token_len is None):

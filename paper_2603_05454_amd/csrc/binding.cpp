@@ -451,7 +451,7 @@ PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
   }
   Memory tab[4];
   Object arrays(PyObject_GetAttr(a[2], k_arrays));
-  ORDINARY(t[6] > 0 && (t[8] > 0 || t[1] == 1) && tables(arrays.o, tab, t[6]));
+  ORDINARY(t[6] > 0 && tables(arrays.o, tab, t[6]));
   lsp_evict_desc d = {};
   d.kv_dtype = int32_t(t[0]); d.B = int32_t(t[1]); d.Hkv = int32_t(t[3]); d.D = int32_t(t[4]); d.C = int32_t(t[5]); d.num_layers = int32_t(t[6]);
   d.cache_batch_stride = t[8];
@@ -643,7 +643,8 @@ PyObject *layer_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
   int32_t type;
   ORDINARY(element_type(*l.first[0], type));
   for (const at::Tensor *t : l.first)
-    ORDINARY(t->dim() == 4 && t->stride(3) == 1 && t->stride(2) == t->size(3) && t->stride(1) == t->size(2) * t->size(3));
+    ORDINARY(t->dim() == 4 && t->stride(3) == 1 && t->stride(2) == t->size(3) && t->stride(1) == t->size(2) * t->size(3) &&
+             (t->stride(0) != 0 || t->size(0) == 1));
   const at::Tensor &ks = *l.first[0], &vs = *l.first[1], &kc = *l.first[2], &vc = *l.first[3];
   ORDINARY(vs.sizes() == ks.sizes() && vc.sizes() == kc.sizes() && same_strides(ks, vs) && same_strides(kc, vc) && kc.size(0) == ks.size(0) &&
            kc.size(2) == ks.size(2) && kc.size(3) == ks.size(3));

@@ -53,3 +53,27 @@ def test_the_native_path_refuses_them_too():
             m.AttnLayerTable([a["q"]], [a["k"]], [a["k"]], [a["c"]], [a["c"]], [a["out"]])
         with pytest.raises(m.LspError, match="broadcast"):
             m.attn_step(a["q"], a["k"], a["k"], a["c"], a["c"], i, i, out=a["out"])
+
+
+@pytest.mark.parametrize("which", ["suffix", "cache"])
+def test_rows_that_are_committed(host, which):
+    """Caches and suffix buffers of a layer table, which commits, appends and evictions go by."""
+    k, c = torch.zeros(2, 4, 2, 64), torch.zeros(2, 16, 2, 64)
+    if which == "suffix":
+        k = k[:1].expand(2, 4, 2, 64)
+    else:
+        c = c[:1].expand(2, 16, 2, 64)
+    with pytest.raises(m.LspError, match="broadcast"):
+        m.LayerTable([k], [k], [c], [c])
+    one = m.LayerTable([k[:1]], [k[:1]], [c[:1]], [c[:1]])      # (one sequence's stride is of no use)
+    assert one.B == 1 and one.C == 16
+
+
+@pytest.mark.gpu
+def test_the_native_table_refuses_them_too():
+    k, c = torch.zeros(2, 4, 2, 64).cuda(), torch.zeros(2, 16, 2, 64).cuda()
+    m.lib()
+    assert m._nat_layer_table is not None
+    for a in ([k[:1].expand(2, 4, 2, 64), c], [k, c[:1].expand(2, 16, 2, 64)]):
+        with pytest.raises(m.LspError, match="broadcast"):
+            m.LayerTable([a[0]], [a[0]], [a[1]], [a[1]])
