@@ -442,6 +442,9 @@ class LayerTable:
                     raise LspError("LayerTable: the rows of a sequence must be dense (only the batch stride is free)")
                 if t.stride(0) == 0 and t.shape[0] > 1:     # (a stride of 0 stands for dense sequences)
                     raise LspError("LayerTable: suffix buffers and caches must not be broadcast over sequences")
+        for k, v in ((k_suf[0], v_suf[0]), (k_cache[0], v_cache[0])):
+            if k.shape != v.shape or (k.shape[0] > 1 and k.stride(0) != v.stride(0)):
+                raise LspError("LayerTable: K and V must share shapes and batch strides")
         if k_cache[0].shape[0] != k_suf[0].shape[0] or k_cache[0].shape[2:] != k_suf[0].shape[2:]:
             raise LspError("LayerTable: caches and suffix buffers disagree on batch, heads or head size")
         Arr = ctypes.c_void_p * n

@@ -77,3 +77,14 @@ def test_the_native_table_refuses_them_too():
     for a in ([k[:1].expand(2, 4, 2, 64), c], [k, c[:1].expand(2, 16, 2, 64)]):
         with pytest.raises(m.LspError, match="broadcast"):
             m.LayerTable([a[0]], [a[0]], [a[1]], [a[1]])
+
+
+def test_keys_and_values_of_a_table_are_laid_out_alike(host):
+    """One batch stride is handed over for both."""
+    k, c = torch.zeros(2, 4, 2, 64), torch.zeros(2, 16, 2, 64)
+    wide = torch.zeros(2, 20, 2, 64)
+    for a in ((k, wide[:, :4], c, c), (wide[:, :4], k, c, c), (k, k, c, wide[:, :16]), (k, k, wide[:, :16], c), (k, k[:, :3], c, c), (k, k, c[:, :9], c)):
+        with pytest.raises(m.LspError, match="share"):
+            m.LayerTable(*[[t] for t in a])
+    m.LayerTable([k], [k], [wide[:, :16]], [wide[:, 4:]])
+    m.LayerTable([k[:1]], [wide[:1, :4]], [c[:1]], [wide[:1, :16]])      # (one sequence's stride is of no use)
