@@ -161,6 +161,12 @@ def _need_kv(q, k_suf, v_suf, k_cache, v_cache, out):
         raise LspError("K and V must share strides")
 
 
+def _not_broadcast(name, t, dims):
+    """Strides of 0 stand for dense ones."""
+    if any(t.stride(k) == 0 and t.shape[k] > 1 for k in range(dims)):
+        raise LspError(f"{name} must not be broadcast")
+
+
 def _need_conf_out(out, B, S):
     if len(out) != 3:
         raise LspError("out must be (top1_id, top1_prob, margin)")
@@ -339,6 +345,7 @@ def confidence(logits, suffix_len=None, out=None, workspace=None):
     B, S, V = logits.shape
     if logits.stride(2) != 1:
         raise LspError("logits rows must be contiguous")
+    _not_broadcast("logits", logits, 2)
     if out is None:
         out = _conf_out(logits)
     _dev(*out)
@@ -370,6 +377,7 @@ def confidence_static(logits, suffix_len, out):
     B, S, V = logits.shape
     if logits.stride(2) != 1:
         raise LspError("logits rows must be contiguous")
+    _not_broadcast("logits", logits, 2)
     _need_conf_out(out, B, S)
     _need("suffix_len", suffix_len, torch.int32, (B,), optional=True)
     rc = lib().lsp_confidence_static(_dtype(logits), _ptr(logits), B, S, V,
@@ -399,6 +407,8 @@ def lm_head_confidence(hidden, weight, suffix_len=None, out=None, workspace=None
         raise LspError(f"weight must be {hidden.dtype} [V, {K}], got {weight.dtype} {tuple(weight.shape)}")
     if hidden.stride(2) != 1 or weight.stride(1) != 1:
         raise LspError("hidden and weight rows must be contiguous")
+    _not_broadcast("hidden", hidden, 2)
+    _not_broadcast("weight", weight, 1)
     if out is None:
         out = _conf_out(hidden)
     _dev(*out)
@@ -722,10 +732,9 @@ def token_scores(logits, token_id=None, suffix_len=None, num_alt=0, out=None, wo
     if logits.dim() != 3 or logits.stride(2) != 1:
         raise LspError("logits are [batch, row, vocabulary] with contiguous rows")
     B, S, V = logits.shape
+    _not_broadcast("logits", logits, 2)
     row = V if S == 1 else logits.stride(1)
     batch = S * row if B == 1 else logits.stride(0)
-    if row == 0 or batch == 0:      # (which would stand for dense rows)
-        raise LspError("logits must not be broadcast")
     K = int(num_alt)
     if not 0 <= K <= 32:
         raise LspError(f"num_alt must be 0..32, got {K}")

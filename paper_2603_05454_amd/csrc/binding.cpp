@@ -84,6 +84,13 @@ bool strides3(const at::Tensor &t, int64_t (&s)[3]) {
 }
 bool same_strides(const at::Tensor &a, const at::Tensor &b) { return a.strides() == b.strides(); }
 
+// strides of 0, which stand for dense ones, in the first `dims` dimensions
+bool broadcast(const at::Tensor &t, int dims) {
+  for (int k = 0; k < dims; ++k)
+    if (t.stride(k) == 0 && t.size(k) > 1) return true;
+  return false;
+}
+
 // false for what is not a number by itself (the general path may still make one of it)
 bool number(PyObject *o, float &x) {
   x = float(PyFloat_AsDouble(o));
@@ -233,7 +240,7 @@ PyObject *confidence(PyObject *, PyObject *const *a, Py_ssize_t n) {
   ARGUMENTS(4);
   const at::Tensor *z = device_tensor(a[0]);
   int32_t type;
-  ORDINARY(z && z->dim() == 3 && z->stride(2) == 1 && element_type(*z, type));
+  ORDINARY(z && z->dim() == 3 && z->stride(2) == 1 && !broadcast(*z, 2) && element_type(*z, type));
   const int64_t B = z->size(0), S = z->size(1), V = z->size(2);
   const at::Tensor *sl = a[1] == Py_None ? nullptr : plain(a[1], at::kInt, B);
   ORDINARY(sl || a[1] == Py_None);
@@ -254,7 +261,7 @@ PyObject *lm_head_confidence(PyObject *, PyObject *const *a, Py_ssize_t n) {
   ARGUMENTS(5);
   const at::Tensor *h = device_tensor(a[0]), *w = device_tensor(a[1]);
   int32_t type;
-  ORDINARY(h && w && h->dim() == 3 && w->dim() == 2 && h->stride(2) == 1 && w->stride(1) == 1 && element_type(*h, type));
+  ORDINARY(h && w && h->dim() == 3 && w->dim() == 2 && h->stride(2) == 1 && w->stride(1) == 1 && !broadcast(*h, 2) && !broadcast(*w, 1) && element_type(*h, type));
   const int64_t B = h->size(0), S = h->size(1), K = h->size(2), V = w->size(0);
   ORDINARY(w->size(1) == K && w->scalar_type() == h->scalar_type());
   const at::Tensor *sl = a[2] == Py_None ? nullptr : plain(a[2], at::kInt, B);
@@ -278,22 +285,14 @@ const at::Tensor *local_tensor(PyObject *o) {
   return t && t->device().index() == c10::hip::current_device() ? t : nullptr;
 }
 
-// Strides of rows and sequences as lsp_token_scores takes them, which has a meaning of its own for 0.
-bool row_strides(const at::Tensor &z, int64_t &row, int64_t &batch) {
-  row = z.size(1) == 1 ? z.size(2) : z.stride(1);
-  batch = z.size(0) == 1 ? row * z.size(1) : z.stride(0);
-  return row > 0 && batch > 0;
-}
 // (logits, token_id or None, suffix_len or None, num_alt, out, workspace or None)
 PyObject *token_scores(PyObject *, PyObject *const *a, Py_ssize_t n) {
   ARGUMENTS(6);
   const at::Tensor *z = local_tensor(a[0]);
   int32_t type;
   long K;
-  ORDINARY(z && z->dim() == 3 && z->stride(2) == 1 && element_type(*z, type) && integer(a[3], K) && K >= 0 && K <= 32);
-  const int64_t B = z->size(0), S = z->size(1), V = z->size(2);
-  int64_t row, batch;
-  ORDINARY(row_strides(*z, row, batch));
+  ORDINARY(z && z->dim() == 3 && z->stride(2) == 1 && !broadcast(*z, 2) && element_type(*z, type) && integer(a[3], K) && K >= 0 && K <= 32);
+  const int64_t B = z->size(0), S = z->size(1), V = z->size(2), row = S == 1 ? V : z->stride(1), batch = B == 1 ? S * row : z->stride(0);
   const at::Tensor *id = a[1] == Py_None ? nullptr : dense(a[1], at::kInt, {B, S}), *sl = a[2] == Py_None ? nullptr : dense(a[2], at::kInt, {B});
   ORDINARY((id || a[1] == Py_None) && (sl || a[2] == Py_None) && PyTuple_Check(a[4]) && PyTuple_GET_SIZE(a[4]) == 4);
   PyObject *const *o = &PyTuple_GET_ITEM(a[4], 0);

@@ -88,3 +88,33 @@ def test_keys_and_values_of_a_table_are_laid_out_alike(host):
             m.LayerTable(*[[t] for t in a])
     m.LayerTable([k], [k], [wide[:, :16]], [wide[:, 4:]])
     m.LayerTable([k[:1]], [wide[:1, :4]], [c[:1]], [wide[:1, :16]])      # (one sequence's stride is of no use)
+
+
+@pytest.mark.parametrize("S", [1, 5])
+def test_logits_hidden_states_and_weights(host, S):
+    """(All but one of size 1 is a tensor that a stride of 0 says nothing about.)"""
+    i = torch.zeros((2, S), dtype=torch.int32)
+    out = (i, i.float(), i.float())
+    z = torch.zeros(8)
+    for bad in (z.expand(2, S, 8), torch.zeros(1, S, 8).expand(2, S, 8), torch.zeros(2, 1, 8).expand(2, 5, 8)):
+        o = tuple(torch.zeros(bad.shape[:2], dtype=t.dtype) for t in out)
+        for call in (lambda: m.confidence(bad), lambda: m.confidence(bad, out=o), lambda: m.confidence_static(bad, None, o),
+                     lambda: m.lm_head_confidence(bad, torch.zeros(16, 8)), lambda: m.lm_head_confidence(bad, torch.zeros(16, 8), out=o)):
+            with pytest.raises(m.LspError, match="broadcast"):
+                call()
+    with pytest.raises(m.LspError, match="broadcast"):
+        m.lm_head_confidence(torch.zeros(2, S, 8), z.expand(16, 8))
+
+
+@pytest.mark.gpu
+def test_the_native_reductions_refuse_them_too():
+    z, w = torch.zeros(2, 5, 64).cuda().bfloat16(), torch.zeros(32, 64).cuda().bfloat16()
+    f = torch.zeros(2, 5).cuda()
+    out = (f.int(), f, f.clone())
+    for bad in (z[:1].expand(2, 5, 64), z[:, :1].expand(2, 5, 64)):
+        for call in (lambda: m.confidence(bad), lambda: m.lm_head_confidence(bad, w, out=out, workspace=torch.zeros(1 << 20, dtype=torch.uint8).cuda()),
+                     lambda: m.token_scores(bad, out=(None, f, None, None))):
+            with pytest.raises(m.LspError, match="broadcast"):
+                call()
+    with pytest.raises(m.LspError, match="broadcast"):
+        m.lm_head_confidence(z, w[:1].expand(32, 64), out=out, workspace=torch.zeros(1 << 20, dtype=torch.uint8).cuda())
