@@ -15,6 +15,13 @@ from . import (BY_PLACE, AttnLayerTable, LayerTable, LspError, ProgressPoll, _co
                lm_head_confidence, lm_head_confidence_workspace_bytes, token_scores, token_scores_workspace_bytes)
 
 
+def _need_on(device, name, t, *rest, **kw):
+    """_need, on this device: what a step finds out later has changed the caller's state by then."""
+    _need(name, t, *rest, **kw)
+    if t is not None and t.device != device:
+        raise LspError(f"decode_loop: {name} is on {t.device}, the sequences are on {device}")
+
+
 class _Scores:
     """What the committed tokens' positions are told about them: buffers of one entry per token of the caller's, filled as `tokens` is."""
 
@@ -29,7 +36,7 @@ class _Scores:
         if "alt_id" in buffers and not 1 <= self.K <= 32:
             raise LspError(f"decode_loop: 1 to 32 alternatives, got {self.K}")
         for k, t in buffers.items():
-            _need(f"scores['{k}']", t, torch.int32 if k == "alt_id" else torch.float32, (B, T, self.K) if k.startswith("alt") else (B, T))
+            _need_on(tokens.device, f"scores['{k}']", t, torch.int32 if k == "alt_id" else torch.float32, (B, T, self.K) if k.startswith("alt") else (B, T))
         self.buffers, self.out, self.workspace = buffers, None, None
         self.place = torch.arange(T, device=tokens.device)
 
@@ -72,13 +79,14 @@ class _Budget:
         shape = (table.n, table.B, table.Hkv, table.C)
         if self.weights is None:
             self.weights = torch.zeros(shape, device=prefix_len.device)
-        _need("cache_len", self.cache_len, torch.int32, (table.B,))
+        dev = prefix_len.device
+        _need_on(dev, "cache_len", self.cache_len, torch.int32, (table.B,))
         if self.cache_len.data_ptr() in (prefix_len.data_ptr(), suffix_len.data_ptr()):
             raise LspError("decode_loop: cache_len is a buffer of its own")
-        _need("weights", self.weights, torch.float32, shape)
+        _need_on(dev, "weights", self.weights, torch.float32, shape)
         if self.positions is None and k["recent"] > 0:
-            self.positions = torch.full(shape, BY_PLACE, dtype=torch.int32, device=prefix_len.device)
-        _need("positions", self.positions, torch.int32, shape, optional=True)
+            self.positions = torch.full(shape, BY_PLACE, dtype=torch.int32, device=dev)
+        _need_on(dev, "positions", self.positions, torch.int32, shape, optional=True)
         left, rows = torch.stack([suffix_len.max(), (suffix_len + self.cache_len).max()]).tolist()
         if max(rows, left + self.kw["high"]) > table.C:
             raise LspError(f"decode_loop: a cache of {table.C} rows has no room for {left} more positions on {self.kw['high']} rows (high), or on those there are")
