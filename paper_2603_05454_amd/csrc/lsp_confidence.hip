@@ -39,6 +39,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLagOctaves = 32.0f;  // the reference may lag the maximum by this much
+// Maxima farther from 0 than 2^26: the reference is a rounded product, and the maximum's own exponent its rounding error, up to half a step of it:
+// 4 octaves here, 512 at 1e10, where 2^512 is infinite.  Such rows' sums are formed anew, and those that such entries (of a mask, say)
+// have made infinite or NaN on the way.
+constexpr float kFar = 67108864.f;
 
 struct Top {
   float m1, m2;  // largest and second largest value seen (duplicates count)
@@ -184,6 +188,21 @@ __device__ __forceinline__ RowStat merge_stats(const Top &t) {
   return wave_combine(t, all_max, __builtin_amdgcn_exp2f((t.m1 - all_max) * kLog2e));  // exp(m1 - max); 0 for the idle lanes
 }
 
+// The sum over [c0, c1) relative to the maximum `top`, with the differences first; one wave's work, for rows with entries far from 0.
+template <typename T>
+__device__ __forceinline__ float sum_of_differences(const T *row, int c0, int c1, float top) {
+  constexpr int kAhead = 8;
+  float s = 0.f;
+  for (int c = c0 + int(threadIdx.x & (kWave - 1)); c < c1; c += kAhead * kWave) {
+    float x[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) x[k] = c + k * kWave < c1 ? Vec<T>::scalar(row + c + k * kWave) : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) s += __builtin_amdgcn_exp2f((x[k] - top) * kLog2e);
+  }
+  return wave_reduce(s, OpAdd());
+}
+
 // One workgroup reduces elements [c0, c1) of one row.  NT threads; U vectors per
 // lane per group; two groups of loads in flight (ping-pong register buffers).
 // The result is valid in wave 0; the other waves only take part.
@@ -321,6 +340,7 @@ __device__ __forceinline__ RowStat segment_stat(const T *row, int c0, int c1) {
     }
     r = merge_stats(t);
   }
+  if ((fabsf(r.m1) > kFar || !(r.s <= FLT_MAX)) && r.m1 > -INFINITY) r.s = sum_of_differences(row, c0, c1, r.m1);
   return r;
 }
 
