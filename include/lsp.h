@@ -404,8 +404,8 @@ int32_t lsp_commit_step(const lsp_commit_desc *desc, const float *margin, const 
  *     alt_logprob[b,i,0..K) = log p of each
  * in fp32 throughout.  Rows i >= N_b are neither read nor written.  -inf entries
  * have probability 0 (as do those of the type's lowest value beside ordinary ones); a row of nothing but -inf
- * gives -inf everywhere and entropy 0.  Where V < K the list ends with id -1 and
- * -inf.  Precondition: no NaN and no +inf in the row.
+ * gives log probabilities -inf, entropy 0 and the ids from 0 on.  Where V < K the list ends with id -1 and
+ * -inf.  Precondition: no NaN and no +inf in the row; finite logits may be of any size.
  * ------------------------------------------------------------------------- */
 /* Bytes of a workspace with which few long rows are shared by several workgroups each; 0 where it is of no use. */
 size_t lsp_token_scores_workspace_bytes(int32_t B, int32_t S, int32_t V, int32_t num_alt);

@@ -10,7 +10,8 @@
 //
 // Which rows are the last: those at the end, as long as rows are only appended.  An eviction puts rows from the end among the others, so that a cache that is evicted from
 // again needs its rows' positions.  They are kept beside the weights, for rows from `keep` on as "by place" (kByPlace), since those in front of the end were appended in
-// order: a row at t is P - t rows old.  An append has nothing to write then, and an eviction writes the positions below `keep`.
+// order: a row at t is P - t rows old.  An append has nothing to write then, and an eviction writes the positions below `keep`.  They cost their bytes and one count more
+// (4 rows to leave: one layer of four heads, 516 rows, 8.5 us by place, 13.1 by position; 32 layers of 8 x 4100 rows of 32 heads, 134 MB of positions, 149 and 218).
 //
 // Where they go: keys carry their positions and the attention has no mask, so the order of cached rows means nothing.  Rows
 // below `keep` that stay do not move; each row from `keep` on that stays goes into the place of one below that leaves (the n-th of
