@@ -151,3 +151,29 @@ def test_graph_replays(lsp):
             assert torch.equal(d.cpu(), h)
         c.append([9, 1])
         c.evict(**kw)
+
+
+def test_more_than_2_31_positions(lsp):
+    """30 layers of 8 x 300 000 rows of 32 heads; the last sequence is cut, in the first and the last layer by the definition."""
+    L, B, H, D, C, keep, recent = 30, 8, 32, 8, 300_000, 299_900, 5000
+    g = torch.Generator(device="cuda").manual_seed(7)
+    caches = [[torch.empty((B, C, H, D), dtype=torch.bfloat16, device="cuda") for _ in range(L)] for _ in range(2)]     # (what moves there is not looked at)
+    w = torch.zeros((L, B, H, C), device="cuda")
+    w[:, -1].uniform_(generator=g)
+    at = torch.full((L, B, H, C), lsp.BY_PLACE, dtype=torch.int32, device="cuda")
+    assert at.numel() > 2**31
+    some = [(0, 0), (L - 1, H - 1)]
+    for l, h in some:
+        at[l, -1, h] = torch.randperm(C, device="cuda", generator=g).to(torch.int32)
+    P = torch.tensor([0] * (B - 1) + [C], dtype=torch.int32, device="cuda")
+    T = P + 70
+    wanted = []
+    for l, h in some:
+        p = at[l, -1, h].cpu().view(1, 1, 1, C).clone()
+        wanted.append((*serving.evict(w[l, -1, h].cpu().view(1, 1, 1, C), P[-1:].cpu(), keep, recent=recent, positions=p, token_len=T[-1:].cpu()), p))
+    suf = [torch.zeros((B, 1, H, D), dtype=torch.bfloat16, device="cuda")] * L
+    lsp.kv_evict(w, P, lsp.LayerTable(suf, suf, *caches), keep=keep, recent=recent, positions=at, token_len=T)
+    assert P.tolist() == [0] * (B - 1) + [keep]
+    for (l, h), (weight, _, _, p) in zip(some, wanted):
+        assert torch.equal(at[l, -1, h].cpu(), p[0, 0, 0]) and torch.equal(w[l, -1, h].cpu(), weight[0, 0, 0])
+    assert (at[:, :-1] == lsp.BY_PLACE).all() and (at[1, -1, 0, keep:] == lsp.BY_PLACE).all() and (at[1, -1, 0, :keep] >= 70).all()
