@@ -68,7 +68,7 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// How many tokens are at or behind a row's: 1 for the last one.  (Differences that wrap: numbers that make no sense may do any harm but undefined.)
+// How many tokens are at or behind a row's: 1 for the last one.  (Unsigned differences: numbers that make no sense give some age.)
 __device__ __forceinline__ int age_of(int32_t position, int32_t tokens, int rows, int t) {
   return position == kByPlace ? rows - t : int32_t(uint32_t(tokens) - uint32_t(position));
 }
