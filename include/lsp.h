@@ -512,6 +512,99 @@ int32_t lsp_kv_evict_positions(const lsp_evict_desc *desc, const float *weights,
                                void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- *
+ * Norms of heads and position rotation of a step's queries and keys, in one pass, as they
+ * come from their projections and before lsp_attn_step.  For every sequence b, active row
+ * u < N_b and head, with x the head's D elements:
+ *     y = x * rsqrt(mean(x^2) + eps) * weight            (y = x without weights)
+ *     (y_i, y_j) -> (y_i cos t - y_j sin t, y_j cos t + y_i sin t),  t = position * inv_freq[p]
+ * for the pairs p < R/2 of the first R elements: i = p, j = p + R/2, or i = 2p, j = 2p + 1
+ * (interleaved).  position = positions[b,u], or prefix_len[b] + u (u without prefix_len).
+ * fp32 throughout, the angle's product and reduction in 64 bits, one rounding at the end.
+ * Rows u >= N_b are neither read nor written.  The outputs may be q and k themselves.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype;          /* lsp_dtype of q, k and the outputs */
+  int32_t B, S, Hq, Hkv;
+  int32_t D;              /* 64 or 128 */
+  int32_t R;              /* elements of a head that turn: 0 to D, a multiple of 16 */
+  int32_t interleaved;    /* which pairs */
+  float eps;
+  /* element strides of (batch, row, head); all three 0 selects the dense default */
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+} lsp_qk_norm_rope_desc;
+
+/*
+ * q [B,S,Hq,D], k [B,S,Hkv,D], q_out, k_out: device, 16-byte aligned, strides multiples of
+ * 16 bytes (slices of one buffer of projections are fine; an output is its input or does not overlap it).  q_weight,
+ * k_weight: device fp32[D], or both NULL.  inv_freq: device fp32[R/2].  prefix_len,
+ * suffix_len: device int32[B], or NULL (0, and all S rows).  positions: device int32 [B,S],
+ * or NULL.  Limits: B, Hq, Hkv <= 65535, S <= 2^24.
+ */
+int32_t lsp_qk_norm_rope(const lsp_qk_norm_rope_desc *desc, const void *q, const void *k, const float *q_weight,
+                         const float *k_weight, const float *inv_freq, const int32_t *prefix_len,
+                         const int32_t *suffix_len, const int32_t *positions, void *q_out, void *k_out, void *stream);
+
+/* ------------------------------------------------------------------------- *
+ * Caches in 8 bits.  A cache [B, C, Hkv, D] holds e4m3 values (four bits of exponent, three
+ * of mantissa, magnitudes up to 448, NaN and no infinity); rows 32 j to 32 j + 31 of a head share the byte
+ * E = scale[b,g,j] and stand for value * 2^(E - 127), 1 <= E <= 246.  scale: uint8
+ * [B, Hkv, ceil(C / 32)], dense.  head_dim 64 or 128; cache strides in elements (bytes), multiples of 16.
+ * ------------------------------------------------------------------------- */
+#define LSP_Q8_BLOCK 32
+
+/*
+ * The rows that lsp_commit has committed, quantised as they are written: for every layer, with
+ * P = prefix_len[b] (cached rows WITH the new ones, as lsp_commit leaves it) and
+ * n = commit_len[b] (cut to S and P), rows [P - n, P) of the cache receive suffix rows [0, n),
+ * each value rounded to the nearest (ties to even).  E of a block is the smallest with which
+ * its largest finite magnitude is at most 448 * 2^(E - 127) (from 1 to 246: magnitudes above
+ * 1.75 * 2^127 become that); infinities and NaN become NaN.  Where the first block has rows from
+ * before it keeps its E if that is larger; if not, its rows are rounded again under the new one.
+ * A second call with the same arguments changes nothing.  Other rows and scales are left as they are.
+ * No length is changed: lsp_commit (with num_layers = 0 and this C) has advanced them; a prompt is
+ * appended with commit_len = prefix_len = its length, S being the rows of the buffers that hold its K/V.
+ * desc: dtype (of the suffix buffers, LSP_F32 or LSP_BF16), B, S, Hkv, D, C, kv_suf_stride, cache_stride
+ * (a cache's rows must be those of one sequence); the rest is not used.  *_layers: HOST arrays of num_layers
+ * DEVICE pointers, as for lsp_commit; buffers 16-byte aligned, scales of any alignment.
+ */
+int32_t lsp_kv_append_q8(const lsp_attn_desc *desc, int32_t num_layers, const void *const *k_suf_layers,
+                         const void *const *v_suf_layers, void *const *k_cache_layers, void *const *v_cache_layers,
+                         void *const *k_scale_layers, void *const *v_scale_layers, const int32_t *commit_len,
+                         const int32_t *prefix_len, void *stream);
+
+/*
+ * Rows [first_row[b], end_row[b]) of the caches as the values they stand for, in rows 0, 1, ... of
+ * k_out, v_out [B, S, Hkv, D] (of the descriptor's dtype and S, strides kv_suf_stride; cut to S rows; first_row is cut to 0..C, end_row
+ * to first_row..C).  Exact in fp32, and in bf16 from E = 10 on (below, what is subnormal there is rounded).  The rest of
+ * the outputs is not written.
+ */
+int32_t lsp_kv_read_q8(const lsp_attn_desc *desc, int32_t num_layers, const void *const *k_cache_layers,
+                       const void *const *v_cache_layers, const void *const *k_scale_layers,
+                       const void *const *v_scale_layers, const int32_t *first_row, const int32_t *end_row,
+                       void *const *k_out_layers, void *const *v_out_layers, void *stream);
+
+/*
+ * lsp_attn_step over caches in 8 bits: the P_b cached rows are the values they stand for, the suffix K/V, queries
+ * and outputs bf16 (dtype LSP_BF16 only).  Arguments as there beside the scales; cache_stride as above.
+ * workspace: device, 16-byte aligned, lsp_attn_q8_workspace_bytes(desc, num_layers) bytes of any content,
+ * for this call alone until it has run; with it the keys of few rows are divided between workgroups, without
+ * (NULL, or fewer bytes) a tile's keys are one workgroup's.
+ * Limits: those of lsp_attn_step; C, S <= 2^30, B * Hkv < 2^26, S * Hq / Hkv <= 2^30.
+ */
+size_t lsp_attn_q8_workspace_bytes(const lsp_attn_desc *desc, int32_t num_layers);
+int32_t lsp_attn_step_q8(const lsp_attn_desc *desc, const void *q, const void *k_suf, const void *v_suf,
+                         const void *k_cache, const void *v_cache, const uint8_t *k_scale, const uint8_t *v_scale,
+                         const int32_t *prefix_len, const int32_t *suffix_len, void *out, void *workspace,
+                         size_t workspace_bytes, void *stream);
+/* and for every layer in one launch (32 layers to a launch), as lsp_attn_step_layers */
+int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *desc, int32_t num_layers, const void *const *q_layers,
+                                const void *const *k_suf_layers, const void *const *v_suf_layers,
+                                const void *const *k_cache_layers, const void *const *v_cache_layers,
+                                const void *const *k_scale_layers, const void *const *v_scale_layers,
+                                const int32_t *prefix_len, const int32_t *suffix_len, void *const *out_layers,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- *
  * Measurement helper (used by the benchmark, not part of the scheduler step):
  * a bare streaming read of `bytes` bytes of device memory by `workgroups`
  * workgroups of 512 threads (16-byte non-temporal loads, each workgroup one

@@ -27,6 +27,7 @@ _nat_addresses = _nat_attn_table = _nat_layer_table = None
 _nat = None     # the native marshalling module, bound to the loaded library (None: not loaded, or not built)
 
 LSP_F32, LSP_BF16 = 0, 1
+Q8_BLOCK = 32   # rows of a head that share a scale in a cache of 8 bits
 LSP_ERR_WORKSPACE = -3
 FLAG_CACHE_FULL, FLAG_TOKENS_FULL = 1, 2
 
@@ -53,6 +54,13 @@ class CommitDesc(ctypes.Structure):
                 ("alpha", ctypes.c_float), ("beta", ctypes.c_float), ("max_commit", ctypes.c_int32)]
 
 
+class QkNormRopeDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("S", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("R", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3), ("q_out_stride", ctypes.c_int64 * 3),
+                ("k_out_stride", ctypes.c_int64 * 3)]
+
+
 class EvictDesc(ctypes.Structure):
     _fields_ = [("kv_dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
                 ("C", ctypes.c_int32), ("num_layers", ctypes.c_int32), ("keep", ctypes.c_int32), ("high", ctypes.c_int32),
@@ -65,13 +73,17 @@ EXPORTS = ["lsp_version", "lsp_last_error", "lsp_attn_workspace_bytes", "lsp_att
            "lsp_commit", "lsp_commit_step", "lsp_flip_update", "lsp_poll_lengths", "lsp_poll_progress", "lsp_select_scattered", "lsp_kv_gather_append",
            "lsp_attn_step_gather", "lsp_lm_head_confidence_workspace_bytes", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma",
            "lsp_token_scores_workspace_bytes", "lsp_token_scores", "lsp_attn_key_weights_workspace_bytes", "lsp_attn_key_weights",
-           "lsp_kv_evict_workspace_bytes", "lsp_kv_evict", "lsp_kv_evict_positions"]
+           "lsp_kv_evict_workspace_bytes", "lsp_kv_evict", "lsp_kv_evict_positions",
+           "lsp_qk_norm_rope"]
+# those of caches in 8 bits (names with a digit are listed by themselves)
+EXPORTS_Q8 = ["lsp_kv_append_q8", "lsp_kv_read_q8", "lsp_attn_q8_workspace_bytes", "lsp_attn_step_q8", "lsp_attn_step_q8_layers"]
 
 # entry points that the native module calls, in the order of its table
 NATIVE_ENTRIES = ("lsp_attn_workspace_bytes", "lsp_attn_step", "lsp_attn_step_layers", "lsp_confidence_workspace_bytes", "lsp_confidence",
                   "lsp_lm_head_confidence_workspace_bytes", "lsp_lm_head_confidence", "lsp_commit", "lsp_flip_update", "lsp_poll_lengths", "lsp_commit_step",
                   "lsp_poll_progress", "lsp_token_scores_workspace_bytes", "lsp_token_scores", "lsp_attn_key_weights_workspace_bytes",
-                  "lsp_attn_key_weights", "lsp_kv_evict_workspace_bytes", "lsp_kv_evict", "lsp_kv_evict_positions")
+                  "lsp_attn_key_weights", "lsp_kv_evict_workspace_bytes", "lsp_kv_evict", "lsp_kv_evict_positions",
+                  "lsp_qk_norm_rope", "lsp_kv_append_q8", "lsp_kv_read_q8", "lsp_attn_q8_workspace_bytes", "lsp_attn_step_q8", "lsp_attn_step_q8_layers")
 
 
 def lib() -> ctypes.CDLL:
@@ -86,11 +98,11 @@ def lib() -> ctypes.CDLL:
         L.lsp_last_error.restype = ctypes.c_char_p
         for n in ("lsp_attn_workspace_bytes", "lsp_confidence_workspace_bytes", "lsp_commit_workspace_bytes",
                   "lsp_lm_head_confidence_workspace_bytes", "lsp_confidence_static_scratch_bytes", "lsp_token_scores_workspace_bytes",
-                  "lsp_attn_key_weights_workspace_bytes", "lsp_kv_evict_workspace_bytes"):
+                  "lsp_attn_key_weights_workspace_bytes", "lsp_kv_evict_workspace_bytes", "lsp_attn_q8_workspace_bytes"):
             getattr(L, n).restype = ctypes.c_size_t
         for n in ("lsp_attn_step", "lsp_attn_step_layers", "lsp_confidence", "lsp_confidence_static", "lsp_commit", "lsp_commit_step", "lsp_flip_update", "lsp_poll_lengths", "lsp_select_scattered",
                   "lsp_kv_gather_append", "lsp_attn_step_gather", "lsp_lm_head_confidence", "lsp_bench_read", "lsp_bench_mfma", "lsp_token_scores", "lsp_attn_key_weights", "lsp_kv_evict",
-                  "lsp_kv_evict_positions"):
+                  "lsp_kv_evict_positions", "lsp_qk_norm_rope", "lsp_kv_append_q8", "lsp_kv_read_q8", "lsp_attn_step_q8", "lsp_attn_step_q8_layers"):
             getattr(L, n).restype = ctypes.c_int32
         try:
             from . import _binding
@@ -878,6 +890,219 @@ def kv_evict(weights, prefix_len, layers: LayerTable, keep, high=None, first=0, 
         rc = lib().lsp_kv_evict_positions(ctypes.byref(d), _ptr(weights), _ptr(positions), _ptr(token_len), *rest)
     _check(rc, "lsp_kv_evict")
     return new_len
+
+
+def _own_strides3(name, t):
+    """Strides of what is written to, or read row by row: sequences, rows and heads of its own."""
+    s = _strides3(t)
+    _not_broadcast(name, t, 3)
+    return s
+
+
+def qk_norm_rope(q, k, inv_freq, q_weight=None, k_weight=None, eps=1e-6, prefix_len=None, suffix_len=None, positions=None, interleaved=False, out=None):
+    """lsp_qk_norm_rope: norms of heads (with q_weight, k_weight fp32 [D]; none without) and position rotation of a step's queries
+    [B,S,Hq,D] and keys [B,S,Hkv,D] in one pass, before attn_step.  inv_freq fp32 [R/2]: the first R elements of a head turn, R a multiple
+    of 16 (0: none), halves with each other or neighbours (interleaved).  Row u of sequence b is at prefix_len[b] + u (at u without it),
+    or at positions int32 [B,S].  Rows >= suffix_len[b] (default: S) are not written.  out: (q_out, k_out), (q, k) for in place;
+    default: new ones.  Returns out."""
+    if out is None:
+        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device))
+    elif len(out) != 2:
+        raise LspError("out must be (q_out, k_out)")
+    if _nat is not None:
+        rc = _nat.qk_norm_rope(q, k, inv_freq, q_weight, k_weight, eps, prefix_len, suffix_len, positions, interleaved, *out)
+        if rc is not None:
+            _check(rc, "lsp_qk_norm_rope")
+            return out
+    _here(q, k, inv_freq, q_weight, k_weight, prefix_len, suffix_len, positions, *out)
+    if q.dim() != 4 or k.dim() != 4:
+        raise LspError("queries and keys are [batch, row, head, D]")
+    B, S, Hq, D = q.shape
+    for name, t, shape in (("k", k, (B, S, k.shape[2], D)), ("out[0] (q_out)", out[0], tuple(q.shape)), ("out[1] (k_out)", out[1], tuple(k.shape))):
+        if t.dtype != q.dtype or tuple(t.shape) != shape:
+            raise LspError(f"{name} must be {q.dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    _need("inv_freq", inv_freq, torch.float32)
+    if inv_freq.dim() != 1 or inv_freq.shape[0] > D // 2:
+        raise LspError(f"inv_freq is [R/2], R at most {D}, got {tuple(inv_freq.shape)}")
+    _need("q_weight", q_weight, torch.float32, (D,), optional=True)
+    _need("k_weight", k_weight, torch.float32, (D,), optional=True)
+    _need("prefix_len", prefix_len, torch.int32, (B,), optional=True)
+    _need("suffix_len", suffix_len, torch.int32, (B,), optional=True)
+    _need("positions", positions, torch.int32, (B, S), optional=True)
+    d = QkNormRopeDesc(dtype=_dtype(q), B=B, S=S, Hq=Hq, Hkv=k.shape[2], D=D, R=2 * inv_freq.shape[0], interleaved=int(bool(interleaved)), eps=float(eps))
+    d.q_stride, d.k_stride = _own_strides3("q", q), _own_strides3("k", k)
+    d.q_out_stride, d.k_out_stride = _own_strides3("out[0] (q_out)", out[0]), _own_strides3("out[1] (k_out)", out[1])
+    rc = lib().lsp_qk_norm_rope(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), _ptr(prefix_len), _ptr(suffix_len),
+                                _ptr(positions), _ptr(out[0]), _ptr(out[1]), _stream())
+    _check(rc, "lsp_qk_norm_rope")
+    return out
+
+
+def q8_cache(B, C, Hkv, D, device="cuda"):
+    """An empty cache in 8 bits: (k_cache, v_cache e4m3 [B,C,Hkv,D], k_scale, v_scale uint8 [B,Hkv,ceil(C/32)])."""
+    f = dict(dtype=torch.uint8, device=device)
+    caches = [torch.zeros((B, C, Hkv, D), **f).view(torch.float8_e4m3fn) for _ in range(2)]
+    return (*caches, *[torch.ones((B, Hkv, -(-C // Q8_BLOCK)), **f) for _ in range(2)])
+
+
+def _q8_desc(k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, q=None, out=None):
+    """The descriptor of suffix buffers and a cache in 8 bits, or of the first layer of several."""
+    for t in (k_suf, k_cache):
+        if t.dim() != 4:
+            raise LspError("suffix buffers and caches are [batch, row, head, D]")
+    B, S, Hkv, D = k_suf.shape
+    C = k_cache.shape[1]
+    e4m3, blocks = torch.float8_e4m3fn, -(-C // Q8_BLOCK)
+    for name, t, dtype, shape in (("v_suf", v_suf, k_suf.dtype, (B, S, Hkv, D)), ("k_cache", k_cache, e4m3, (B, C, Hkv, D)),
+                                  ("v_cache", v_cache, e4m3, (B, C, Hkv, D)), ("k_scale", k_scale, torch.uint8, (B, Hkv, blocks)),
+                                  ("v_scale", v_scale, torch.uint8, (B, Hkv, blocks))):
+        if t.dtype != dtype or tuple(t.shape) != shape:
+            raise LspError(f"{name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    if v_suf.stride() != k_suf.stride() or v_cache.stride() != k_cache.stride():
+        raise LspError("K and V must share strides")
+    _need("k_scale", k_scale, torch.uint8)
+    _need("v_scale", v_scale, torch.uint8)
+    d = AttnDesc(dtype=_dtype(k_suf), B=B, S=S, Hq=Hkv, Hkv=Hkv, D=D, C=C)
+    d.kv_suf_stride, d.cache_stride = _strides3(k_suf), _strides3(k_cache)
+    if q is not None:
+        if q.dim() != 4 or q.dtype != k_suf.dtype or (q.shape[0], q.shape[1], q.shape[3]) != (B, S, D):
+            raise LspError(f"q must be {k_suf.dtype} [{B}, {S}, heads, {D}], got {q.dtype} {tuple(q.shape)}")
+        if out.dtype != q.dtype or out.shape != q.shape:
+            raise LspError(f"out must be {q.dtype} {tuple(q.shape)}, got {out.dtype} {tuple(out.shape)}")
+        d.Hq = q.shape[2]
+        d.q_stride, d.o_stride = _strides3(q), _own_strides3("out", out)
+    return d
+
+
+class Q8LayerTable:
+    """Host arrays of per-layer device pointers for caches in 8 bits, built once and reused (all layers share shapes, strides and element
+    types): lists of suffix buffers [B,S,Hkv,D], caches (torch.float8_e4m3fn [B,C,Hkv,D]) and scales (uint8 [B,Hkv,ceil(C/32)]), as q8_cache
+    makes them; with q and out [B,S,Hq,D] for attn_step_q8_layers."""
+
+    def __init__(self, k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, q=None, out=None):
+        if (q is None) != (out is None):
+            raise LspError("Q8LayerTable: q and out come together")
+        lists = (k_suf, v_suf, k_cache, v_cache, k_scale, v_scale) + (() if q is None else (q, out))
+        n = len(k_suf)
+        if n == 0 or any(len(lst) != n for lst in lists):
+            raise LspError("Q8LayerTable: one tensor of each kind per layer, at least one layer")
+        lib()
+        made = _nat.q8_table(*lists) if _nat is not None else None
+        if made is None:
+            for lst in lists:
+                for t in lst:
+                    _dev(t)
+                    if t.shape != lst[0].shape or t.stride() != lst[0].stride() or t.dtype != lst[0].dtype or t.device != k_suf[0].device:
+                        raise LspError("Q8LayerTable: all layers must share shape, strides, element type and device")
+            d = _q8_desc(*[lst[0] for lst in lists])
+            arrays = [bytes((ctypes.c_void_p * n)(*[t.data_ptr() for t in lst])) for lst in lists]
+            made = bytes(d), arrays + (arrays[:2] if q is None else [])
+        self.n, self.keep, self.out, (self.packed, self.arrays) = n, lists, out, made
+
+    @property
+    def desc(self):
+        return AttnDesc.from_buffer_copy(self.packed)
+
+    def pointers(self, k):
+        return (ctypes.c_void_p * self.n).from_buffer_copy(self.arrays[k])
+
+
+def kv_append_q8(layers: Q8LayerTable, commit_len, prefix_len):
+    """lsp_kv_append_q8: the rows that commit(..., layers=None, C=...) has committed go into the caches of `layers`: rows [prefix_len[b] - commit_len[b],
+    prefix_len[b]) receive suffix rows [0, commit_len[b]), quantised as they are written.  prefix_len: as commit leaves it, with the new
+    rows.  A prompt: commit_len = prefix_len = its length."""
+    _table_here(layers.keep[2][0])
+    if _nat is not None:
+        rc = _nat.kv_append_q8(layers.packed, layers.n, layers.arrays, commit_len, prefix_len)
+        if rc is not None:
+            return _check(rc, "lsp_kv_append_q8")
+    d, a = layers.desc, layers.pointers
+    _here(commit_len, prefix_len)
+    _need("commit_len", commit_len, torch.int32, (d.B,))
+    _need("prefix_len", prefix_len, torch.int32, (d.B,))
+    _not_broadcast("k_cache", layers.keep[2][0], 3)
+    _check(lib().lsp_kv_append_q8(ctypes.byref(d), layers.n, *[a(k) for k in range(6)], _ptr(commit_len), _ptr(prefix_len), _stream()), "lsp_kv_append_q8")
+
+
+def kv_read_q8(layers: Q8LayerTable, first_row, end_row, k_out, v_out):
+    """lsp_kv_read_q8: rows first_row[b] to end_row[b] of the caches of `layers` as the values they stand for, in the rows from 0 on of k_out, v_out
+    (lists of a tensor [B,R,Hkv,D], bf16 or fp32, per layer).  Returns (k_out, v_out)."""
+    _table_here(layers.keep[2][0])
+    if _nat is not None:
+        rc = _nat.kv_read_q8(layers.packed, layers.n, layers.arrays, first_row, end_row, k_out, v_out)
+        if rc is not None:
+            _check(rc, "lsp_kv_read_q8")
+            return k_out, v_out
+    d, a = layers.desc, layers.pointers
+    _here(first_row, end_row, *k_out, *v_out)
+    _need("first_row", first_row, torch.int32, (d.B,))
+    _need("end_row", end_row, torch.int32, (d.B,))
+    if len(k_out) != layers.n or len(v_out) != layers.n:
+        raise LspError(f"k_out and v_out hold a tensor per layer, {layers.n}")
+    first = k_out[0]
+    for t in (*k_out, *v_out):
+        if t.dim() != 4 or (t.shape[0], t.shape[2], t.shape[3]) != (d.B, d.Hkv, d.D):
+            raise LspError(f"k_out and v_out are [{d.B}, rows, {d.Hkv}, {d.D}], got {tuple(t.shape)}")
+        if t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype:
+            raise LspError("k_out and v_out must share shape, strides and element type")
+    d.dtype, d.S = _dtype(first), first.shape[1]
+    d.kv_suf_stride = _own_strides3("k_out", first)
+    Arr = ctypes.c_void_p * layers.n
+    _check(lib().lsp_kv_read_q8(ctypes.byref(d), layers.n, a(2), a(3), a(4), a(5), _ptr(first_row), _ptr(end_row), Arr(*[t.data_ptr() for t in k_out]),
+                                Arr(*[t.data_ptr() for t in v_out]), _stream()), "lsp_kv_read_q8")
+    return k_out, v_out
+
+
+def attn_q8_workspace_bytes(B, S, Hq, Hkv, D, C, num_layers=1) -> int:
+    d = AttnDesc(dtype=LSP_BF16, B=B, S=S, Hq=Hq, Hkv=Hkv, D=D, C=C)
+    return lib().lsp_attn_q8_workspace_bytes(ctypes.byref(d), num_layers)
+
+
+def _attn_q8(d, n, arrays, prefix_len, suffix_len, scale, workspace, device):
+    _here(prefix_len, suffix_len)
+    _need("prefix_len", prefix_len, torch.int32, (d.B,))
+    _need("suffix_len", suffix_len, torch.int32, (d.B,))
+    d.scale = float(scale)
+    need = lib().lsp_attn_q8_workspace_bytes(ctypes.byref(d), n)
+    try:
+        workspace = _call_workspace(workspace, need, device)
+    except torch.OutOfMemoryError:
+        workspace, need = None, 0
+    _check(lib().lsp_attn_step_q8_layers(ctypes.byref(d), n, arrays[6], *arrays[:6], _ptr(prefix_len), _ptr(suffix_len), arrays[7], _ptr(workspace),
+                                         ctypes.c_size_t(need), _stream()), "lsp_attn_step_q8")
+
+
+def attn_step_q8(q, k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, prefix_len, suffix_len, scale=0.0, out=None, workspace=None):
+    """lsp_attn_step_q8: attn_step over a cache in 8 bits (bf16 queries and suffix): k_cache/v_cache torch.float8_e4m3fn [B,C,Hkv,D], k_scale/v_scale
+    uint8 [B,Hkv,ceil(C/32)].  Returns out [B,S,Hq,D]; rows >= suffix_len[b] are not written.
+    workspace: contiguous device memory of attn_q8_workspace_bytes(...) bytes and any content, aligned to 16 bytes, for this call alone
+    until it has run; without one that will do, a call that wants one takes its own from torch's allocator."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if _nat is not None:
+        rc = _nat.attn_step_q8(q, k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, prefix_len, suffix_len, scale, out, workspace)
+        if rc is not None:
+            _check(rc, "lsp_attn_step_q8")
+            return out
+    ts = (k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, q, out)
+    _here(*ts)
+    d = _q8_desc(*ts)
+    _attn_q8(d, 1, [(ctypes.c_void_p * 1)(t.data_ptr()) for t in ts], prefix_len, suffix_len, scale, workspace, q.device)
+    return out
+
+
+def attn_step_q8_layers(table: Q8LayerTable, prefix_len, suffix_len, scale=0.0, workspace=None):
+    """lsp_attn_step_q8_layers: the attention of every layer of `table` (with q and out) in one launch.  Returns table.out."""
+    if table.out is None:
+        raise LspError("attn_step_q8_layers: the table has no q and out")
+    _table_here(table.keep[0][0])
+    if _nat is not None:
+        rc = _nat.attn_step_q8_layers(table.packed, table.n, table.arrays, prefix_len, suffix_len, scale, workspace)
+        if rc is not None:
+            _check(rc, "lsp_attn_step_q8")
+            return table.out
+    _attn_q8(table.desc, table.n, [table.pointers(k) for k in range(8)], prefix_len, suffix_len, scale, workspace, table.keep[0][0].device)
+    return table.out
 
 
 def bench_read(buffer, workgroups, out):

@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "liblsp.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["lsp_common.hip", "lsp_confidence.hip", "lsp_commit.hip", "lsp_attn.hip",
            "lsp_attn_f32.hip", "lsp_attn_bf16.hip", "lsp_scattered.hip", "lsp_lm_head.hip", "lsp_token_scores.hip",
-           "lsp_key_weights.hip", "lsp_evict.hip"]
+           "lsp_key_weights.hip", "lsp_evict.hip", "lsp_kv_q8.hip", "lsp_attn_q8.hip", "lsp_qk_norm_rope.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wall", "-Wno-unused-result"]

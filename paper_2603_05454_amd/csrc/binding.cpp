@@ -18,6 +18,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <chrono>
+#include <cstring>
 #include <initializer_list>
 
 #include "binding_workspace.h"
@@ -46,8 +47,14 @@ struct Entry {
   decltype(&lsp_kv_evict_workspace_bytes) kv_evict_workspace_bytes;
   decltype(&lsp_kv_evict) kv_evict;
   decltype(&lsp_kv_evict_positions) kv_evict_positions;
+  decltype(&lsp_qk_norm_rope) qk_norm_rope;
+  decltype(&lsp_kv_append_q8) kv_append_q8;
+  decltype(&lsp_kv_read_q8) kv_read_q8;
+  decltype(&lsp_attn_q8_workspace_bytes) attn_q8_workspace_bytes;
+  decltype(&lsp_attn_step_q8) attn_step_q8;
+  decltype(&lsp_attn_step_q8_layers) attn_step_q8_layers;
 } g;
-constexpr int kEntries = 19;
+constexpr int kEntries = 25;
 
 const at::Tensor *tensor(PyObject *o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
 const at::Tensor *device_tensor(PyObject *o) {
@@ -179,6 +186,12 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   g.kv_evict_workspace_bytes = reinterpret_cast<decltype(g.kv_evict_workspace_bytes)>(p[16]);
   g.kv_evict = reinterpret_cast<decltype(g.kv_evict)>(p[17]);
   g.kv_evict_positions = reinterpret_cast<decltype(g.kv_evict_positions)>(p[18]);
+  g.qk_norm_rope = reinterpret_cast<decltype(g.qk_norm_rope)>(p[19]);
+  g.kv_append_q8 = reinterpret_cast<decltype(g.kv_append_q8)>(p[20]);
+  g.kv_read_q8 = reinterpret_cast<decltype(g.kv_read_q8)>(p[21]);
+  g.attn_q8_workspace_bytes = reinterpret_cast<decltype(g.attn_q8_workspace_bytes)>(p[22]);
+  g.attn_step_q8 = reinterpret_cast<decltype(g.attn_step_q8)>(p[23]);
+  g.attn_step_q8_layers = reinterpret_cast<decltype(g.attn_step_q8_layers)>(p[24]);
   Py_RETURN_NONE;
 }
 
@@ -651,6 +664,153 @@ PyObject *layer_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
                        (long long)kc.size(1), (long long)ks.stride(0), (long long)kc.stride(0), l.bytes[0]->o, l.bytes[1]->o, l.bytes[2]->o, l.bytes[3]->o);
 }
 
+// Strides of a [batch, row, head, D] tensor whose sequences, rows and heads are its own (what is written to must be).
+bool own_strides3(const at::Tensor &t, int64_t (&s)[3]) { return t.dim() == 4 && !broadcast(t, 3) && strides3(t, s); }
+bool q8_scales(const at::Tensor &t, int64_t B, int64_t Hkv, int64_t C) {
+  return t.scalar_type() == at::kByte && t.is_contiguous() && t.dim() == 3 && t.size(0) == B && t.size(1) == Hkv && t.size(2) == (C + LSP_Q8_BLOCK - 1) / LSP_Q8_BLOCK;
+}
+// Descriptor of suffix buffers and caches in 8 bits.
+bool q8_desc(const at::Tensor &ks, const at::Tensor &vs, const at::Tensor &kc, const at::Tensor &vc, const at::Tensor &ke, const at::Tensor &ve,
+             lsp_attn_desc &d) {
+  if (ks.dim() != 4 || kc.dim() != 4 || !element_type(ks, d.dtype)) return false;
+  const int64_t B = ks.size(0), S = ks.size(1), Hkv = ks.size(2), D = ks.size(3), C = kc.size(1);
+  if (vs.scalar_type() != ks.scalar_type() || kc.scalar_type() != at::kFloat8_e4m3fn || vc.scalar_type() != at::kFloat8_e4m3fn) return false;
+  if (vs.sizes() != ks.sizes() || !shape4(kc, B, C, Hkv, D) || vc.sizes() != kc.sizes() || !same_strides(ks, vs) || !same_strides(kc, vc)) return false;
+  d.B = int32_t(B); d.S = int32_t(S); d.Hq = d.Hkv = int32_t(Hkv); d.D = int32_t(D); d.C = int32_t(C);
+  return strides3(ks, d.kv_suf_stride) && strides3(kc, d.cache_stride) && q8_scales(ke, B, Hkv, C) && q8_scales(ve, B, Hkv, C);
+}
+bool q8_queries(const at::Tensor &q, const at::Tensor &out, const at::Tensor &ks, lsp_attn_desc &d) {
+  if (q.dim() != 4 || q.scalar_type() != ks.scalar_type() || out.scalar_type() != ks.scalar_type() || out.sizes() != q.sizes() || q.size(0) != d.B ||
+      q.size(1) != d.S || q.size(3) != d.D)
+    return false;
+  d.Hq = int32_t(q.size(2));
+  return strides3(q, d.q_stride) && own_strides3(out, d.o_stride);
+}
+// a list of N lists of addresses (bytes) of `layers` each
+template <int N>
+bool address_lists(PyObject *list, const void *const *(&at)[N], long layers) {
+  if (!PyList_Check(list) || PyList_GET_SIZE(list) != N) return false;
+  for (int k = 0; k < N; ++k) {
+    PyObject *b = PyList_GET_ITEM(list, k);
+    if (!PyBytes_Check(b) || PyBytes_GET_SIZE(b) != layers * Py_ssize_t(sizeof(void *))) return false;
+    at[k] = reinterpret_cast<const void *const *>(PyBytes_AS_STRING(b));
+  }
+  return true;
+}
+bool q8_table_of(PyObject *desc, PyObject *layers, PyObject *arrays, lsp_attn_desc &d, long &n, const void *const *(&at)[8]) {
+  if (!PyBytes_Check(desc) || PyBytes_GET_SIZE(desc) != Py_ssize_t(sizeof d) || !integer(layers, n) || n <= 0 || !address_lists(arrays, at, n)) return false;
+  memcpy(&d, PyBytes_AS_STRING(desc), sizeof d);
+  return true;
+}
+void *const *writable(const void *const *p) { return (void *const *)p; }
+
+// (k_suf, v_suf, k_cache, v_cache, k_scale, v_scale[, q, out]) -> (descriptor, eight lists of addresses), all bytes; the lists of q and out are those of
+// k_suf where they are not given
+PyObject *q8_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  const bool queries = n == 8;
+  ARGUMENTS((queries ? 8 : 6));
+  lsp_attn_desc d = {};
+  PyObject *lists[8];
+  Lists<2> suf, cache, scale, qo;
+  ORDINARY(suf.of(a) && cache.of(a + 2) && scale.of(a + 4) && (!queries || qo.of(a + 6)));
+  const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+  ORDINARY(PyList_GET_SIZE(a[2]) == count && PyList_GET_SIZE(a[4]) == count && (!queries || PyList_GET_SIZE(a[6]) == count));
+  ORDINARY(cache.first[0]->device() == suf.first[0]->device() && scale.first[0]->device() == suf.first[0]->device() &&
+           (!queries || qo.first[0]->device() == suf.first[0]->device()));
+  ORDINARY(q8_desc(*suf.first[0], *suf.first[1], *cache.first[0], *cache.first[1], *scale.first[0], *scale.first[1], d));
+  ORDINARY(!queries || q8_queries(*qo.first[0], *qo.first[1], *suf.first[0], d));
+  for (int k = 0; k < 2; ++k) {
+    lists[k] = suf.bytes[k]->o;
+    lists[2 + k] = cache.bytes[k]->o;
+    lists[4 + k] = scale.bytes[k]->o;
+    lists[6 + k] = queries ? qo.bytes[k]->o : suf.bytes[k]->o;
+  }
+  return Py_BuildValue("(y#[OOOOOOOO])", reinterpret_cast<const char *>(&d), Py_ssize_t(sizeof(d)), lists[0], lists[1], lists[2], lists[3], lists[4], lists[5],
+                       lists[6], lists[7]);
+}
+// (descriptor, layers, lists, commit_len, prefix_len)
+PyObject *kv_append_q8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(5);
+  lsp_attn_desc d;
+  long layers;
+  const void *const *t[8];
+  ORDINARY(q8_table_of(a[0], a[1], a[2], d, layers, t));
+  const at::Tensor *cl = dense(a[3], at::kInt, {d.B}), *pl = dense(a[4], at::kInt, {d.B});
+  ORDINARY(cl && pl && (d.B == 1 || d.cache_stride[0] != 0));
+  return status(g.kv_append_q8, &d, int32_t(layers), t[0], t[1], writable(t[2]), writable(t[3]), writable(t[4]), writable(t[5]), data<int32_t>(cl),
+                data<int32_t>(pl), stream());
+}
+// (descriptor, layers, lists, first_row, end_row, k_out, v_out)
+PyObject *kv_read_q8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(7);
+  lsp_attn_desc d;
+  long layers;
+  const void *const *t[8];
+  Lists<2> out;
+  ORDINARY(q8_table_of(a[0], a[1], a[2], d, layers, t) && out.of(a + 5) && PyList_GET_SIZE(a[5]) == layers);
+  const at::Tensor *first = dense(a[3], at::kInt, {d.B}), *end = dense(a[4], at::kInt, {d.B}), &k = *out.first[0], &v = *out.first[1];
+  ORDINARY(first && end && k.device() == first->device() && k.dim() == 4 && v.sizes() == k.sizes() && same_strides(k, v) && v.scalar_type() == k.scalar_type() &&
+           shape4(k, d.B, k.size(1), d.Hkv, d.D) && element_type(k, d.dtype) && own_strides3(k, d.kv_suf_stride));
+  d.S = int32_t(k.size(1));
+  auto at = [&](int i) { return reinterpret_cast<void *const *>(PyBytes_AS_STRING(out.bytes[i]->o)); };
+  return status(g.kv_read_q8, &d, int32_t(layers), t[2], t[3], t[4], t[5], data<int32_t>(first), data<int32_t>(end), at(0), at(1), stream());
+}
+PyObject *q8_step(lsp_attn_desc &d, long layers, const void *const *(&t)[8], PyObject *prefix_len, PyObject *suffix_len, PyObject *scale, PyObject *workspace) {
+  const at::Tensor *pl = dense(prefix_len, at::kInt, {d.B}), *sl = dense(suffix_len, at::kInt, {d.B});
+  ORDINARY(pl && sl && number(scale, d.scale));
+  const Workspace work(g.attn_q8_workspace_bytes(&d, int32_t(layers)), local_tensor(workspace));
+  return status(g.attn_step_q8_layers, &d, int32_t(layers), t[6], t[0], t[1], t[2], t[3], t[4], t[5], data<int32_t>(pl), data<int32_t>(sl), writable(t[7]),
+                work.at, work.bytes, stream());
+}
+// (q, k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, prefix_len, suffix_len, scale, out, workspace)
+PyObject *attn_step_q8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(12);
+  const at::Tensor *q = local_tensor(a[0]), *ks = local_tensor(a[1]), *vs = local_tensor(a[2]), *kc = local_tensor(a[3]), *vc = local_tensor(a[4]),
+                   *ke = local_tensor(a[5]), *ve = local_tensor(a[6]), *out = local_tensor(a[10]);
+  lsp_attn_desc d = {};
+  ORDINARY(q && ks && vs && kc && vc && ke && ve && out && q8_desc(*ks, *vs, *kc, *vc, *ke, *ve, d) && q8_queries(*q, *out, *ks, d));
+  const void *p[8] = {ks->const_data_ptr(), vs->const_data_ptr(), kc->const_data_ptr(), vc->const_data_ptr(), ke->const_data_ptr(), ve->const_data_ptr(),
+                      q->const_data_ptr(), out->mutable_data_ptr()};
+  const void *const *t[8] = {&p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7]};
+  return q8_step(d, 1, t, a[7], a[8], a[9], a[11]);
+}
+// (descriptor, layers, lists, prefix_len, suffix_len, scale, workspace)
+PyObject *attn_step_q8_layers(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(7);
+  lsp_attn_desc d;
+  long layers;
+  const void *const *t[8];
+  ORDINARY(q8_table_of(a[0], a[1], a[2], d, layers, t) && t[6] != t[0]);
+  return q8_step(d, layers, t, a[3], a[4], a[5], a[6]);
+}
+
+// (q, k, inv_freq, q_weight, k_weight, eps, prefix_len, suffix_len, positions, interleaved, q_out, k_out); any of the weights, lengths and positions None
+PyObject *qk_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  ARGUMENTS(12);
+  const at::Tensor *q = local_tensor(a[0]), *k = local_tensor(a[1]), *qo = local_tensor(a[10]), *ko = local_tensor(a[11]), *f = local_tensor(a[2]);
+  lsp_qk_norm_rope_desc d = {};
+  ORDINARY(q && k && qo && ko && f && q->dim() == 4 && k->dim() == 4 && element_type(*q, d.dtype));
+  const int64_t B = q->size(0), S = q->size(1), D = q->size(3);
+  ORDINARY(k->scalar_type() == q->scalar_type() && qo->scalar_type() == q->scalar_type() && ko->scalar_type() == q->scalar_type() &&
+           shape4(*k, B, S, k->size(2), D) && qo->sizes() == q->sizes() && ko->sizes() == k->sizes());
+  ORDINARY(own_strides3(*q, d.q_stride) && own_strides3(*k, d.k_stride) && own_strides3(*qo, d.q_out_stride) && own_strides3(*ko, d.k_out_stride));
+  ORDINARY(f->scalar_type() == at::kFloat && f->dim() == 1 && f->is_contiguous() && f->size(0) <= D / 2);
+  const at::Tensor *x[5];
+  const int place[5] = {3, 4, 6, 7, 8};
+  for (int i = 0; i < 5; ++i) {
+    PyObject *o = a[place[i]];
+    x[i] = o == Py_None ? nullptr : i < 2 ? dense(o, at::kFloat, {D}) : i < 4 ? dense(o, at::kInt, {B}) : dense(o, at::kInt, {B, S});
+    ORDINARY(x[i] || o == Py_None);
+  }
+  const int pairs = PyObject_IsTrue(a[9]);
+  if (pairs < 0) PyErr_Clear();
+  ORDINARY(pairs >= 0 && number(a[5], d.eps));
+  d.B = int32_t(B); d.S = int32_t(S); d.Hq = int32_t(q->size(2)); d.Hkv = int32_t(k->size(2)); d.D = int32_t(D); d.R = int32_t(2 * f->size(0));
+  d.interleaved = pairs;
+  return status(g.qk_norm_rope, &d, q->const_data_ptr(), k->const_data_ptr(), data<const float>(x[0]), data<const float>(x[1]), data<const float>(f),
+                data<const int32_t>(x[2]), data<const int32_t>(x[3]), data<const int32_t>(x[4]), data<void>(qo), data<void>(ko), stream());
+}
+
 // No C++ exception may reach the interpreter: torch throws where a tensor has no strides or no
 // storage (sparse, batched by vmap), there is no device or a subclass written in Python raises (the error is then
 // set as well), and the general path meets the same and raises it.
@@ -673,7 +833,8 @@ PyMethodDef methods[] = {fast<bind>("bind"), fast<attn_step>("attn_step"), fast<
                          fast<poll_start>("poll_start"), fast<poll_wait>("poll_wait"), fast<addresses>("addresses"),
                          fast<token_scores>("token_scores"), fast<attn_key_weights>("attn_key_weights"),
                          fast<attn_key_weights_layers>("attn_key_weights_layers"), fast<kv_evict>("kv_evict"), fast<attn_table>("attn_table"),
-                         fast<layer_table>("layer_table"), {nullptr, nullptr, 0, nullptr}};
+                         fast<layer_table>("layer_table"), fast<q8_table>("q8_table"), fast<kv_append_q8>("kv_append_q8"), fast<kv_read_q8>("kv_read_q8"),
+                         fast<attn_step_q8>("attn_step_q8"), fast<attn_step_q8_layers>("attn_step_q8_layers"), fast<qk_norm_rope>("qk_norm_rope"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
