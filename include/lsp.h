@@ -589,7 +589,8 @@ int32_t lsp_kv_read_q8(const lsp_attn_desc *desc, int32_t num_layers, const void
  * workspace: device, 16-byte aligned, lsp_attn_q8_workspace_bytes(desc, num_layers) bytes of any content,
  * for this call alone until it has run; with it the keys of few rows are divided between workgroups, without
  * (NULL, or fewer bytes) a tile's keys are one workgroup's.
- * Limits: those of lsp_attn_step; C, S <= 2^30, B * Hkv < 2^26, S * Hq / Hkv <= 2^30.
+ * Limits: those of lsp_attn_step; C, S <= 2^30, B * Hkv < 2^23, B * S * Hq and S * Hq / Hkv < 2^30; a row stride of K and V of
+ * at least D.
  */
 size_t lsp_attn_q8_workspace_bytes(const lsp_attn_desc *desc, int32_t num_layers);
 int32_t lsp_attn_step_q8(const lsp_attn_desc *desc, const void *q, const void *k_suf, const void *v_suf,

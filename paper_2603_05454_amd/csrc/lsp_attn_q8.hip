@@ -14,17 +14,28 @@
 namespace lsp {
 namespace {
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWaves = 8;
-constexpr int kThreads = kWaves * kWave;
-constexpr float kLag = 8.f;  // octaves that a maximum may exceed the reference by before that moves
+constexpr float kLag = 8.f;      // octaves that a maximum may exceed the reference by before that moves
+constexpr int kStep = 64;        // keys of a step: of the cache or of the suffix
+constexpr int kShort = 64;       // entries of a unit up to which its tiles are short ones
+constexpr int kTall = 128;       // entries of a tall tile
+constexpr int kXcds = 8;
+constexpr int kSlots = 2048;     // parts of 32 entries in the workspace
+constexpr int kPartKeys = 1024;  // C + S beyond which keys are divided at all
+constexpr int kLeast = 4;        // steps of a part, at least
 
 struct Q8AttnArgs {
   const int32_t *prefix_len, *suffix_len;
-  int32_t B, S, Hkv, C, rep, blocks, units, tiles;
-  float c;  // scale log2(e)
-  Div by_tiles, by_heads, by_units, by_rep;
+  int32_t B, S, Hkv, C, rep, blocks, per_seq;  // per_seq: units of a sequence, layers * Hkv
+  int32_t pieces, per_xcd;                     // each unit's items are dealt out to `pieces` lists, of which every XCD has per_xcd of a sequence
+  int32_t groups;                              // workgroups
+  float c;                                     // scale log2(e)
+  Div by_heads, by_rep;
   int64_t qs[3], ks[3], cs[3], os[3];  // bytes: sequence, row, head
+  float *parts;
 };
 
 __device__ __forceinline__ uint32_t word(bf16x2 x) { return __builtin_bit_cast(uint32_t, x); }
@@ -33,99 +44,244 @@ __device__ __forceinline__ bf16x8 fragment(uint32_t a, uint32_t b, uint32_t c, u
 __device__ __forceinline__ uint32_t low(uint32_t w, float s) { return word(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false)); }
 __device__ __forceinline__ uint32_t high(uint32_t w, float s) { return word(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)); }
 __device__ __forceinline__ uint32_t pick(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
+// bytes j of four words, in order
+__device__ __forceinline__ void turn_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&t)[4]) {
+  const uint32_t ab = pick(b, a, 0x05010400), cd = pick(d, c, 0x05010400), ab2 = pick(b, a, 0x07030602), cd2 = pick(d, c, 0x07030602);
+  t[0] = pick(cd, ab, 0x05040100);
+  t[1] = pick(cd, ab, 0x07060302);
+  t[2] = pick(cd2, ab2, 0x05040100);
+  t[3] = pick(cd2, ab2, 0x07060302);
+}
 
-__device__ __forceinline__ float across(float x, bool sum) {  // over the four lanes that have an entry
+// The rows of a block or step, as a buffer: what is read beyond the last one that there is comes as 0.
+struct Rows {
+  __amdgpu_buffer_rsrc_t at;
+  int row;
+  __device__ __forceinline__ Rows(const char *base, int64_t stride, int first, int valid, int bytes)
+      : at(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + first * stride), 0,
+                                             __builtin_amdgcn_readfirstlane(max(valid - 1, 0) * int(stride) + bytes), 0x00020000)),
+        row(int(stride)) {}
+};
+// 16, 8 or 4 bytes, `rows` (the same for all lanes) behind byte v.  FULL: all rows are there, and the distance is the instruction's scalar offset; how that counts
+// where a read is to be found out of range is not relied on, elsewhere it is added.
+template <bool FULL>
+__device__ __forceinline__ u32x4 load16(const Rows &r, int v, int rows) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r.at, FULL ? v : v + rows * r.row, FULL ? rows * r.row : 0, 0));
+}
+template <bool FULL>
+__device__ __forceinline__ u32x2 load8(const Rows &r, int v, int rows) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r.at, FULL ? v : v + rows * r.row, FULL ? rows * r.row : 0, 0));
+}
+template <bool FULL>
+__device__ __forceinline__ uint32_t load4(const Rows &r, int v, int rows) {
+  return __builtin_amdgcn_raw_buffer_load_b32(r.at, FULL ? v : v + rows * r.row, FULL ? rows * r.row : 0, 0);
+}
+// The compiler takes what is made of x for new every time: it is not kept in registers from one step to the next.
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+__device__ __forceinline__ float quad_max(float x) {  // over the lanes l % 16
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// ---- what there is to do ---------------------------------------------------------------
+struct Lens {
+  int N, P;
+};
+struct Shape {  // of a sequence's units
+  int entries, rows, tiles, steps, cached;  // rows: entries of a tile; steps: of all keys, `cached` of them of the cache
+};
+__device__ __forceinline__ Shape shape_of(const Q8AttnArgs &a, Lens n) {
+  Shape s;
+  s.entries = n.N * a.rep;
+  s.rows = s.entries > kShort ? kTall : s.entries > 16 ? 32 : 16;
+  s.tiles = (s.entries + s.rows - 1) / s.rows;
+  s.cached = (n.P + kStep - 1) / kStep;
+  s.steps = s.cached + (n.N + kStep - 1) / kStep;
+  return s;
+}
+__device__ __forceinline__ Lens lens_of(const Q8AttnArgs &a, int b) {
+  if (b >= a.B) return {0, 0};
+  return {min(max(a.suffix_len[b], 0), a.S), min(max(a.prefix_len[b], 0), a.C)};
+}
+__device__ __forceinline__ int first_lane(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
-  for (int m = 16; m < 64; m <<= 1) {
-    const float y = __shfl_xor(x, m);
-    x = sum ? x + y : fmaxf(x, y);
+  for (int m = 1; m < kWave; m <<= 1) x += __shfl_xor(x, m);
+  return first_lane(x);
+}
+__device__ __forceinline__ int running_sum(int x, int lane) {
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) {
+    const int y = __shfl_up(x, m);
+    x += lane >= m ? y : 0;
   }
   return x;
 }
 
+// The sequences, 64 at a time, a lane each.
+struct Plan {
+  int chunk;          // steps of an item, at most
+  bool split;         // whether some tile is more than one item
+  int b0;             // the first of the sequences that the lanes have
+  Lens n;
+  int end, base;      // running sum of the items of an XCD, those of sequences before b0
+  int slot_end, slot_base;  // the same of the parts of 32 entries
+
+  __device__ __forceinline__ int splits_of(const Shape &s) const { return split ? (s.steps + chunk - 1) / chunk : 1; }  // of a tile
+  __device__ __forceinline__ void take(const Q8AttnArgs &a, int lane) {
+    n = lens_of(a, b0 + lane);
+    const Shape s = shape_of(a, n);
+    const int items = s.tiles * splits_of(s);
+    end = running_sum(a.per_xcd * ((items + a.pieces - 1) / a.pieces), lane);
+    slot_end = split ? running_sum(a.per_seq * items * ((s.rows + 31) / 32), lane) : 0;
+  }
+  // How long the items are: all keys of a tile, or, where workgroups would be without one, part of them.  Lane i looks at i + 1 parts (from 32 on at
+  // multiples of 8).  A round of items takes its steps and about four steps' time to begin and end, joining the parts as much again.
+  __device__ __forceinline__ void start(const Q8AttnArgs &a, int lane) {
+    chunk = 1 << 30;
+    split = false;
+    if (a.parts != nullptr) {
+      int tiles = 0, slots = 0, most = 0;
+      for (int b = 0; b < a.B; b += kWave) {
+        const Shape x = shape_of(a, lens_of(a, b + lane));
+        tiles += a.per_seq * x.tiles;
+        slots += a.per_seq * x.tiles * ((x.rows + 31) / 32);
+        most = max(most, x.tiles > 0 ? x.steps : 0);
+      }
+      tiles = wave_sum(tiles);
+      slots = wave_sum(slots);
+#pragma unroll
+      for (int m = 1; m < kWave; m <<= 1) most = max(most, __shfl_xor(most, m));
+      if (tiles > 0 && slots <= kSlots / 2) {
+        const int k = lane < 32 ? lane + 1 : 32 + 8 * (lane - 31), part = (most + k - 1) / k;
+        const bool fits = k == 1 || (int64_t(slots) * k <= kSlots && part >= kLeast);
+        int cost = fits ? int((int64_t(tiles) * k + a.groups - 1) / a.groups) * (part + 4) + (k > 1 ? 4 + k / 8 : 0) : 1 << 29;
+        int best = lane;
+#pragma unroll
+        for (int m = 1; m < kWave; m <<= 1) {
+          const int c = __shfl_xor(cost, m), l = __shfl_xor(best, m);
+          if (c < cost || (c == cost && l < best)) cost = c, best = l;
+        }
+        best = first_lane(best);
+        if (best > 0) {
+          const int k2 = best < 32 ? best + 1 : 32 + 8 * (best - 31);
+          chunk = (first_lane(most) + k2 - 1) / k2;
+          split = true;
+        }
+      }
+    }
+    b0 = base = slot_base = 0;
+    take(a, lane);
+  }
+  // Brings the lanes to the sequence of item q of an XCD's list: its lane, or -1 behind the last item.
+  __device__ __forceinline__ int find(const Q8AttnArgs &a, int q, int lane) {
+    for (;;) {
+      const uint64_t behind = __ballot(q < base + end);
+      if (behind != 0) return __builtin_ctzll(behind);
+      base += __builtin_amdgcn_readlane(end, kWave - 1);
+      slot_base += __builtin_amdgcn_readlane(slot_end, kWave - 1);
+      b0 += kWave;
+      if (b0 >= a.B) return -1;
+      take(a, lane);
+    }
+  }
+};
+__device__ __forceinline__ int at_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
+
+struct Item {
+  int b, l, g, N, P, entries, entry, rows;
+  int from, to, cached;  // steps
+  int slot;              // of its part, or -1: the item is all of a tile
+};
+
+// Where a unit's rows are.
+struct Unit {
+  const char *q, *ks, *vs, *kc, *vc;
+  const uint8_t *ke, *ve;
+  char *out;
+  __device__ __forceinline__ Unit(const Q8AttnArgs &a, const Q8Layers &L, const Item &t) {
+    q = L.q[t.l] + t.b * a.qs[0] + t.g * a.rep * a.qs[2];
+    out = L.out[t.l] + t.b * a.os[0] + t.g * a.rep * a.os[2];
+    const int64_t c = t.b * a.cs[0] + t.g * a.cs[2], s = t.b * a.ks[0] + t.g * a.ks[2], e = (int64_t(t.b) * a.Hkv + t.g) * a.blocks;
+    kc = L.k_cache[t.l] + c; vc = L.v_cache[t.l] + c;
+    ks = L.k_suf[t.l] + s; vs = L.v_suf[t.l] + s;
+    ke = L.k_scale[t.l] + e; ve = L.v_scale[t.l] + e;
+  }
+};
+// entry e of a unit: its row and head
+__device__ __forceinline__ int64_t entry_at(const Q8AttnArgs &a, int e, const int64_t (&s)[3]) {
+  const int u = quotient(e, a.by_rep);
+  return u * s[1] + (e - u * a.rep) * s[2];
+}
+// part of 32 entries: their sums, then reference and sum of weights of each
+template <int D>
+__device__ __forceinline__ float *part_at(const Q8AttnArgs &a, int slot, int row) { return a.parts + (int64_t(slot) + (row >> 5)) * 32 * (D + 2) + (row & 31) * D; }
+template <int D>
+__device__ __forceinline__ float *part_stats(const Q8AttnArgs &a, int slot, int row) { return a.parts + (int64_t(slot) + (row >> 5)) * 32 * (D + 2) + 32 * D + 2 * (row & 31); }
+
+// ---- short tiles -----------------------------------------------------------------------
 // Lanes l % 16 = r, l / 16 = h.  Of the keys: rows 16 k + r of the block, elements 64 i + 16 h of 16; of the values: rows 16 k + 4 h + e, of which
 // VJ elements from VJ r on.
 template <int D>
 struct Keys {
   static constexpr int KI = D / 64, KC = D / 32, VJ = D / 16;
-  bf16x8 k[2][KC], v[VJ];
+  u32x4 kw[2][KI];
+  uint32_t w[8][VJ / 4];
 
   // row of the block that element e (of eight) of a lane's values is of
   static __device__ __forceinline__ int value_row(int h, int e) { return 16 * (e >> 2) + 4 * h + (e & 3); }
 
-  __device__ __forceinline__ void cached(const char *kp, const char *vp, int64_t row, int last, float ks, float vs, int r, int h) {
-    u32x4 kw[2][KI];
-    uint32_t w[8][VJ / 4];
+  // kv, vv: r * row + 16 h, 4 h * row + VJ r
+  template <bool FULL>
+  __device__ __forceinline__ void load(const Rows &k, const Rows &v, int kv, int vv) {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < KI; ++i) kw[b][i] = *reinterpret_cast<const u32x4 *>(kp + min(16 * b + r, last) * row + 64 * i + 16 * h);
+      for (int i = 0; i < KI; ++i) kw[b][i] = load16<FULL>(k, kv + 64 * i, 16 * b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const uint32_t *p = reinterpret_cast<const uint32_t *>(vp + min(value_row(h, e), last) * row + VJ * r);
-#pragma unroll
-      for (int j = 0; j < VJ / 4; ++j) w[e][j] = p[j];
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < KI; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          k[b][2 * i + j] = fragment(low(kw[b][i][2 * j], ks), high(kw[b][i][2 * j], ks), low(kw[b][i][2 * j + 1], ks), high(kw[b][i][2 * j + 1], ks));
-#pragma unroll
-    for (int q = 0; q < VJ / 4; ++q) {
-      uint32_t t[4][2];  // element j of keys 4 m to 4 m + 3
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const uint32_t a = w[4 * m][q], b = w[4 * m + 1][q], c = w[4 * m + 2][q], d = w[4 * m + 3][q];
-        const uint32_t ab = pick(b, a, 0x05010400), cd = pick(d, c, 0x05010400), ab2 = pick(b, a, 0x07030602), cd2 = pick(d, c, 0x07030602);
-        t[0][m] = pick(cd, ab, 0x05040100);
-        t[1][m] = pick(cd, ab, 0x07060302);
-        t[2][m] = pick(cd2, ab2, 0x05040100);
-        t[3][m] = pick(cd2, ab2, 0x07060302);
+      if constexpr (VJ == 8) {
+        const u32x2 x = load8<FULL>(v, vv, value_row(0, e));
+        w[e][0] = x[0], w[e][1] = x[1];
+      } else {
+        w[e][0] = load4<FULL>(v, vv, value_row(0, e));
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[4 * q + j] = fragment(low(t[j][0], vs), high(t[j][0], vs), low(t[j][1], vs), high(t[j][1], vs));
     }
   }
-
-  __device__ __forceinline__ void suffix(const char *kp, const char *vp, int64_t row, int last, int r, int h) {
+  __device__ __forceinline__ bf16x8 key(int b, int c, float s) const {
+    const u32x4 x = kw[b][c >> 1];
+    const int j = 2 * (c & 1);
+    return fragment(low(x[j], s), high(x[j], s), low(x[j + 1], s), high(x[j + 1], s));
+  }
+  __device__ __forceinline__ void turned(int q, bf16x8 (&v)[4], float s) const {  // elements 4 q to 4 q + 3 of the lane's
+    uint32_t t[2][4];  // element j of keys 4 m to 4 m + 3
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int m = 0; m < 2; ++m) turn_bytes(w[4 * m][q], w[4 * m + 1][q], w[4 * m + 2][q], w[4 * m + 3][q], t[m]);
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
-        k[b][c] = *reinterpret_cast<const bf16x8 *>(kp + min(16 * b + r, last) * row + 128 * (c >> 1) + 32 * h + 16 * (c & 1));
-    uint32_t w[8][VJ / 2];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t *p = reinterpret_cast<const uint32_t *>(vp + min(value_row(h, e), last) * row + 2 * VJ * r);
-#pragma unroll
-      for (int j = 0; j < VJ / 2; ++j) w[e][j] = p[j];
-    }
-#pragma unroll
-    for (int j = 0; j < VJ; ++j) {
-      uint32_t t[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) t[m] = pick(w[2 * m + 1][j >> 1], w[2 * m][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
-      v[j] = fragment(t[0], t[1], t[2], t[3]);
-    }
+    for (int j = 0; j < 4; ++j) v[j] = fragment(low(t[0][j], s), high(t[0][j], s), low(t[1][j], s), high(t[1][j], s));
   }
 };
 
 // NB tiles of 16 entries
 template <int D, int NB>
-struct Rows {
+struct Short {
   static constexpr int KC = D / 32, VJ = D / 16;
   bf16x8 q[NB][KC];
-  f32x4 o[NB][VJ];   // o[n][j][i]: element 4 VJ h + VJ i + j of entry r
+  f32x4 o[NB][VJ];     // o[n][j][i]: element 4 VJ h + VJ i + j of entry r
   float m[NB], l[NB];  // reference (base 2, scaled), this lane's part of the sum
 
   __device__ __forceinline__ void start(const Q8AttnArgs &a, const char *q0, int entry, int entries, int r, int h) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      const int e = min(entry + 16 * n + r, entries - 1), u = quotient(e, a.by_rep);
-      const char *p = q0 + u * a.qs[1] + (e - u * a.rep) * a.qs[2];
+      const char *p = q0 + entry_at(a, min(entry + 16 * n + r, entries - 1), a.qs);
 #pragma unroll
       for (int c = 0; c < KC; ++c) q[n][c] = *reinterpret_cast<const bf16x8 *>(p + 128 * (c >> 1) + 32 * h + 16 * (c & 1));
 #pragma unroll
@@ -134,149 +290,566 @@ struct Rows {
       l[n] = 0.f;
     }
   }
-
-  // valid: keys of the block that there are
-  __device__ __forceinline__ void meet(const Keys<D> &x, float c, int valid, int h) {
+  // scores of entries n -> probabilities; valid: keys of the block that there are
+  __device__ __forceinline__ bf16x8 weigh(int n, f32x4 (&s)[2], float c, int valid, int h) {
+    if (valid < kQ8Block)
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int k = 0; k < KC; ++k)
+        for (int i = 0; i < 4; ++i) s[b][i] = 16 * b + 4 * h + i < valid ? s[b][i] : -INFINITY;
+    float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    most = quad_max(most) * c;
+    if (__any(most > m[n] + kLag)) {
+      const float to = fmaxf(m[n], most), f = to > m[n] ? __builtin_amdgcn_exp2f(m[n] - to) : 1.f;
+      m[n] = to;
+      l[n] *= f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[b][k], q[n][k], s[b], 0, 0, 0);
-      if (valid < kQ8Block)
+      for (int j = 0; j < VJ; ++j) o[n][j] *= f;
+    }
+    bf16x8 P;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+    for (int e = 0; e < 8; ++e) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], c, -m[n]));
+      l[n] += p;
+      P[e] = __bf16(p);
+    }
+    return P;
+  }
+  __device__ __forceinline__ void meet(const Keys<D> &x, float ks, float vs, float c, int valid, int h) {
+    f32x4 s[NB][2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[b][i] = 16 * b + 4 * h + i < valid ? s[b][i] : -INFINITY;
-      float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-      most = across(most, false) * c;
-      if (__any(most > m[n] + kLag)) {
-        const float to = fmaxf(m[n], most), f = to > m[n] ? __builtin_amdgcn_exp2f(m[n] - to) : 1.f;
-        m[n] = to;
-        l[n] *= f;
+    for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < VJ; ++j) o[n][j] *= f;
+    for (int k = 0; k < KC; ++k)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const bf16x8 f = x.key(b, k, ks);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[n][k], s[n][b], 0, 0, 0);
       }
-      float p[8];
+    bf16x8 P[NB];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], c, -m[n]));
-        l[n] += p[e];
+    for (int n = 0; n < NB; ++n) P[n] = weigh(n, s[n], c, valid, h);
+#pragma unroll
+    for (int p = 0; p < VJ / 4; ++p) {
+      bf16x8 v[4];
+      x.turned(p, v, vs);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n][4 * p + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j], P[n], o[n][4 * p + j], 0, 0, 0);
+    }
+  }
+  // 32 rows of the suffix
+  __device__ __forceinline__ void meet_suffix(const Rows &kr, const Rows &vr, float c, int valid, int r, int h) {
+    const int kv = anew(r * kr.row + 32 * h), vv = anew(4 * h * vr.row + 2 * VJ * r);
+    f32x4 s[NB][2];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        const bf16x8 f = __builtin_bit_cast(bf16x8, load16<false>(kr, kv + 128 * (k >> 1) + 16 * (k & 1), 16 * b));
+#pragma unroll
+        for (int n = 0; n < NB; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[n][k], s[n][b], 0, 0, 0);
       }
-      bf16x8 P;
+    uint32_t w[8][VJ / 2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) P[e] = __bf16(p[e]);
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (VJ == 8) {
+        const u32x4 x = load16<false>(vr, vv, Keys<D>::value_row(0, e));
 #pragma unroll
-      for (int j = 0; j < VJ; ++j) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v[j], P, o[n][j], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) w[e][j] = x[j];
+      } else {
+        const u32x2 x = load8<false>(vr, vv, Keys<D>::value_row(0, e));
+        w[e][0] = x[0], w[e][1] = x[1];
+      }
+    }
+    bf16x8 P[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) P[n] = weigh(n, s[n], c, valid, h);
+#pragma unroll
+    for (int j = 0; j < VJ; ++j) {
+      uint32_t t[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) t[m] = pick(w[2 * m + 1][j >> 1], w[2 * m][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
+      const bf16x8 v = fragment(t[0], t[1], t[2], t[3]);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[n], o[n][j], 0, 0, 0);
     }
   }
 };
 
-template <int D, int NB>
-__global__ __launch_bounds__(kThreads) void attn_q8_kernel(Q8AttnArgs a, Q8Layers L) {
-  constexpr int VJ = D / 16;
-  __shared__ f32x4 s_o[kWaves][VJ][kWave];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  const int id = workgroup_id(), lane = threadIdx.x & (kWave - 1), r = lane & 15, h = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  // the tiles of a unit on one XCD
-  const int m8 = id >> 3, turn = quotient(m8, a.by_tiles), tile = m8 - turn * a.tiles, unit = turn * 8 + (id & 7);
-  if (unit >= a.units) return;
-  const int per_layer = a.B * a.Hkv, layer = quotient(unit, a.by_units), in_layer = unit - layer * per_layer;
-  const int b = quotient(in_layer, a.by_heads), g = in_layer - b * a.Hkv;
-  const int N = min(max(a.suffix_len[b], 0), a.S), P = min(max(a.prefix_len[b], 0), a.C);
-  const int entries = N * a.rep, entry = tile * 16 * NB;
-  if (entry >= entries) return;
+// LDS of a workgroup.  Short tiles: what its waves join.  Tall ones: two steps' keys [64][D] and values [D][64], bf16.
+template <int D, int WAVES>
+struct Joined {
+  f32x4 o[WAVES][D / 16][kWave];
+  float m[WAVES][16], l[WAVES][16];
+};
+template <int D>
+struct Staged {
+  uint32_t k[2][kStep * D / 2], v[2][kStep * D / 2];
+};
 
-  Rows<D, NB> rows;
-  rows.start(a, L.q[layer] + b * a.qs[0] + g * a.rep * a.qs[2], entry, entries, r, h);
-  const char *kc = L.k_cache[layer] + b * a.cs[0] + g * a.cs[2], *vc = L.v_cache[layer] + b * a.cs[0] + g * a.cs[2];
-  const char *ks = L.k_suf[layer] + b * a.ks[0] + g * a.ks[2], *vs = L.v_suf[layer] + b * a.ks[0] + g * a.ks[2];
-  const int64_t scales = (int64_t(b) * a.Hkv + g) * a.blocks;
-  const uint8_t *ke = L.k_scale[layer] + scales, *ve = L.v_scale[layer] + scales;
-  const int cached = (P + kQ8Block - 1) / kQ8Block, all = cached + (N + kQ8Block - 1) / kQ8Block;
-  for (int s = wave; s < all; s += kWaves) {
-    Keys<D> x;
-    int valid;
-    if (s < cached) {
-      valid = P - s * kQ8Block;
-      const int64_t at = int64_t(s) * kQ8Block * a.cs[1];
-      x.cached(kc + at, vc + at, a.cs[1], valid - 1, q8_scale(ke[s]), q8_scale(ve[s]), r, h);
-    } else {
-      const int t = s - cached;
-      valid = N - t * kQ8Block;
-      const int64_t at = int64_t(t) * kQ8Block * a.ks[1];
-      x.suffix(ks + at, vs + at, a.ks[1], valid - 1, r, h);
+template <int D, int NB, int WAVES>
+__device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Joined<D, WAVES> &s, int lane, int wave) {
+  constexpr int VJ = D / 16;
+  const int r = lane & 15, h = lane >> 4;
+  Short<D, NB> x;
+  x.start(a, u.q, t.entry, t.entries, r, h);
+  // blocks of 32 keys: of the cache, the waves taking turns, the next one on its way while one is met
+  const int row = int(a.cs[1]), kv = r * row + 16 * h, vv = 4 * h * row + VJ * r;
+  const int c_end = min(2 * min(t.to, t.cached), (t.P + kQ8Block - 1) / kQ8Block);
+  int j = 2 * t.from + wave;
+  if (j < c_end) {
+    Keys<D> next;
+    auto load = [&](int j) {
+      const int valid = min(t.P - j * kQ8Block, kQ8Block);
+      const Rows k(u.kc, a.cs[1], j * kQ8Block, valid, D), v(u.vc, a.cs[1], j * kQ8Block, valid, D);
+      if (valid == kQ8Block) next.template load<true>(k, v, kv, vv);
+      else next.template load<false>(k, v, anew(kv), anew(vv));
+    };
+    load(j);
+    float ks = q8_scale(u.ke[j]), vs = q8_scale(u.ve[j]);
+    for (; j < c_end; j += WAVES) {
+      const Keys<D> now = next;
+      const float ks0 = ks, vs0 = vs;
+      if (j + WAVES < c_end) {
+        load(j + WAVES);
+        ks = q8_scale(u.ke[j + WAVES]), vs = q8_scale(u.ve[j + WAVES]);
+      }
+      x.meet(now, ks0, vs0, a.c, t.P - j * kQ8Block, h);
     }
-    rows.meet(x, a.c, valid, h);
+  }
+  // of the suffix
+  const int s_end = min(2 * (t.to - t.cached), (t.N + kQ8Block - 1) / kQ8Block);
+  for (int i = 2 * max(t.from - t.cached, 0) + (WAVES - 1 - wave); i < s_end; i += WAVES) {
+    const int valid = t.N - i * kQ8Block;
+    x.meet_suffix(Rows(u.ks, a.ks[1], i * kQ8Block, min(valid, kQ8Block), 2 * D), Rows(u.vs, a.ks[1], i * kQ8Block, min(valid, kQ8Block), 2 * D), a.c, valid,
+                  r, h);
   }
 
-  // the waves' parts, joined in LDS: wave w adds what all have in place w of their lanes
-  char *out = L.out[layer] + b * a.os[0] + g * a.rep * a.os[2];
+  // The waves' parts: what all have in a place of their lanes is added by one of them.
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const float l = across(rows.l[n], true);
+    const float l = quad_sum(x.l[n]);
     if (n > 0) __syncthreads();
-    if (h == 0) s_m[wave][r] = rows.m[n], s_l[wave][r] = l;
+    if (h == 0) s.m[wave][r] = x.m[n], s.l[wave][r] = l;
     __syncthreads();
     float m = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_m[w][r]);
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s.m[w][r]);
+    // (a wave that met no key has zeros)
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += s_l[w][r] > 0.f || s_l[w][r] != s_l[w][r] ? s_l[w][r] * __builtin_amdgcn_exp2f(s_m[w][r] - m) : 0.f;
-    const float f = l > 0.f ? __builtin_amdgcn_exp2f(rows.m[n] - m) : l;  // (a wave that met no key has zeros)
+    for (int w = 0; w < WAVES; ++w) sum += s.l[w][r] != 0.f ? s.l[w][r] * __builtin_amdgcn_exp2f(s.m[w][r] - m) : 0.f;
+    const float f = l != 0.f ? __builtin_amdgcn_exp2f(x.m[n] - m) : 0.f;
 #pragma unroll
     for (int p = 0; p < VJ; ++p) {  // elements 4 p to 4 p + 3 of the lane's 4 VJ
-      f32x4 x;
+      f32x4 y;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = f * rows.o[n][(4 * p + j) % VJ][(4 * p + j) / VJ];
-      s_o[wave][p][lane] = x;
+      for (int j = 0; j < 4; ++j) y[j] = f * x.o[n][(4 * p + j) % VJ][(4 * p + j) / VJ];
+      s.o[wave][p][lane] = y;
     }
     __syncthreads();
-    if (wave < VJ) {
-      f32x4 x = s_o[0][wave][lane];
+    const int e = 16 * n + r;
+    if (t.entry + e < t.entries) {
+      for (int p = wave; p < VJ; p += WAVES) {
+        f32x4 y = s.o[0][p][lane];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) x += s_o[w][wave][lane];
-      const int e = entry + 16 * n + r;
-      if (e < entries) {
-        const int u = quotient(e, a.by_rep);
-        const float inv = 1.f / sum;
-        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<bf16x4 *>(out + u * a.os[1] + (e - u * a.rep) * a.os[2] + 2 * (4 * VJ * h + 4 * wave)) =
-            bf16x4{__bf16(x[0] * inv), __bf16(x[1] * inv), __bf16(x[2] * inv), __bf16(x[3] * inv)};
+        for (int w = 1; w < WAVES; ++w) y += s.o[w][p][lane];
+        const int d = 4 * VJ * h + 4 * p;
+        if (t.slot < 0) {
+          const float inv = 1.f / sum;
+          *reinterpret_cast<bf16x4 *>(u.out + entry_at(a, t.entry + e, a.os) + 2 * d) =
+              bf16x4{__bf16(y[0] * inv), __bf16(y[1] * inv), __bf16(y[2] * inv), __bf16(y[3] * inv)};
+        } else {
+          *reinterpret_cast<f32x4 *>(part_at<D>(a, t.slot, e) + d) = y;
+          if (p == 0 && h == 0) *reinterpret_cast<f32x2 *>(part_stats<D>(a, t.slot, e)) = f32x2{m, sum};
+        }
       }
     }
   }
 }
 
-int32_t launch(const Q8AttnArgs &args, int D, const Q8Layers &L, int layers, hipStream_t st) {
-  Q8AttnArgs a = args;
-  a.units = layers * a.B * a.Hkv;
-  const int NB = int64_t(a.rep) * a.S > 16 ? 2 : 1;
-  const int64_t tiles = (int64_t(a.rep) * a.S + 16 * NB - 1) / (16 * NB), nwg = (int64_t(a.units) + 7) / 8 * 8 * tiles;
-  LSP_CHECK_ARG(nwg < kMaxGrid, "lsp_attn_step_q8: too many rows for one launch");
-  a.tiles = int32_t(tiles);
-  a.by_tiles = div_by(tiles);
-  a.by_heads = div_by(a.Hkv);
-  a.by_units = div_by(int64_t(a.B) * a.Hkv);
-  a.by_rep = div_by(a.rep);
-  const dim3 grid = grid_of(nwg);
-  if (D == 64) {
-    if (NB == 1) attn_q8_kernel<64, 1><<<grid, kThreads, 0, st>>>(a, L);
-    else attn_q8_kernel<64, 2><<<grid, kThreads, 0, st>>>(a, L);
-  } else {
-    if (NB == 1) attn_q8_kernel<128, 1><<<grid, kThreads, 0, st>>>(a, L);
-    else attn_q8_kernel<128, 2><<<grid, kThreads, 0, st>>>(a, L);
+// ---- tall tiles ------------------------------------------------------------------------
+// Four waves of 32 entries each, which share steps of 64 keys in LDS, bf16 by then.  The scores of a wave are keys x entries (32x32x16): lane l has those
+// of entry l % 32 with keys 8 j + 4 h + i of 32, h = l / 32, and these are, eight at a time, the operand of the second product, whose other one is
+// V^T: eight keys' values of one element, 16 bytes.  So the values are turned as they are written to LDS: row d holds for each (32 keys, 16 of them,
+// h) the eight keys 8 x + 4 h + i in the order of x, i.
+// 16-byte pieces are exchanged against bank conflicts: piece p of a key's 256 bytes at p ^ (key % 16) (of 128: p ^ (key / 2 % 8)); piece p of
+// the 128 bytes of element d at p ^ ((d / 8 % 4 ^ d / 2) % 8), which serves both the writes, of every eighth d, and the reads, of neighbours.
+template <int D>
+struct Tall {
+  static constexpr int KC = D / 16, DB = D / 32, VB = D / 16;  // VB: elements of four keys' values that a thread turns
+  static constexpr int KR = D / 64, VR = D / 64 * 4;           // loads of 16 bytes of a step's keys in 8 bits; words of its values
+
+  // in words
+  static __device__ __forceinline__ int key_piece(int key, int p) {
+    return D == 128 ? key * 64 + 4 * (p ^ (key & 15)) : key * 32 + 4 * (p ^ (key >> 1 & 7));
   }
+  static __device__ __forceinline__ int value_piece(int d, int p) { return d * 32 + 4 * (p ^ (((d >> 3 & 3) ^ d >> 1) & 7)); }
+
+  uint32_t raw[4 * 4 * D / 64];  // what a thread has on its way: half of it keys, half values
+
+  // cached: keys tid / (D / 16) on, 16 bytes each; values of four keys, VB bytes each.  Suffix: twice the bytes.
+  template <bool FULL>
+  __device__ __forceinline__ void load_cached(const Rows &k, const Rows &v, int tid) {
+    const int kv = anew(tid / (D / 16) * k.row + tid % (D / 16) * 16), vv = anew(tid / 16 * 4 * v.row + tid % 16 * VB);
+#pragma unroll
+    for (int i = 0; i < KR; ++i) {
+      const u32x4 x = load16<FULL>(k, kv, 256 / (D / 16) * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) raw[4 * i + j] = x[j];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (VB == 8) {
+        const u32x2 x = load8<FULL>(v, vv, i);
+        raw[8 + 2 * i] = x[0], raw[8 + 2 * i + 1] = x[1];
+      } else {
+        raw[4 + i] = load4<FULL>(v, vv, i);
+      }
+    }
+  }
+  template <bool FULL>
+  __device__ __forceinline__ void load_suffix(const Rows &k, const Rows &v, int tid) {
+    const int kv = anew(tid / (D / 8) * k.row + tid % (D / 8) * 16), vv = anew(tid / 16 * 4 * v.row + tid % 16 * VB * 2);
+#pragma unroll
+    for (int i = 0; i < 2 * KR; ++i) {
+      const u32x4 x = load16<FULL>(k, kv, 256 / (D / 8) * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) raw[4 * i + j] = x[j];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (VB == 8) {
+        const u32x4 x = load16<FULL>(v, vv, i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) raw[16 + 4 * i + j] = x[j];
+      } else {
+        const u32x2 x = load8<FULL>(v, vv, i);
+        raw[8 + 2 * i] = x[0], raw[8 + 2 * i + 1] = x[1];
+      }
+    }
+  }
+  // Where element j of the thread's values of four keys goes: keys 4 f to 4 f + 3, f = tid / 16 = 8 kb + 4 t + 2 x + h, are half x of piece 4 kb + 2 t + h.
+  static __device__ __forceinline__ int value_base(int tid) {
+    const int f = tid / 16;
+    return value_piece(tid % 16 * VB, f >> 3 << 2 | (f >> 2 & 1) << 1 | (f & 1)) + 2 * (f >> 1 & 1);
+  }
+  static __device__ __forceinline__ int value_at(int base, int j) { return (base ^ 4 * (j >> 1)) + 32 * j; }
+
+  // ks, vs: scales of the step's two blocks of 32 keys
+  __device__ __forceinline__ void store_cached(uint32_t *k, uint32_t *v, const float (&ks)[2], const float (&vs)[2], int tid) {
+    const int key0 = tid / (D / 16), k0 = anew(key_piece(key0, tid % (D / 16) * 2)), v0 = anew(value_base(tid));
+#pragma unroll
+    for (int i = 0; i < KR; ++i) {
+      const float s = KR == 2 ? ks[i] : key0 < 32 ? ks[0] : ks[1];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        *reinterpret_cast<u32x4 *>(k + (k0 ^ 4 * j) + i * 32 * (D / 2)) =
+            u32x4{low(raw[4 * i + 2 * j], s), high(raw[4 * i + 2 * j], s), low(raw[4 * i + 2 * j + 1], s), high(raw[4 * i + 2 * j + 1], s)};
+    }
+    const float s = tid < 128 ? vs[0] : vs[1];
+#pragma unroll
+    for (int q = 0; q < VB / 4; ++q) {
+      uint32_t t[4];
+      constexpr int W = VB / 4, at = 4 * KR;
+      turn_bytes(raw[at + q], raw[at + W + q], raw[at + 2 * W + q], raw[at + 3 * W + q], t);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x2 *>(v + value_at(v0, 4 * q + j)) = u32x2{low(t[j], s), high(t[j], s)};
+    }
+  }
+  __device__ __forceinline__ void store_suffix(uint32_t *k, uint32_t *v, int tid) {
+    // (rows 16 (or 32) further on have the same exchange)
+    const int k0 = anew(key_piece(tid / (D / 8), tid % (D / 8))), v0 = anew(value_base(tid));
+#pragma unroll
+    for (int i = 0; i < 2 * KR; ++i)
+      *reinterpret_cast<u32x4 *>(k + k0 + i * (256 / (D / 8)) * (D / 2)) = u32x4{raw[4 * i], raw[4 * i + 1], raw[4 * i + 2], raw[4 * i + 3]};
+#pragma unroll
+    for (int j = 0; j < VB; ++j) {
+      constexpr int W = VB / 2, at = 8 * KR;
+      const uint32_t sel = j & 1 ? 0x07060302 : 0x05040100, q = j >> 1;
+      *reinterpret_cast<u32x2 *>(v + value_at(v0, j)) = u32x2{pick(raw[at + W + q], raw[at + q], sel), pick(raw[at + 3 * W + q], raw[at + 2 * W + q], sel)};
+    }
+  }
+};
+
+template <int D>
+__device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Staged<D> &s, int lane, int wave) {
+  typedef Tall<D> T;
+  constexpr int KC = T::KC, DB = T::DB;
+  const int tid = threadIdx.x, r = lane & 31, h = lane >> 5;
+  const int mine = t.entry + 32 * wave;
+  const bool live = mine < t.entries;  // (a wave without entries stages with the others)
+  bf16x8 q[KC];
+  f32x16 o[DB];
+  {
+    const char *p = u.q + entry_at(a, min(mine + r, t.entries - 1), a.qs);
+#pragma unroll
+    for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const bf16x8 *>(p + 32 * c + 16 * h);
+  }
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  T stage;
+  float ks[2], vs[2];
+  const int last_block = (t.P + kQ8Block - 1) / kQ8Block - 1;
+  auto load = [&](int j) {
+    if (j < t.cached) {
+      const int valid = min(t.P - j * kStep, kStep);
+      const Rows k(u.kc, a.cs[1], j * kStep, valid, D), v(u.vc, a.cs[1], j * kStep, valid, D);
+      if (valid == kStep) stage.template load_cached<true>(k, v, tid);
+      else stage.template load_cached<false>(k, v, tid);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) ks[i] = q8_scale(u.ke[min(2 * j + i, last_block)]), vs[i] = q8_scale(u.ve[min(2 * j + i, last_block)]);
+    } else {
+      const int i = j - t.cached, valid = min(t.N - i * kStep, kStep);
+      const Rows k(u.ks, a.ks[1], i * kStep, valid, 2 * D), v(u.vs, a.ks[1], i * kStep, valid, 2 * D);
+      if (valid == kStep) stage.template load_suffix<true>(k, v, tid);
+      else stage.template load_suffix<false>(k, v, tid);
+    }
+  };
+  auto store = [&](int j) {
+    if (j < t.cached) stage.store_cached(s.k[j & 1], s.v[j & 1], ks, vs, tid);
+    else stage.store_suffix(s.k[j & 1], s.v[j & 1], tid);
+  };
+  load(t.from);
+  store(t.from);
+  if (t.from + 1 < t.to) load(t.from + 1);
+  __syncthreads();
+  for (int j = t.from; j < t.to; ++j) {
+    if (j + 1 < t.to) store(j + 1);
+    if (j + 2 < t.to) load(j + 2);
+    if (live) {
+      const uint32_t *k = s.k[j & 1], *v = s.v[j & 1];
+      const int valid = j < t.cached ? t.P - j * kStep : t.N - (j - t.cached) * kStep;
+      const int k0 = anew(T::key_piece(r, h)), v0 = anew(T::value_piece(r, h));
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f32x16 z;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(k + (k0 ^ 8 * c) + 32 * b * (D / 2)), q[c], z, 0, 0, 0);
+        if (valid < kStep)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) z[i] = 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) < valid ? z[i] : -INFINITY;
+        float most = z[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, z[i]);
+        most = fmaxf(most, __shfl_xor(most, 32)) * a.c;
+        if (__any(most > m + kLag)) {
+          const float to = fmaxf(m, most), f = to > m ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+          m = to;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[d] *= f;
+        }
+        bf16x8 P[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m));
+          l += p;
+          P[i >> 3][i & 7] = __bf16(p);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(v + (v0 ^ 8 * (2 * b + i)) + 1024 * d), P[i], o[d], 0, 0, 0);
+      }
+    }
+    __syncthreads();
+  }
+  if (!live || mine + r >= t.entries) return;
+  l += __shfl_xor(l, 32);
+  // element 32 d + 8 j + 4 h + i
+  if (t.slot < 0) {
+    const float inv = 1.f / l;
+    char *out = u.out + entry_at(a, mine + r, a.os);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<bf16x4 *>(out + 2 * (32 * d + 8 * j + 4 * h)) =
+            bf16x4{__bf16(o[d][4 * j] * inv), __bf16(o[d][4 * j + 1] * inv), __bf16(o[d][4 * j + 2] * inv), __bf16(o[d][4 * j + 3] * inv)};
+  } else {
+    float *to = part_at<D>(a, t.slot, 32 * wave + r);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(to + 32 * d + 8 * j + 4 * h) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    if (h == 0) *reinterpret_cast<f32x2 *>(part_stats<D>(a, t.slot, 32 * wave + r)) = f32x2{m, l};
+  }
+}
+
+// ---- kernels ---------------------------------------------------------------------------
+// Workgroups that stay, and take every groups / 8-th item of their XCD's list.  In it: sequences; of a sequence this XCD's share of its units (so that what
+// meets the same keys shares an L2); of a unit its tiles, their parts.  Where a sequence's units are no multiple of 8, each unit's items are dealt out to
+// `pieces` XCDs.
+template <int D, int WAVES, bool TALL>
+__global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a, Q8Layers L) {
+  union Shared {
+    Joined<D, WAVES> joined;
+    Staged<TALL ? D : 64> staged;
+    __device__ Shared() {}
+  };
+  __shared__ Shared s;
+  const int lane = threadIdx.x & (kWave - 1), wave = first_lane(threadIdx.x / kWave);
+  const int xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds, stride = a.groups / kXcds;
+  Plan plan;
+  plan.start(a, lane);
+  for (int q = mine;; q += stride) {
+    const int at = plan.find(a, q, lane);
+    if (at < 0) break;
+    Item t;
+    t.b = plan.b0 + at;
+    t.N = at_lane(plan.n.N, at);
+    t.P = at_lane(plan.n.P, at);
+    const Shape shape = shape_of(a, {t.N, t.P});
+    t.entries = shape.entries;
+    t.rows = shape.rows;
+    t.cached = shape.cached;
+    const int splits = plan.splits_of(shape), items = shape.tiles * splits;
+    const int before = plan.base + (at > 0 ? at_lane(plan.end, max(at - 1, 0)) : 0), in_seq = q - before;
+    const int per_piece = (items + a.pieces - 1) / a.pieces, piece = in_seq / per_piece;
+    const int list = piece * kXcds + xcd, unit = list / a.pieces, item = (in_seq - piece * per_piece) * a.pieces + list % a.pieces;
+    if (item >= items) continue;
+    t.b = first_lane(t.b);
+    t.l = first_lane(quotient(unit, a.by_heads));
+    t.g = first_lane(unit - t.l * a.Hkv);
+    const int tile = item / splits, part = item - tile * splits;
+    t.entry = first_lane(tile * t.rows);
+    t.from = first_lane(part * plan.chunk);
+    t.to = splits == 1 ? shape.steps : min(t.from + plan.chunk, shape.steps);
+    t.slot = -1;
+    if (splits > 1) {
+      const int slots = plan.slot_base + (at > 0 ? at_lane(plan.slot_end, max(at - 1, 0)) : 0);
+      t.slot = slots + (unit * items + item) * ((t.rows + 31) / 32);
+    }
+    const Unit u(a, L, t);
+    if (TALL && t.rows == kTall) {
+      if constexpr (TALL) tall_item<D>(a, u, t, s.staged, lane, wave);
+    } else if (t.rows == 32) {
+      short_item<D, 2, WAVES>(a, u, t, s.joined, lane, wave);
+    } else {
+      short_item<D, 1, WAVES>(a, u, t, s.joined, lane, wave);
+    }
+    __syncthreads();
+  }
+}
+
+// The parts of divided tiles, joined: a wave to an entry.
+template <int D>
+__global__ __launch_bounds__(256) void join_kernel(Q8AttnArgs a, Q8Layers L) {
+  const int lane = threadIdx.x & (kWave - 1);
+  Plan plan;
+  plan.start(a, lane);
+  if (!plan.split) return;
+  // entries of all units of sequences, instead of items of an XCD
+  const int waves = gridDim.x * 4;
+  int first = blockIdx.x * 4 + first_lane(threadIdx.x / kWave), slots = 0, before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    plan.b0 = b0;
+    plan.take(a, lane);
+    const Shape mine = shape_of(a, plan.n);
+    const int n = a.per_seq * mine.entries, splits_mine = plan.splits_of(mine), end = running_sum(n, lane), all = at_lane(end, kWave - 1);
+    for (; first < before + all; first += waves) {
+      const int at = __builtin_ctzll(__ballot(first < before + end));
+      const int entries = at_lane(mine.entries, at), splits = at_lane(splits_mine, at), rows = at_lane(mine.rows, at), tiles = at_lane(mine.tiles, at);
+      if (splits <= 1) continue;
+      const int i = first - before - (at_lane(end, at) - at_lane(n, at)), unit = i / entries, e = i - unit * entries, tile = e / rows;
+      const int per_part = (rows + 31) / 32, items = tiles * splits;
+      const int slot = slots + (at_lane(plan.slot_end, at) - a.per_seq * items * per_part) + (unit * items + tile * splits) * per_part;
+      const int row = e - tile * rows;
+      float m = -INFINITY;
+      for (int k = lane; k < splits; k += kWave) m = fmaxf(m, part_stats<D>(a, slot + k * per_part, row)[0]);
+#pragma unroll
+      for (int x = 1; x < kWave; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+      float o[D / kWave] = {}, sum = 0.f;
+      for (int k = 0; k < splits; ++k) {
+        const float *st = part_stats<D>(a, slot + k * per_part, row), *p = part_at<D>(a, slot + k * per_part, row) + lane * (D / kWave);
+        const float f = __builtin_amdgcn_exp2f(st[0] - m);
+        sum += st[1] * f;
+#pragma unroll
+        for (int j = 0; j < D / kWave; ++j) o[j] += p[j] * f;
+      }
+      Item t = {};
+      t.b = b0 + at;
+      t.l = quotient(unit, a.by_heads);
+      t.g = unit - t.l * a.Hkv;
+      const Unit u(a, L, t);
+      const float inv = 1.f / sum;
+      __bf16 *out = reinterpret_cast<__bf16 *>(u.out + entry_at(a, e, a.os)) + lane * (D / kWave);
+#pragma unroll
+      for (int j = 0; j < D / kWave; ++j) out[j] = __bf16(o[j] * inv);
+    }
+    before += all;
+    slots += at_lane(plan.slot_end, kWave - 1);
+  }
+}
+
+bool divides(int64_t C, int64_t S) { return C + S > kPartKeys; }
+
+template <int D>
+int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_t st) {
+  Q8AttnArgs a = args;
+  a.per_seq = layers * a.Hkv;
+  a.pieces = 1;
+  while ((int64_t(a.per_seq) * a.pieces) % kXcds != 0) a.pieces *= 2;
+  a.per_xcd = int32_t(int64_t(a.per_seq) * a.pieces / kXcds);
+  a.by_heads = div_by(a.Hkv);
+  a.by_rep = div_by(a.rep);
+  const bool tall = int64_t(a.rep) * a.S > kShort;
+  const bool wide = !tall && int64_t(a.per_seq) * a.B <= 256;
+  a.groups = wide ? 256 : 512;
+  if (tall) attn_q8_kernel<D, 4, true><<<a.groups, 256, 0, st>>>(a, L);
+  else if (wide) attn_q8_kernel<D, 8, false><<<a.groups, 512, 0, st>>>(a, L);
+  else attn_q8_kernel<D, 4, false><<<a.groups, 256, 0, st>>>(a, L);
   LSP_CHECK_LAUNCH("lsp_attn_step_q8: launch");
+  if (a.parts != nullptr) {
+    join_kernel<D><<<512, 256, 0, st>>>(a, L);
+    LSP_CHECK_LAUNCH("lsp_attn_step_q8: launch");
+  }
   return LSP_OK;
 }
 
 }  // namespace
 }  // namespace lsp
 
-extern "C" size_t lsp_attn_q8_workspace_bytes(const lsp_attn_desc *d, int32_t num_layers) { return 0; }
+namespace lsp {
+namespace {
+int32_t check(const char *what, const lsp_attn_desc *d, int32_t num_layers, AttnArgs &c) {
+  const int32_t rc = check_q8(what, d, true, c);
+  if (rc != LSP_OK) return rc;
+  if (d->dtype != LSP_BF16) {
+    set_error("%s: bf16 queries only", what);
+    return LSP_ERR_UNSUPPORTED;
+  }
+  LSP_CHECK_ARG(num_layers > 0, "%s: num_layers must be positive", what);
+  LSP_CHECK_ARG(c.B == 1 || c.os[0] > 0, "%s: the output must not be shared by sequences", what);
+  LSP_CHECK_ARG(c.cs[1] >= c.D && c.ks[1] >= c.D, "%s: rows of keys and values must not overlap", what);
+  // items, and parts of 32 entries, are counted in 32 bits
+  const int64_t heads = int64_t(c.B) * c.Hkv * kMaxAttnLayers, items = (int64_t(c.S) * (c.Hq / c.Hkv) + kTall - 1) / kTall + 4;
+  LSP_CHECK_ARG(heads * kXcds < int64_t(1) << 31 && items < int64_t(1) << 24 && heads * items < int64_t(1) << 28,
+                "%s: B * Hkv must be < 2^23, B * S * Hq and S * Hq / Hkv < 2^30", what);
+  return LSP_OK;
+}
+}  // namespace
+}  // namespace lsp
+
+extern "C" size_t lsp_attn_q8_workspace_bytes(const lsp_attn_desc *d, int32_t num_layers) {
+  using namespace lsp;
+  AttnArgs c;
+  if (check("lsp_attn_q8_workspace_bytes", d, num_layers, c) != LSP_OK) return 0;
+  return divides(c.C, c.S) ? size_t(kSlots) * 32 * (c.D + 2) * sizeof(float) : 0;
+}
 
 extern "C" int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *d, int32_t num_layers, const void *const *q_layers, const void *const *k_suf_layers,
                                            const void *const *v_suf_layers, const void *const *k_cache_layers, const void *const *v_cache_layers,
@@ -286,19 +859,11 @@ extern "C" int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *d, int32_t num_l
   using namespace lsp;
   const char *what = "lsp_attn_step_q8";
   AttnArgs c;
-  const int32_t rc = check_q8(what, d, true, c);
+  const int32_t rc = check(what, d, num_layers, c);
   if (rc != LSP_OK) return rc;
-  if (d->dtype != LSP_BF16) {
-    set_error("%s: bf16 queries only", what);
-    return LSP_ERR_UNSUPPORTED;
-  }
-  LSP_CHECK_ARG(num_layers > 0, "%s: num_layers must be positive", what);
   LSP_CHECK_ARG(q_layers && k_suf_layers && v_suf_layers && k_cache_layers && v_cache_layers && k_scale_layers && v_scale_layers && out_layers &&
                     prefix_len && suffix_len,
                 "%s: null pointer", what);
-  LSP_CHECK_ARG(c.B == 1 || c.os[0] > 0, "%s: the output must not be shared by sequences", what);
-  LSP_CHECK_ARG(int64_t(kMaxAttnLayers) * c.B * c.Hkv < int64_t(1) << 31 && int64_t(c.S) * (c.Hq / c.Hkv) <= 1 << 30,
-                "%s: B * Hkv must be < 2^26, S * Hq / Hkv <= 2^30", what);
   for (int l = 0; l < num_layers; ++l) {
     LSP_CHECK_ARG(q_layers[l] && k_suf_layers[l] && v_suf_layers[l] && k_cache_layers[l] && v_cache_layers[l] && k_scale_layers[l] &&
                       v_scale_layers[l] && out_layers[l],
@@ -311,6 +876,8 @@ extern "C" int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *d, int32_t num_l
   a.prefix_len = prefix_len; a.suffix_len = suffix_len;
   a.B = c.B; a.S = c.S; a.Hkv = c.Hkv; a.C = c.C; a.rep = c.Hq / c.Hkv; a.blocks = (c.C + kQ8Block - 1) / kQ8Block;
   a.c = c.scale * kLog2e;
+  const size_t need = lsp_attn_q8_workspace_bytes(d, num_layers);
+  a.parts = need > 0 && workspace != nullptr && workspace_bytes >= need && aligned16(workspace) ? static_cast<float *>(workspace) : nullptr;
   for (int k = 0; k < 3; ++k) a.qs[k] = 2 * c.qs[k], a.ks[k] = 2 * c.ks[k], a.cs[k] = c.cs[k], a.os[k] = 2 * c.os[k];
   for (int l0 = 0; l0 < num_layers; l0 += kMaxAttnLayers) {
     const int nl = num_layers - l0 < kMaxAttnLayers ? num_layers - l0 : kMaxAttnLayers;
@@ -322,7 +889,7 @@ extern "C" int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *d, int32_t num_l
       L.k_scale[l] = static_cast<uint8_t *>(const_cast<void *>(k_scale_layers[l0 + l])); L.v_scale[l] = static_cast<uint8_t *>(const_cast<void *>(v_scale_layers[l0 + l]));
       L.out[l] = static_cast<char *>(out_layers[l0 + l]);
     }
-    const int32_t r = launch(a, c.D, L, nl, static_cast<hipStream_t>(stream));
+    const int32_t r = c.D == 64 ? launch<64>(a, L, nl, static_cast<hipStream_t>(stream)) : launch<128>(a, L, nl, static_cast<hipStream_t>(stream));
     if (r != LSP_OK) return r;
   }
   return LSP_OK;

@@ -62,7 +62,7 @@ def test_read(desc, kw, rc, word):
 
 @pytest.mark.parametrize("desc, kw, rc, word", COMMON + [
     (dict(dtype=0), {}, -2, b"bf16"), (dict(Hq=3), {}, -1, b"multiple"), (dict(scale=-1.0), {}, -1, b"scale"),
-    (dict(B=2, o_stride=_strides(0, 512, 128)), {}, -1, b"shared"), (dict(S=1 << 27, Hq=32, Hkv=1), {}, -1, b"2^30"), (dict(B=65535, Hq=2048, Hkv=2048), {}, -1, b"2^26"),
+    (dict(B=2, o_stride=_strides(0, 512, 128)), {}, -1, b"shared"), (dict(S=1 << 27, Hq=32, Hkv=1), {}, -1, b"2^30"), (dict(B=65535, Hq=2048, Hkv=2048), {}, -1, b"2^23"),
     ({}, dict(q=NULL), -1, b"layer 0"), ({}, dict(out=ODD), -1, b"aligned")])
 def test_attention(desc, kw, rc, word):
     def call(d, n=1, q=ONE, ks=ONE, vs=ONE, kc=ONE, vc=ONE, ke=ONE, ve=ONE, x=_p(), y=_p(), out=ONE):
