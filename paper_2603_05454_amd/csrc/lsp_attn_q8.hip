@@ -9,6 +9,8 @@
 // block's scale: exact).
 #include <math.h>
 
+#include <type_traits>
+
 #include "lsp_q8.h"
 
 namespace lsp {
@@ -21,9 +23,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLag = 8.f;      // octaves that a maximum may exceed the reference by before that moves
 constexpr int kStep = 64;        // keys of a step: of the cache or of the suffix
 constexpr int kShort = 64;       // entries of a unit up to which its tiles are short ones
-constexpr int kTall = 128;       // entries of a tall tile
+constexpr int kTall = 128;       // entries up to which, beyond that, a tile has as many
+constexpr int kTallest = 256;    // entries of a tile of the others (heads of 128)
 constexpr int kXcds = 8;
-constexpr int kSlots = 2048;     // parts of 32 entries in the workspace
+constexpr int kSlots = 2048;     // parts of 32 entries in the workspace, for each of two kernels
 constexpr int kPartKeys = 1024;  // C + S beyond which keys are divided at all
 constexpr int kLeast = 4;        // steps of a part, at least
 
@@ -32,6 +35,7 @@ struct Q8AttnArgs {
   int32_t B, S, Hkv, C, rep, blocks, per_seq;  // per_seq: units of a sequence, layers * Hkv
   int32_t pieces, per_xcd;                     // each unit's items are dealt out to `pieces` lists, of which every XCD has per_xcd of a sequence
   int32_t groups;                              // workgroups
+  int32_t above, up_to, tall;                  // entries of the units that are this kernel's; of a tall tile
   float c;                                     // scale log2(e)
   Div by_heads, by_rep;
   int64_t qs[3], ks[3], cs[3], os[3];  // bytes: sequence, row, head
@@ -101,7 +105,8 @@ struct Shape {  // of a sequence's units
 __device__ __forceinline__ Shape shape_of(const Q8AttnArgs &a, Lens n) {
   Shape s;
   s.entries = n.N * a.rep;
-  s.rows = s.entries > kShort ? kTall : s.entries > 16 ? 32 : 16;
+  if (s.entries <= a.above || s.entries > a.up_to) s.entries = 0;
+  s.rows = s.entries > kShort ? a.tall : s.entries > 16 ? 32 : 16;
   s.tiles = (s.entries + s.rows - 1) / s.rows;
   s.cached = (n.P + kStep - 1) / kStep;
   s.steps = s.cached + (n.N + kStep - 1) / kStep;
@@ -381,7 +386,7 @@ struct Short {
   }
 };
 
-// LDS of a workgroup.  Short tiles: what its waves join.  Tall ones: two steps' keys [64][D] and values [D][64], bf16.
+// LDS of a workgroup.  Short tiles: what its waves join.  Tall ones: four blocks' keys [32][D] and two steps' values [D][64], bf16.
 template <int D, int WAVES>
 struct Joined {
   f32x4 o[WAVES][D / 16][kWave];
@@ -389,7 +394,7 @@ struct Joined {
 };
 template <int D>
 struct Staged {
-  uint32_t k[2][kStep * D / 2], v[2][kStep * D / 2];
+  uint32_t k[4][kQ8Block * D / 2], v[2][kStep * D / 2];
 };
 
 template <int D, int NB, int WAVES>
@@ -473,114 +478,115 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, c
 }
 
 // ---- tall tiles ------------------------------------------------------------------------
-// Four waves of 32 entries each, which share steps of 64 keys in LDS, bf16 by then.  The scores of a wave are keys x entries (32x32x16): lane l has those
+// Waves of 32 entries each, which share keys and values in LDS, bf16 by then.  The scores of a wave are keys x entries (32x32x16): lane l has those
 // of entry l % 32 with keys 8 j + 4 h + i of 32, h = l / 32, and these are, eight at a time, the operand of the second product, whose other one is
 // V^T: eight keys' values of one element, 16 bytes.  So the values are turned as they are written to LDS: row d holds for each (32 keys, 16 of them,
 // h) the eight keys 8 x + 4 h + i in the order of x, i.
 // 16-byte pieces are exchanged against bank conflicts: piece p of a key's 256 bytes at p ^ (key % 16) (of 128: p ^ (key / 2 % 8)); piece p of
-// the 128 bytes of element d at p ^ ((d / 8 % 4 ^ d / 2) % 8), which serves both the writes, of every eighth d, and the reads, of neighbours.
-template <int D>
+// the 128 bytes of element d at p ^ (d / 2 % 8), and ^ 6 for every other sixteen, which serves both the writes, of every eighth d, and the reads, of
+// neighbours (a wave's read of 1 KB takes 4.3 clocks so, 8.1 with any two of its lanes in the same place).
+template <int D, int WAVES>
 struct Tall {
-  static constexpr int KC = D / 16, DB = D / 32, VB = D / 16;  // VB: elements of four keys' values that a thread turns
-  static constexpr int KR = D / 64, VR = D / 64 * 4;           // loads of 16 bytes of a step's keys in 8 bits; words of its values
+  static constexpr int KC = D / 16, DB = D / 32;
+  static constexpr int VB = 4 * D / (16 * WAVES), kTurning = D / VB;  // elements of four keys' values that a thread turns; threads that have those of four keys
+  static constexpr int KP = D / 64;                                   // pieces of a block's keys that a thread has
+  static constexpr int kSets = 8 / WAVES;                             // of a step's two blocks
 
   // in words
   static __device__ __forceinline__ int key_piece(int key, int p) {
     return D == 128 ? key * 64 + 4 * (p ^ (key & 15)) : key * 32 + 4 * (p ^ (key >> 1 & 7));
   }
-  static __device__ __forceinline__ int value_piece(int d, int p) { return d * 32 + 4 * (p ^ (((d >> 3 & 3) ^ d >> 1) & 7)); }
+  static __device__ __forceinline__ int value_piece(int d, int p) { return d * 32 + 4 * (p ^ ((d >> 1 ^ (d & 16 ? 6 : 0)) & 7)); }
 
-  uint32_t raw[4 * 4 * D / 64];  // what a thread has on its way: half of it keys, half values
+  // what a thread has on its way: of two blocks of 32 keys, of a step's values (half as much of the cache), and of their exponents (the keys': a byte each)
+  uint32_t rk[kSets][4 * KP], rv[2 * VB], ke, ve;
 
-  // cached: keys tid / (D / 16) on, 16 bytes each; values of four keys, VB bytes each.  Suffix: twice the bytes.
-  template <bool FULL>
-  __device__ __forceinline__ void load_cached(const Rows &k, const Rows &v, int tid) {
-    const int kv = anew(tid / (D / 16) * k.row + tid % (D / 16) * 16), vv = anew(tid / 16 * 4 * v.row + tid % 16 * VB);
+  // a block's keys: a thread has D / 8 elements of key tid / 8 % 32
+  __device__ __forceinline__ void load_keys(int i, const Rows &k, int tid, bool cached) {
+    const int at = anew(tid / 8 % 32 * k.row + tid % 8 * (cached ? D / 8 : D / 4));
+    if (!cached) {
 #pragma unroll
-    for (int i = 0; i < KR; ++i) {
-      const u32x4 x = load16<FULL>(k, kv, 256 / (D / 16) * i);
+      for (int p = 0; p < KP; ++p) {
+        const u32x4 x = load16<false>(k, at + 16 * p, 0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) raw[4 * i + j] = x[j];
+        for (int j = 0; j < 4; ++j) rk[i][4 * p + j] = x[j];
+      }
+    } else if constexpr (D == 128) {
+      const u32x4 x = load16<false>(k, at, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) rk[i][j] = x[j];
+    } else {
+      const u32x2 x = load8<false>(k, at, 0);
+      rk[i][0] = x[0], rk[i][1] = x[1];
     }
+  }
+  __device__ __forceinline__ void store_keys(int i, uint32_t *k, float s, int tid, bool cached) const {
+    const int k0 = anew(key_piece(tid / 8 % 32, KP * (tid % 8)));
+#pragma unroll
+    for (int p = 0; p < KP; ++p)
+      *reinterpret_cast<u32x4 *>(k + (k0 ^ 4 * p)) = cached ? u32x4{low(rk[i][2 * p], s), high(rk[i][2 * p], s), low(rk[i][2 * p + 1], s), high(rk[i][2 * p + 1], s)}
+                                                            : u32x4{rk[i][4 * p], rk[i][4 * p + 1], rk[i][4 * p + 2], rk[i][4 * p + 3]};
+  }
+  // a step's values: VB elements of four keys
+  __device__ __forceinline__ void load_values(const Rows &v, int tid, bool cached) {
+    const int vv = anew(tid / kTurning * 4 * v.row + tid % kTurning * (cached ? VB : 2 * VB)), bytes = cached ? VB : 2 * VB;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if constexpr (VB == 8) {
-        const u32x2 x = load8<FULL>(v, vv, i);
-        raw[8 + 2 * i] = x[0], raw[8 + 2 * i + 1] = x[1];
+      if (bytes == 16) {
+        const u32x4 x = load16<false>(v, vv, i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rv[4 * i + j] = x[j];
+      } else if (bytes == 8) {
+        const u32x2 x = load8<false>(v, vv, i);
+        rv[2 * i] = x[0], rv[2 * i + 1] = x[1];
       } else {
-        raw[4 + i] = load4<FULL>(v, vv, i);
+        rv[i] = load4<false>(v, vv, i);
       }
     }
   }
-  template <bool FULL>
-  __device__ __forceinline__ void load_suffix(const Rows &k, const Rows &v, int tid) {
-    const int kv = anew(tid / (D / 8) * k.row + tid % (D / 8) * 16), vv = anew(tid / 16 * 4 * v.row + tid % 16 * VB * 2);
-#pragma unroll
-    for (int i = 0; i < 2 * KR; ++i) {
-      const u32x4 x = load16<FULL>(k, kv, 256 / (D / 8) * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) raw[4 * i + j] = x[j];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (VB == 8) {
-        const u32x4 x = load16<FULL>(v, vv, i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) raw[16 + 4 * i + j] = x[j];
-      } else {
-        const u32x2 x = load8<FULL>(v, vv, i);
-        raw[8 + 2 * i] = x[0], raw[8 + 2 * i + 1] = x[1];
-      }
-    }
-  }
-  // Where element j of the thread's values of four keys goes: keys 4 f to 4 f + 3, f = tid / 16 = 8 kb + 4 t + 2 x + h, are half x of piece 4 kb + 2 t + h.
+  // Where the thread's values of four keys go: keys 4 f to 4 f + 3, f = tid / kTurning = 8 kb + 4 t + 2 x + h, are half x of piece 4 kb + 2 t + h of row d.  Every
+  // other thread stores its rows 2 i + 1 before 2 i: rows of one parity share 32 banks (a wave's store of 8 bytes 16 clocks, 8 so).
   static __device__ __forceinline__ int value_base(int tid) {
-    const int f = tid / 16;
-    return value_piece(tid % 16 * VB, f >> 3 << 2 | (f >> 2 & 1) << 1 | (f & 1)) + 2 * (f >> 1 & 1);
+    const int f = tid / kTurning;
+    return value_piece(tid % kTurning * VB, f >> 3 << 2 | (f >> 2 & 1) << 1 | (f & 1)) + 2 * (f >> 1 & 1);
   }
-  static __device__ __forceinline__ int value_at(int base, int j) { return (base ^ 4 * (j >> 1)) + 32 * j; }
-
-  // ks, vs: scales of the step's two blocks of 32 keys
-  __device__ __forceinline__ void store_cached(uint32_t *k, uint32_t *v, const float (&ks)[2], const float (&vs)[2], int tid) {
-    const int key0 = tid / (D / 16), k0 = anew(key_piece(key0, tid % (D / 16) * 2)), v0 = anew(value_base(tid));
+  __device__ __forceinline__ void store_values(uint32_t *v, float s, int tid, bool cached) const {
+    const int base = anew(value_base(tid)), odd = tid & 1, to0 = base + 32 * odd, to1 = base + 32 - 32 * odd;
+    const uint32_t even_first = 0x05040100, odd_first = 0x07060302, s0 = odd ? odd_first : even_first, s1 = odd ? even_first : odd_first;
+    auto at = [&](int j) { return reinterpret_cast<u32x2 *>(v + ((j & 1 ? to1 : to0) ^ 4 * (j >> 1)) + 64 * (j >> 1)); };
+    if (cached) {
+      constexpr int W = VB / 4;
 #pragma unroll
-    for (int i = 0; i < KR; ++i) {
-      const float s = KR == 2 ? ks[i] : key0 < 32 ? ks[0] : ks[1];
+      for (int q = 0; q < W; ++q) {
+        const uint32_t a = rv[q], b = rv[W + q], c = rv[2 * W + q], d = rv[3 * W + q];
+        const uint32_t ab = pick(b, a, 0x05010400), cd = pick(d, c, 0x05010400), ab2 = pick(b, a, 0x07030602), cd2 = pick(d, c, 0x07030602);
+        const uint32_t t[4] = {pick(cd, ab, s0), pick(cd, ab, s1), pick(cd2, ab2, s0), pick(cd2, ab2, s1)};
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        *reinterpret_cast<u32x4 *>(k + (k0 ^ 4 * j) + i * 32 * (D / 2)) =
-            u32x4{low(raw[4 * i + 2 * j], s), high(raw[4 * i + 2 * j], s), low(raw[4 * i + 2 * j + 1], s), high(raw[4 * i + 2 * j + 1], s)};
-    }
-    const float s = tid < 128 ? vs[0] : vs[1];
+        for (int j = 0; j < 4; ++j) *at(4 * q + j) = u32x2{low(t[j], s), high(t[j], s)};
+      }
+    } else {
+      constexpr int W = VB / 2;
 #pragma unroll
-    for (int q = 0; q < VB / 4; ++q) {
-      uint32_t t[4];
-      constexpr int W = VB / 4, at = 4 * KR;
-      turn_bytes(raw[at + q], raw[at + W + q], raw[at + 2 * W + q], raw[at + 3 * W + q], t);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x2 *>(v + value_at(v0, 4 * q + j)) = u32x2{low(t[j], s), high(t[j], s)};
-    }
-  }
-  __device__ __forceinline__ void store_suffix(uint32_t *k, uint32_t *v, int tid) {
-    // (rows 16 (or 32) further on have the same exchange)
-    const int k0 = anew(key_piece(tid / (D / 8), tid % (D / 8))), v0 = anew(value_base(tid));
-#pragma unroll
-    for (int i = 0; i < 2 * KR; ++i)
-      *reinterpret_cast<u32x4 *>(k + k0 + i * (256 / (D / 8)) * (D / 2)) = u32x4{raw[4 * i], raw[4 * i + 1], raw[4 * i + 2], raw[4 * i + 3]};
-#pragma unroll
-    for (int j = 0; j < VB; ++j) {
-      constexpr int W = VB / 2, at = 8 * KR;
-      const uint32_t sel = j & 1 ? 0x07060302 : 0x05040100, q = j >> 1;
-      *reinterpret_cast<u32x2 *>(v + value_at(v0, j)) = u32x2{pick(raw[at + W + q], raw[at + q], sel), pick(raw[at + 3 * W + q], raw[at + 2 * W + q], sel)};
+      for (int j = 0; j < VB; ++j) {
+        const int q = j >> 1;
+        const uint32_t sel = j & 1 ? s1 : s0;
+        *at(j) = u32x2{pick(rv[W + q], rv[q], sel), pick(rv[3 * W + q], rv[2 * W + q], sel)};
+      }
     }
   }
 };
 
-template <int D>
+// What stands before it is issued before what stands behind.
+__device__ __forceinline__ void here() { __builtin_amdgcn_sched_barrier(0); }
+
+// Blocks of 32 keys: the scores of the next block (eight matrix instructions) stand beside the exponentials of this one, and this one's values (eight) beside
+// the next one's maximum; a slice of vector instructions behind every matrix instruction, laid by hand.  Operands are read from LDS four
+// instructions ahead.  The keys are in LDS a block earlier than the values: a ring of four blocks, two of which are read and two written in a step of two.
+template <int D, int WAVES>
 __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Staged<D> &s, int lane, int wave) {
-  typedef Tall<D> T;
+  typedef Tall<D, WAVES> T;
   constexpr int KC = T::KC, DB = T::DB;
-  const int tid = threadIdx.x, r = lane & 31, h = lane >> 5;
+  const int tid = wave * kWave + lane, r = lane & 31, h = lane >> 5;
   const int mine = t.entry + 32 * wave;
   const bool live = mine < t.entries;  // (a wave without entries stages with the others)
   bf16x8 q[KC];
@@ -596,76 +602,204 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  T stage;
-  float ks[2], vs[2];
-  const int last_block = (t.P + kQ8Block - 1) / kQ8Block - 1;
-  auto load = [&](int j) {
+  const int last_block = (t.P + kQ8Block - 1) / kQ8Block - 1, end = 2 * t.to;
+  auto valid_in = [&](int j) { return j < t.cached ? t.P - j * kStep : t.N - (j - t.cached) * kStep; };  // keys of step j that there are
+  auto load_keys = [&](T &to, int i, int b) {  // block b
+    const int j = b >> 1, valid = min(valid_in(j) - (b & 1) * kQ8Block, kQ8Block);
+    if (b >= end || valid <= 0) return;
     if (j < t.cached) {
-      const int valid = min(t.P - j * kStep, kStep);
-      const Rows k(u.kc, a.cs[1], j * kStep, valid, D), v(u.vc, a.cs[1], j * kStep, valid, D);
-      if (valid == kStep) stage.template load_cached<true>(k, v, tid);
-      else stage.template load_cached<false>(k, v, tid);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) ks[i] = q8_scale(u.ke[min(2 * j + i, last_block)]), vs[i] = q8_scale(u.ve[min(2 * j + i, last_block)]);
+      const Rows k(u.kc, a.cs[1], b * kQ8Block, valid, D);
+      to.load_keys(i, k, tid, true);
+      to.ke = i == 0 ? u.ke[b] : to.ke | u.ke[b] << 8;
     } else {
-      const int i = j - t.cached, valid = min(t.N - i * kStep, kStep);
-      const Rows k(u.ks, a.ks[1], i * kStep, valid, 2 * D), v(u.vs, a.ks[1], i * kStep, valid, 2 * D);
-      if (valid == kStep) stage.template load_suffix<true>(k, v, tid);
-      else stage.template load_suffix<false>(k, v, tid);
+      const Rows k(u.ks, a.ks[1], (b - 2 * t.cached) * kQ8Block, valid, 2 * D);
+      to.load_keys(i, k, tid, false);
+      to.ke = i == 0 ? 127 : to.ke | 127 << 8;
     }
   };
-  auto store = [&](int j) {
-    if (j < t.cached) stage.store_cached(s.k[j & 1], s.v[j & 1], ks, vs, tid);
-    else stage.store_suffix(s.k[j & 1], s.v[j & 1], tid);
+  auto load_values = [&](T &to, int j) {
+    if (j >= t.to) return;
+    const int valid = min(valid_in(j), kStep);
+    if (j < t.cached) {
+      const Rows v(u.vc, a.cs[1], j * kStep, valid, D);
+      to.load_values(v, tid, true);
+      to.ve = u.ve[min(2 * j + tid / (32 * WAVES), last_block)];
+    } else {
+      const Rows v(u.vs, a.ks[1], (j - t.cached) * kStep, valid, 2 * D);
+      to.load_values(v, tid, false);
+      to.ve = 127;
+    }
   };
-  load(t.from);
-  store(t.from);
-  if (t.from + 1 < t.to) load(t.from + 1);
-  __syncthreads();
-  for (int j = t.from; j < t.to; ++j) {
-    if (j + 1 < t.to) store(j + 1);
-    if (j + 2 < t.to) load(j + 2);
-    if (live) {
-      const uint32_t *k = s.k[j & 1], *v = s.v[j & 1];
-      const int valid = j < t.cached ? t.P - j * kStep : t.N - (j - t.cached) * kStep;
-      const int k0 = anew(T::key_piece(r, h)), v0 = anew(T::value_piece(r, h));
+  auto store_keys = [&](const T &from, int i, int b) {
+    if (b >= end) return;
+    if (b < 2 * t.cached) from.store_keys(i, s.k[b & 3], q8_scale(i == 0 ? from.ke & 255 : from.ke >> 8), tid, true);
+    else from.store_keys(i, s.k[b & 3], 1.f, tid, false);
+  };
+  auto store_values = [&](const T &from, int j) {
+    if (j >= t.to) return;
+    if (j < t.cached) from.store_values(s.v[j & 1], q8_scale(from.ve), tid, true);
+    else from.store_values(s.v[j & 1], 1.f, tid, false);
+  };
+  auto mask = [&](f32x16 &z, int b) {
+    const int valid = valid_in(b >> 1) - (b & 1) * kQ8Block;
+    if (valid < kQ8Block)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        f32x16 z;
+      for (int i = 0; i < 16; ++i) z[i] = 8 * (i >> 2) + 4 * h + (i & 3) < valid ? z[i] : -INFINITY;
+  };
+  // the largest score of each entry, against the reference
+  auto look = [&](float most) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+    most = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.c;
+    if (__any(most > m + kLag)) {
+      const float to = fmaxf(m, most), f = to > m ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+      m = to;
+      l *= f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] = 0.f;
+      for (int d = 0; d < DB; ++d) o[d] *= f;
+    }
+  };
+  constexpr int kAhead = 4, kValues = 2 * DB;
+  auto clear = [](f32x16 &z) {
 #pragma unroll
-        for (int c = 0; c < KC; ++c)
-          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(k + (k0 ^ 8 * c) + 32 * b * (D / 2)), q[c], z, 0, 0, 0);
-        if (valid < kStep)
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  };
+  bf16x8 f[kAhead];  // operands on their way
+  // block b: z are its scores, y becomes the next one's (MORE).  PAIR: 1 the next block's first operands are read at its end, 2 these have been
+  auto block = [&](int b, f32x16 &z, f32x16 &y, auto more, auto pair) {
+    constexpr bool MORE = decltype(more)::value;
+    constexpr int PAIR = decltype(pair)::value;
+    const uint32_t *k = s.k[(b + 1) & 3], *v = s.v[b >> 1 & 1];
+    const int k0 = anew(T::key_piece(r, h)), v0 = anew(T::value_piece(r, h) ^ 16 * (b & 1));
+    auto key = [&](int c) { return *reinterpret_cast<const bf16x8 *>(k + (k0 ^ 8 * c)); };
+    auto value = [&](int i) { return *reinterpret_cast<const bf16x8 *>(v + (v0 ^ 8 * (i / DB)) + 1024 * (i % DB)); };
+    u32x4 P[2];
+    float part[2] = {0.f, 0.f};
+    if (MORE) {
+      clear(y);
+      if (PAIR != 2)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) z[i] = 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) < valid ? z[i] : -INFINITY;
-        float most = z[0];
+        for (int c = 0; c < kAhead; ++c) f[c] = key(c);
+    }
+    here();
 #pragma unroll
-        for (int i = 1; i < 16; ++i) most = fmaxf(most, z[i]);
-        most = fmaxf(most, __shfl_xor(most, 32)) * a.c;
-        if (__any(most > m + kLag)) {
-          const float to = fmaxf(m, most), f = to > m ? __builtin_amdgcn_exp2f(m - to) : 1.f;
-          m = to;
-          l *= f;
-#pragma unroll
-          for (int d = 0; d < DB; ++d) o[d] *= f;
-        }
-        bf16x8 P[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m));
-          l += p;
-          P[i >> 3][i & 7] = __bf16(p);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int d = 0; d < DB; ++d)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(v + (v0 ^ 8 * (2 * b + i)) + 1024 * d), P[i], o[d], 0, 0, 0);
+    for (int c = 0; c < KC; ++c) {
+      if (MORE) {
+        y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[c % kAhead], q[c], y, 0, 0, 0);
+        if (c + kAhead < KC) f[c % kAhead] = key(c + kAhead);
       }
+      if (c + kAhead >= KC) f[c % kAhead] = value(c + kAhead - KC);
+#pragma unroll
+      for (int i = 8 * c / KC; i < 8 * (c + 1) / KC; ++i) {
+        bf16x2 two;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(z[2 * i + e], a.c, -m));
+          part[e] += p;
+          two[e] = __bf16(p);
+        }
+        P[i >> 2][i & 3] = word(two);
+        asm volatile("" : "+v"(P[i >> 2][i & 3]), "+v"(part[0]), "+v"(part[1]));  // (not later, behind the next branch)
+      }
+      here();
     }
+    l += part[0] + part[1];
+    if (MORE) mask(y, b + 1);
+    float most = -INFINITY;
+    here();
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], __builtin_bit_cast(bf16x8, P[i / DB]), o[i % DB], 0, 0, 0);
+      if (i + kAhead < kValues) f[i % kAhead] = value(i + kAhead);
+      else if (PAIR == 1) f[i % kAhead] = *reinterpret_cast<const bf16x8 *>(s.k[(b + 2) & 3] + (k0 ^ 8 * (i + kAhead - kValues)));
+      if (MORE)
+#pragma unroll
+        for (int e = 16 * i / kValues; e < 16 * (i + 1) / kValues; e += 2) most = fmaxf(fmaxf(most, y[e]), y[e + 1]);
+      here();
+    }
+    if (MORE) look(most);
+  };
+
+  const int b0 = 2 * t.from, second = wave / 4;  // (of eight waves four have the one of two blocks, four the other)
+  // what step j stores.  (A new one each time: what a load leaves out is not the former's.)
+  auto load_next = [&](int j) {
+    T n;
+    const int b = 2 * j + 3 + second;
+    if (j + 2 < min(t.to, t.cached)) {  // all of it of the cache: one run of loads
+      const Rows v(u.vc, a.cs[1], (j + 1) * kStep, kStep, D);
+#pragma unroll
+      for (int i = 0; i < T::kSets; ++i) n.load_keys(i, Rows(u.kc, a.cs[1], (b + i) * kQ8Block, min(t.P - (b + i) * kQ8Block, kQ8Block), D), tid, true);
+      n.load_values(v, tid, true);
+      if constexpr (T::kSets == 2) {
+        uint16_t two;
+        __builtin_memcpy(&two, u.ke + b, 2);
+        n.ke = two;
+      } else {
+        n.ke = u.ke[b];
+      }
+      n.ve = u.ve[2 * (j + 1) + tid / (32 * WAVES)];
+    } else if (j + 1 >= t.cached && j + 2 < t.to) {
+      const int at = (b - 2 * t.cached) * kQ8Block;
+      const Rows v(u.vs, a.ks[1], (j + 1 - t.cached) * kStep, kStep, 2 * D);
+#pragma unroll
+      for (int i = 0; i < T::kSets; ++i) n.load_keys(i, Rows(u.ks, a.ks[1], at + i * kQ8Block, min(t.N - at - i * kQ8Block, kQ8Block), 2 * D), tid, false);
+      n.load_values(v, tid, false);
+      n.ke = u.ke[0], n.ve = u.ve[0];  // (of no use, but a constant in their place would wait for the loads before)
+    } else {
+#pragma unroll
+      for (int i = 0; i < T::kSets; ++i) load_keys(n, i, b + i);
+      load_values(n, j + 1);
+    }
+    return n;
+  };
+  auto store_next = [&](const T &n, int j) {
+#pragma unroll
+    for (int i = 0; i < T::kSets; ++i) store_keys(n, i, 2 * j + 3 + second + i);
+    store_values(n, j + 1);
+  };
+  {
+    T n, third;
+#pragma unroll
+    for (int i = 0; i < T::kSets; ++i) load_keys(n, i, b0 + second + i);
+    if (second == 0) load_keys(third, 0, b0 + 2);
+    load_values(n, t.from);
+#pragma unroll
+    for (int i = 0; i < T::kSets; ++i) store_keys(n, i, b0 + second + i);
+    if (second == 0) store_keys(third, 0, b0 + 2);
+    store_values(n, t.from);
+  }
+  T next = load_next(t.from);
+  __syncthreads();
+  if (live) {
+    f32x16 z, y;
+    clear(z);
+    {
+      const uint32_t *k = s.k[b0 & 3];
+      const int k0 = T::key_piece(r, h);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(k + (k0 ^ 8 * c)), q[c], z, 0, 0, 0);
+      mask(z, b0);
+      float most = fmaxf(z[0], z[1]);
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) most = fmaxf(fmaxf(most, z[i]), z[i + 1]);
+      look(most);
+    }
+    __syncthreads();  // (the first step writes over the first block's keys)
+    for (int j = t.from; j + 1 < t.to; ++j) {
+      store_next(next, j);
+      next = load_next(j + 1);
+      block(2 * j, z, y, std::true_type(), std::integral_constant<int, 1>());
+      block(2 * j + 1, y, z, std::true_type(), std::integral_constant<int, 2>());
+      __syncthreads();
+    }
+    block(end - 2, z, y, std::true_type(), std::integral_constant<int, 0>());
+    block(end - 1, y, z, std::false_type(), std::integral_constant<int, 0>());
+  } else {  // (as many barriers)
     __syncthreads();
+    for (int j = t.from; j + 1 < t.to; ++j) {
+      store_next(next, j);
+      next = load_next(j + 1);
+      __syncthreads();
+    }
   }
   if (!live || mine + r >= t.entries) return;
   l += __shfl_xor(l, 32);
@@ -692,20 +826,13 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
 // ---- kernels ---------------------------------------------------------------------------
 // Workgroups that stay, and take every groups / 8-th item of their XCD's list.  In it: sequences; of a sequence this XCD's share of its units (so that what
 // meets the same keys shares an L2); of a unit its tiles, their parts.  Where a sequence's units are no multiple of 8, each unit's items are dealt out to
-// `pieces` XCDs.
-template <int D, int WAVES, bool TALL>
-__global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a, Q8Layers L) {
-  union Shared {
-    Joined<D, WAVES> joined;
-    Staged<TALL ? D : 64> staged;
-    __device__ Shared() {}
-  };
-  __shared__ Shared s;
-  const int lane = threadIdx.x & (kWave - 1), wave = first_lane(threadIdx.x / kWave);
-  const int xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds, stride = a.groups / kXcds;
+// `pieces` XCDs.  does(item, unit)
+template <typename F>
+__device__ __forceinline__ void all_items(const Q8AttnArgs &a, const Q8Layers &L, int lane, F does) {
+  const int xcd = blockIdx.x % kXcds, stride = a.groups / kXcds;
   Plan plan;
   plan.start(a, lane);
-  for (int q = mine;; q += stride) {
+  for (int q = blockIdx.x / kXcds;; q += stride) {
     const int at = plan.find(a, q, lane);
     if (at < 0) break;
     Item t;
@@ -733,22 +860,43 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a,
       const int slots = plan.slot_base + (at > 0 ? at_lane(plan.slot_end, max(at - 1, 0)) : 0);
       t.slot = slots + (unit * items + item) * ((t.rows + 31) / 32);
     }
-    const Unit u(a, L, t);
-    if (TALL && t.rows == kTall) {
-      if constexpr (TALL) tall_item<D>(a, u, t, s.staged, lane, wave);
-    } else if (t.rows == 32) {
-      short_item<D, 2, WAVES>(a, u, t, s.joined, lane, wave);
-    } else {
-      short_item<D, 1, WAVES>(a, u, t, s.joined, lane, wave);
-    }
+    does(t, Unit(a, L, t));
     __syncthreads();
   }
 }
 
+// Short tiles, and (TALL) tall ones of four waves.
+template <int D, int WAVES, bool TALL>
+__global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a, Q8Layers L) {
+  union Shared {
+    Joined<D, WAVES> joined;
+    Staged<TALL ? D : 64> staged;
+    __device__ Shared() {}
+  };
+  __shared__ Shared s;
+  const int lane = threadIdx.x & (kWave - 1), wave = first_lane(threadIdx.x / kWave);
+  all_items(a, L, lane, [&](const Item &t, const Unit &u) {
+    const int own = anew(lane);  // (what an item makes of it is not kept for the next one, in registers that the other kinds of items need)
+    if (TALL && t.rows > 32) {
+      if constexpr (TALL) tall_item<D, WAVES>(a, u, t, s.staged, own, wave);
+    } else if (t.rows == 32) {
+      short_item<D, 2, WAVES>(a, u, t, s.joined, own, wave);
+    } else {
+      short_item<D, 1, WAVES>(a, u, t, s.joined, own, wave);
+    }
+  });
+}
+// Tall tiles of eight waves.
+template <int D>
+__global__ __launch_bounds__(512, 2) void attn_q8_tall_kernel(Q8AttnArgs a, Q8Layers L) {
+  __shared__ Staged<D> s;
+  const int lane = threadIdx.x & (kWave - 1), wave = first_lane(threadIdx.x / kWave);
+  all_items(a, L, lane, [&](const Item &t, const Unit &u) { tall_item<D, 8>(a, u, t, s, anew(lane), wave); });
+}
+
 // The parts of divided tiles, joined: a wave to an entry.
 template <int D>
-__global__ __launch_bounds__(256) void join_kernel(Q8AttnArgs a, Q8Layers L) {
-  const int lane = threadIdx.x & (kWave - 1);
+__device__ __forceinline__ void join(const Q8AttnArgs &a, const Q8Layers &L, int lane) {
   Plan plan;
   plan.start(a, lane);
   if (!plan.split) return;
@@ -795,7 +943,17 @@ __global__ __launch_bounds__(256) void join_kernel(Q8AttnArgs a, Q8Layers L) {
   }
 }
 
+template <int D>
+__global__ __launch_bounds__(256) void join_kernel(Q8AttnArgs a, Q8AttnArgs tallest, Q8Layers L) {
+  const int lane = threadIdx.x & (kWave - 1);
+  join<D>(a, L, lane);
+  if (tallest.groups > 0) join<D>(tallest, L, lane);
+}
+
 bool divides(int64_t C, int64_t S) { return C + S > kPartKeys; }
+// whether some unit may have more entries than tiles of four waves are for
+bool has_tallest(int64_t entries, int D) { return D == 128 && entries > kTall; }
+size_t parts_bytes(int D) { return size_t(kSlots) * 32 * (D + 2) * sizeof(float); }
 
 template <int D>
 int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_t st) {
@@ -806,15 +964,27 @@ int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_
   a.per_xcd = int32_t(int64_t(a.per_seq) * a.pieces / kXcds);
   a.by_heads = div_by(a.Hkv);
   a.by_rep = div_by(a.rep);
-  const bool tall = int64_t(a.rep) * a.S > kShort;
+  const int64_t entries = int64_t(a.rep) * a.S;
+  const bool tall = entries > kShort, tallest = has_tallest(entries, D);
   const bool wide = !tall && int64_t(a.per_seq) * a.B <= 256;
   a.groups = wide ? 256 : 512;
+  a.above = 0;
+  a.up_to = tallest ? kTall : 1 << 30;
+  a.tall = kTall;
+  Q8AttnArgs b = a;
+  b.groups = tallest ? 256 : 0;
+  b.above = kTall;
+  b.up_to = 1 << 30;
+  b.tall = kTallest;
+  if (a.parts != nullptr) b.parts = a.parts + parts_bytes(D) / sizeof(float);
+  if constexpr (D == 128)
+    if (tallest) attn_q8_tall_kernel<D><<<b.groups, 512, 0, st>>>(b, L);
   if (tall) attn_q8_kernel<D, 4, true><<<a.groups, 256, 0, st>>>(a, L);
   else if (wide) attn_q8_kernel<D, 8, false><<<a.groups, 512, 0, st>>>(a, L);
   else attn_q8_kernel<D, 4, false><<<a.groups, 256, 0, st>>>(a, L);
   LSP_CHECK_LAUNCH("lsp_attn_step_q8: launch");
   if (a.parts != nullptr) {
-    join_kernel<D><<<512, 256, 0, st>>>(a, L);
+    join_kernel<D><<<512, 256, 0, st>>>(a, b, L);
     LSP_CHECK_LAUNCH("lsp_attn_step_q8: launch");
   }
   return LSP_OK;
@@ -848,7 +1018,7 @@ extern "C" size_t lsp_attn_q8_workspace_bytes(const lsp_attn_desc *d, int32_t nu
   using namespace lsp;
   AttnArgs c;
   if (check("lsp_attn_q8_workspace_bytes", d, num_layers, c) != LSP_OK) return 0;
-  return divides(c.C, c.S) ? size_t(kSlots) * 32 * (c.D + 2) * sizeof(float) : 0;
+  return divides(c.C, c.S) ? parts_bytes(c.D) * (has_tallest(int64_t(c.S) * (c.Hq / c.Hkv), c.D) ? 2 : 1) : 0;
 }
 
 extern "C" int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *d, int32_t num_layers, const void *const *q_layers, const void *const *k_suf_layers,
