@@ -63,7 +63,7 @@ struct Rows {
   int row;
   __device__ __forceinline__ Rows(const char *base, int64_t stride, int first, int valid, int bytes)
       : at(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + first * stride), 0,
-                                             __builtin_amdgcn_readfirstlane(max(valid - 1, 0) * int(stride) + bytes), 0x00020000)),
+                                             __builtin_amdgcn_readfirstlane(valid > 0 ? (valid - 1) * int(stride) + bytes : 0), 0x00020000)),
         row(int(stride)) {}
 };
 // 16, 8 or 4 bytes, `rows` (the same for all lanes) behind byte v.  FULL: all rows are there, and the distance is the instruction's scalar offset; how that counts
@@ -86,13 +86,19 @@ __device__ __forceinline__ int anew(int x) {
   return x;
 }
 
-__device__ __forceinline__ float quad_max(float x) {  // over the lanes l % 16
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+// over the lanes l % 16: rows of 16 lanes are exchanged, then halves
+template <typename F>
+__device__ __forceinline__ float quad(float x, F f) {
+  auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float quad_max(float x) {
+  return quad(x, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float quad_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  return quad(x, [](float a, float b) { return a + b; });
 }
 
 // ---- what there is to do ---------------------------------------------------------------
@@ -235,30 +241,79 @@ __device__ __forceinline__ float *part_stats(const Q8AttnArgs &a, int slot, int 
 // ---- short tiles -----------------------------------------------------------------------
 // Lanes l % 16 = r, l / 16 = h.  Of the keys: rows 16 k + r of the block, elements 64 i + 16 h of 16; of the values: rows 16 k + 4 h + e, of which
 // VJ elements from VJ r on.
+// A block of the cache comes to LDS by loads that go straight there, each of whole rows (as loads to registers, of which neighbouring lanes belong to
+// different rows, 16 x 21 rows on 1515 took 376 us), and stays the wave's own.  Its 16-byte pieces are exchanged, those of keys at p ^ (row / 2 % 8) (heads of 64: row / 4 % 4), the values' rows with
+// their neighbours where row / 4 is odd (heads of 64: at row ^ (row / 4 % 4)), so that what lanes read together lies in different banks.
 template <int D>
 struct Keys {
   static constexpr int KI = D / 64, KC = D / 32, VJ = D / 16;
+  static constexpr int kBytes = kQ8Block * D, kLoads = kBytes / 1024, kRows = 1024 / D;  // of a block's keys or values; loads; rows of one
   u32x4 kw[2][KI];
   uint32_t w[8][VJ / 4];
 
   // row of the block that element e (of eight) of a lane's values is of
   static __device__ __forceinline__ int value_row(int h, int e) { return 16 * (e >> 2) + 4 * h + (e & 3); }
 
-  // kv, vv: r * row + 16 h, 4 h * row + VJ r
-  template <bool FULL>
-  __device__ __forceinline__ void load(const Rows &k, const Rows &v, int kv, int vv) {
+  // The lane's part of load 0 (the others are kRows rows further on; of keys of 128, every other one has its pieces 4 apart).
+  static __device__ __forceinline__ int key_source(int lane, int row) {
+    return D == 128 ? lane / 8 * row + 16 * (lane % 8 ^ lane / 16) : lane / 4 * row + 16 * (lane % 4 ^ lane / 16);
+  }
+  static __device__ __forceinline__ int value_source(int lane, int row) {
+    const int p = D == 128 ? lane / 8 : lane / 4;
+    return (p ^ (D == 128 ? p >> 2 : p >> 2 & 3)) * row + 16 * (D == 128 ? lane % 8 : lane % 4);
+  }
+  typedef __attribute__((address_space(3))) void *Lds;
+  static __device__ __forceinline__ void ask_keys(const Rows &k, int source, char *to) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int i = 0; i < kLoads; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(k.at, (Lds)(to + 1024 * i), 16, (D == 128 && (i & 1) ? source ^ 64 : source) + i * kRows * k.row, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void ask_values(const Rows &v, int source, char *to) {
 #pragma unroll
-      for (int i = 0; i < KI; ++i) kw[b][i] = load16<FULL>(k, kv + 64 * i, 16 * b);
+    for (int i = 0; i < kLoads; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(v.at, (Lds)(to + 1024 * i), 16, source + i * kRows * v.row, 0, 0, 0);
+  }
+  // What a lane reads first, in bytes of a slot.
+  static __device__ __forceinline__ int key_place(int r, int h) { return D == 128 ? r * 128 + 16 * (h ^ r / 2 % 8) : r * 64 + 16 * (h ^ r / 4 % 4); }
+  static __device__ __forceinline__ int value_place(int r, int h) { return D == 128 ? 4 * h * 128 + 8 * r : 4 * h * 64 + 4 * r; }
+  // Waits for a block's keys (or values), behind which three times as many loads have been asked for, reads them and waits for that, in one.
+  template <int SLOT>
+  __device__ __forceinline__ void read_keys(uint32_t at) {
+    if constexpr (D == 128) {
+      asm volatile(
+          "s_waitcnt vmcnt(12)\n\tds_read_b128 %0, %4 offset:%6\n\tds_read_b128 %1, %5 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %5 offset:%7\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(kw[0][0]), "=&v"(kw[0][1]), "=&v"(kw[1][0]), "=&v"(kw[1][1])
+          : "v"(at), "v"(at ^ 64), "i"(SLOT * 2 * kBytes), "i"(SLOT * 2 * kBytes + 2048)
+          : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(6)\n\tds_read_b128 %0, %2 offset:%3\n\tds_read_b128 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                   : "=&v"(kw[0][0]), "=&v"(kw[1][0])
+                   : "v"(at), "i"(SLOT * 2 * kBytes), "i"(SLOT * 2 * kBytes + 1024)
+                   : "memory");
+    }
+  }
+  template <int SLOT>
+  __device__ __forceinline__ void read_values(uint32_t at, int h) {
+    constexpr int V = SLOT * 2 * kBytes + kBytes;
+    if constexpr (D == 128) {
+      const uint32_t a = at + 128 * (h & 1), b = at + 128 - 128 * (h & 1);
+      u32x2 x[8];
+      asm volatile(
+          "s_waitcnt vmcnt(12)\n\tds_read_b64 %0, %8 offset:%10\n\tds_read_b64 %1, %9 offset:%10\n\tds_read_b64 %2, %8 offset:%11\n\tds_read_b64 %3, %9 offset:%11\n\t"
+          "ds_read_b64 %4, %8 offset:%12\n\tds_read_b64 %5, %9 offset:%12\n\tds_read_b64 %6, %8 offset:%13\n\tds_read_b64 %7, %9 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+          : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+          : "v"(a), "v"(b), "i"(V), "i"(V + 256), "i"(V + 2048), "i"(V + 2304)
+          : "memory");
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (VJ == 8) {
-        const u32x2 x = load8<FULL>(v, vv, value_row(0, e));
-        w[e][0] = x[0], w[e][1] = x[1];
-      } else {
-        w[e][0] = load4<FULL>(v, vv, value_row(0, e));
-      }
+      for (int i = 0; i < 8; ++i) w[i][0] = x[i][0], w[i][1] = x[i][1];
+    } else {
+      const uint32_t a0 = at + 64 * h, a1 = at + 64 * (h ^ 1), a2 = at + 64 * (h ^ 2), a3 = at + 64 * (h ^ 3);
+      asm volatile(
+          "s_waitcnt vmcnt(6)\n\tds_read_b32 %0, %8 offset:%12\n\tds_read_b32 %1, %9 offset:%12\n\tds_read_b32 %2, %10 offset:%12\n\tds_read_b32 %3, %11 offset:%12\n\t"
+          "ds_read_b32 %4, %8 offset:%13\n\tds_read_b32 %5, %9 offset:%13\n\tds_read_b32 %6, %10 offset:%13\n\tds_read_b32 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+          : "=&v"(w[0][0]), "=&v"(w[1][0]), "=&v"(w[2][0]), "=&v"(w[3][0]), "=&v"(w[4][0]), "=&v"(w[5][0]), "=&v"(w[6][0]), "=&v"(w[7][0])
+          : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "i"(V), "i"(V + 1024)
+          : "memory");
     }
   }
   __device__ __forceinline__ bf16x8 key(int b, int c, float s) const {
@@ -295,6 +350,13 @@ struct Short {
       l[n] = 0.f;
     }
   }
+  // the queries are waited for here, not in a loop, where the wait would count what is under way by then
+  __device__ __forceinline__ void arrived() {
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int c = 0; c < KC; ++c) asm volatile("" : "+v"(q[n][c]));
+  }
   // scores of entries n -> probabilities; valid: keys of the block that there are
   __device__ __forceinline__ bf16x8 weigh(int n, f32x4 (&s)[2], float c, int valid, int h) {
     if (valid < kQ8Block)
@@ -320,7 +382,11 @@ struct Short {
     }
     return P;
   }
-  __device__ __forceinline__ void meet(const Keys<D> &x, float ks, float vs, float c, int valid, int h) {
+  // A block that is in a slot: keys(x) and values(x) read it and answer their scale; what follows it there is asked for as soon as it is in registers.
+  template <typename K, typename V>
+  __device__ __forceinline__ void meet(float c, int valid, int h, K keys, V values) {
+    Keys<D> x;
+    const float ks = keys(x);
     f32x4 s[NB][2];
 #pragma unroll
     for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -335,6 +401,7 @@ struct Short {
     bf16x8 P[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) P[n] = weigh(n, s[n], c, valid, h);
+    const float vs = values(x);
 #pragma unroll
     for (int p = 0; p < VJ / 4; ++p) {
       bf16x8 v[4];
@@ -386,11 +453,14 @@ struct Short {
   }
 };
 
-// LDS of a workgroup.  Short tiles: what its waves join.  Tall ones: four blocks' keys [32][D] and two steps' values [D][64], bf16.
+// LDS of a workgroup.  Short tiles: two blocks' keys and values of each wave, then what the waves join.  Tall ones: four blocks' keys [32][D] and two steps' values [D][64], bf16.
 template <int D, int WAVES>
-struct Joined {
-  f32x4 o[WAVES][D / 16][kWave];
-  float m[WAVES][16], l[WAVES][16];
+union Joined {
+  struct {
+    f32x4 o[WAVES][D / 16][kWave];
+    float m[WAVES][16], l[WAVES][16];
+  };
+  char slots[WAVES][4 * Keys<D>::kBytes];
 };
 template <int D>
 struct Staged {
@@ -401,31 +471,52 @@ template <int D, int NB, int WAVES>
 __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Joined<D, WAVES> &s, int lane, int wave) {
   constexpr int VJ = D / 16;
   const int r = lane & 15, h = lane >> 4;
+  // blocks of 32 keys: of the cache, the waves taking turns
+  const int row = int(a.cs[1]), k_source = Keys<D>::key_source(lane, row), v_source = Keys<D>::value_source(lane, row);
+  const int c_end = min(2 * min(t.to, t.cached), (t.P + kQ8Block - 1) / kQ8Block);
+  char *slots = s.slots[wave];
+  const uint32_t at = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)slots));
+  const uint32_t k_at = at + Keys<D>::key_place(r, h), v_at = at + Keys<D>::value_place(r, h);
+  // (beyond the last block the rows are none, and come as zeros: the waits count on as many loads everywhere)
+  auto ask_keys = [&](int i, int j) {
+    Keys<D>::ask_keys(Rows(u.kc, a.cs[1], min(j, c_end - 1) * kQ8Block, min(t.P - j * kQ8Block, j < c_end ? kQ8Block : 0), D), anew(k_source),
+                      slots + i * 2 * Keys<D>::kBytes);
+  };
+  auto ask_values = [&](int i, int j) {
+    Keys<D>::ask_values(Rows(u.vc, a.cs[1], min(j, c_end - 1) * kQ8Block, min(t.P - j * kQ8Block, j < c_end ? kQ8Block : 0), D), anew(v_source),
+                        slots + i * 2 * Keys<D>::kBytes + Keys<D>::kBytes);
+  };
+  int j = 2 * t.from + wave;
   Short<D, NB> x;
   x.start(a, u.q, t.entry, t.entries, r, h);
-  // blocks of 32 keys: of the cache, the waves taking turns, the next one on its way while one is met
-  const int row = int(a.cs[1]), kv = r * row + 16 * h, vv = 4 * h * row + VJ * r;
-  const int c_end = min(2 * min(t.to, t.cached), (t.P + kQ8Block - 1) / kQ8Block);
-  int j = 2 * t.from + wave;
-  if (j < c_end) {
-    Keys<D> next;
-    auto load = [&](int j) {
-      const int valid = min(t.P - j * kQ8Block, kQ8Block);
-      const Rows k(u.kc, a.cs[1], j * kQ8Block, valid, D), v(u.vc, a.cs[1], j * kQ8Block, valid, D);
-      if (valid == kQ8Block) next.template load<true>(k, v, kv, vv);
-      else next.template load<false>(k, v, anew(kv), anew(vv));
+  while (j < c_end) {  // 64 of the wave's blocks at a time: lane i has the exponents of the i-th
+    const int first = j, end = min(c_end, j + kWave * WAVES), mine = min(j + lane * WAVES, c_end - 1);
+    uint32_t ke = u.ke[mine], ve = u.ve[mine];
+    ask_keys(0, j), ask_values(0, j), ask_keys(1, j + WAVES), ask_values(1, j + WAVES);
+    asm volatile("" : "+v"(ke), "+v"(ve));
+    x.arrived();
+    auto meet = [&](auto slot) {
+      constexpr int I = decltype(slot)::value;
+      const int n = (j - first) / WAVES;
+      x.meet(a.c, t.P - j * kQ8Block, h,
+             [&](Keys<D> &k) {
+               k.template read_keys<I>(k_at);
+               ask_keys(I, j + 2 * WAVES);
+               return q8_scale(__builtin_amdgcn_readlane(ke, n));
+             },
+             [&](Keys<D> &k) {
+               k.template read_values<I>(v_at, h);
+               ask_values(I, j + 2 * WAVES);
+               return q8_scale(__builtin_amdgcn_readlane(ve, n));
+             });
     };
-    load(j);
-    float ks = q8_scale(u.ke[j]), vs = q8_scale(u.ve[j]);
-    for (; j < c_end; j += WAVES) {
-      const Keys<D> now = next;
-      const float ks0 = ks, vs0 = vs;
-      if (j + WAVES < c_end) {
-        load(j + WAVES);
-        ks = q8_scale(u.ke[j + WAVES]), vs = q8_scale(u.ve[j + WAVES]);
-      }
-      x.meet(now, ks0, vs0, a.c, t.P - j * kQ8Block, h);
+    for (;;) {
+      meet(std::integral_constant<int, 0>());
+      if ((j += WAVES) >= end) break;
+      meet(std::integral_constant<int, 1>());
+      if ((j += WAVES) >= end) break;
     }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing comes to the slots any more
   }
   // of the suffix
   const int s_end = min(2 * (t.to - t.cached), (t.N + kQ8Block - 1) / kQ8Block);
@@ -436,6 +527,7 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, c
   }
 
   // The waves' parts: what all have in a place of their lanes is added by one of them.
+  __syncthreads();
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const float l = quad_sum(x.l[n]);
@@ -868,7 +960,7 @@ __device__ __forceinline__ void all_items(const Q8AttnArgs &a, const Q8Layers &L
 // Short tiles, and (TALL) tall ones of four waves.
 template <int D, int WAVES, bool TALL>
 __global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a, Q8Layers L) {
-  union Shared {
+  union alignas(1024) Shared {
     Joined<D, WAVES> joined;
     Staged<TALL ? D : 64> staged;
     __device__ Shared() {}
