@@ -27,13 +27,18 @@ constexpr int kTall = 128;       // entries up to which, beyond that, a tile has
 constexpr int kTallest = 256;    // entries of a tile of the others (heads of 128)
 constexpr int kXcds = 8;
 constexpr int kSlots = 2048;     // parts of 32 entries in the workspace, for each of two kernels
-constexpr int kPartKeys = 1024;  // C + S beyond which keys are divided at all
+constexpr int kPartKeys = 2048;  // C + S beyond which keys are divided at all: one row on 2000 keys takes 16.8 us in one part and 17.0 in several, on 4000 keys 27.5 and 19.4
 constexpr int kLeast = 4;        // steps of a part, at least
+constexpr int kOnce = 2;         // of a buffer read: nontemporal, the caches need not keep it
+// Steps of all short tiles from which on a workgroup's waves have up to four heads beside each other.  A row of the cache holds a head's 128 bytes beside the next one's: four
+// waves that read the same rows fetch 512 bytes in a piece (21 rows each on 533 keys of 16 sequences, 8 layers: 302 us where a workgroup's waves divide the keys
+// of one head among themselves 362).  With less to do the waves divide the keys, so that more of them work.
+constexpr float kBeside = 8192;
 
 struct Q8AttnArgs {
   const int32_t *prefix_len, *suffix_len;
   int32_t B, S, Hkv, C, rep, blocks, per_seq;  // per_seq: units of a sequence, layers * Hkv
-  int32_t pieces, per_xcd;                     // each unit's items are dealt out to `pieces` lists, of which every XCD has per_xcd of a sequence
+  int32_t heads;                               // log2 of the heads that a short tile's workgroup may have beside each other
   int32_t groups;                              // workgroups
   int32_t above, up_to, tall;                  // entries of the units that are this kernel's; of a tall tile
   float c;                                     // scale log2(e)
@@ -123,68 +128,78 @@ __device__ __forceinline__ Lens lens_of(const Q8AttnArgs &a, int b) {
   return {min(max(a.suffix_len[b], 0), a.S), min(max(a.prefix_len[b], 0), a.C)};
 }
 __device__ __forceinline__ int first_lane(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) x += __shfl_xor(x, m);
-  return first_lane(x);
+__device__ __forceinline__ int at_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
+// What f makes of lanes 0 to l, in lane l; f(x, none) = x.  By moves between lanes in registers: a plan's sums through LDS were 2 us of a call.
+template <int MOVE, int ROWS, typename F>
+__device__ __forceinline__ int meet_lane(int x, int none, F f) {
+  return f(x, __builtin_amdgcn_update_dpp(none, x, MOVE, ROWS, 0xf, false));
 }
-__device__ __forceinline__ int running_sum(int x, int lane) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) {
-    const int y = __shfl_up(x, m);
-    x += lane >= m ? y : 0;
-  }
-  return x;
+template <typename F>
+__device__ __forceinline__ int running(int x, int none, F f) {
+  x = meet_lane<0x111, 0xf>(x, none, f);  // within 16 lanes from 1, 2, 4, 8 below
+  x = meet_lane<0x112, 0xf>(x, none, f);
+  x = meet_lane<0x114, 0xf>(x, none, f);
+  x = meet_lane<0x118, 0xf>(x, none, f);
+  x = meet_lane<0x142, 0xa>(x, none, f);  // lane 15 of the 16 below, then lane 31
+  return meet_lane<0x143, 0xc>(x, none, f);
 }
+__device__ __forceinline__ int running_sum(int x) {
+  return running(x, 0, [](int p, int q) { return p + q; });
+}
+__device__ __forceinline__ int wave_sum(int x) { return at_lane(running_sum(x), kWave - 1); }
 
 // The sequences, 64 at a time, a lane each.
 struct Plan {
   int chunk;          // steps of an item, at most
+  int heads;          // log2 of the heads of a short item
   bool split;         // whether some tile is more than one item
   int b0;             // the first of the sequences that the lanes have
   Lens n;
   int end, base;      // running sum of the items of an XCD, those of sequences before b0
   int slot_end, slot_base;  // the same of the parts of 32 entries
 
+  __device__ __forceinline__ int heads_of(const Shape &s) const { return s.rows > 32 ? 0 : heads; }
+  // Items are dealt out to the XCDs by unit (of a short tile: by its heads); where a sequence's units are no multiple of 8, each unit's items to 2^pieces of them.
+  __device__ __forceinline__ static int pieces_of(int units) { return 3 - min(__builtin_ctz(units), 3); }
   __device__ __forceinline__ int splits_of(const Shape &s) const { return split ? (s.steps + chunk - 1) / chunk : 1; }  // of a tile
   __device__ __forceinline__ void take(const Q8AttnArgs &a, int lane) {
     n = lens_of(a, b0 + lane);
     const Shape s = shape_of(a, n);
-    const int items = s.tiles * splits_of(s);
-    end = running_sum(a.per_xcd * ((items + a.pieces - 1) / a.pieces), lane);
-    slot_end = split ? running_sum(a.per_seq * items * ((s.rows + 31) / 32), lane) : 0;
+    const int items = s.tiles * splits_of(s), units = a.per_seq >> heads_of(s), pieces = pieces_of(units);
+    end = running_sum((units << pieces) / kXcds * ((items + (1 << pieces) - 1) >> pieces));
+    slot_end = split ? running_sum(a.per_seq * items * ((s.rows + 31) / 32)) : 0;
   }
   // How long the items are: all keys of a tile, or, where workgroups would be without one, part of them.  Lane i looks at i + 1 parts (from 32 on at
   // multiples of 8).  A round of items takes its steps and about four steps' time to begin and end, joining the parts as much again.
   __device__ __forceinline__ void start(const Q8AttnArgs &a, int lane) {
     chunk = 1 << 30;
     split = false;
-    if (a.parts != nullptr) {
-      int tiles = 0, slots = 0, most = 0;
+    heads = 0;
+    if (a.parts != nullptr || a.heads > 0) {
+      int all = 0, slots = 0, most = 0;
+      float work = 0.f;
       for (int b = 0; b < a.B; b += kWave) {
         const Shape x = shape_of(a, lens_of(a, b + lane));
-        tiles += a.per_seq * x.tiles;
+        all += a.per_seq * x.tiles;
         slots += a.per_seq * x.tiles * ((x.rows + 31) / 32);
         most = max(most, x.tiles > 0 ? x.steps : 0);
+        work += x.rows > 32 ? 0.f : float(a.per_seq * x.tiles) * float(x.steps);
       }
-      tiles = wave_sum(tiles);
+      all = wave_sum(all);
       slots = wave_sum(slots);
-#pragma unroll
-      for (int m = 1; m < kWave; m <<= 1) most = max(most, __shfl_xor(most, m));
-      if (tiles > 0 && slots <= kSlots / 2) {
+      most = at_lane(running(most, 0, [](int p, int q) { return max(p, q); }), kWave - 1);
+      const int total = at_lane(running(__float_as_int(work), 0, [](int p, int q) { return __float_as_int(__int_as_float(p) + __int_as_float(q)); }), kWave - 1);
+      if (__int_as_float(total) >= kBeside) heads = a.heads;
+      const int tiles = (all + (1 << heads) - 1) >> heads;
+      if (a.parts != nullptr && tiles > 0 && slots <= kSlots / 2) {
         const int k = lane < 32 ? lane + 1 : 32 + 8 * (lane - 31), part = (most + k - 1) / k;
         const bool fits = k == 1 || (int64_t(slots) * k <= kSlots && part >= kLeast);
-        int cost = fits ? int((int64_t(tiles) * k + a.groups - 1) / a.groups) * (part + 4) + (k > 1 ? 4 + k / 8 : 0) : 1 << 29;
-        int best = lane;
-#pragma unroll
-        for (int m = 1; m < kWave; m <<= 1) {
-          const int c = __shfl_xor(cost, m), l = __shfl_xor(best, m);
-          if (c < cost || (c == cost && l < best)) cost = c, best = l;
-        }
-        best = first_lane(best);
+        const int64_t rounds = (int64_t(tiles) * k + a.groups - 1) / a.groups, cost = rounds * ((part << heads) + 4) + (k > 1 ? 4 + k / 8 : 0);
+        const int least = fits ? int(min(cost, int64_t(1) << 24)) * kWave + lane : 0x7fffffff;
+        const int best = at_lane(running(least, 0x7fffffff, [](int p, int q) { return min(p, q); }), kWave - 1) % kWave;
         if (best > 0) {
           const int k2 = best < 32 ? best + 1 : 32 + 8 * (best - 31);
-          chunk = (first_lane(most) + k2 - 1) / k2;
+          chunk = (most + k2 - 1) / k2;
           split = true;
         }
       }
@@ -205,12 +220,12 @@ struct Plan {
     }
   }
 };
-__device__ __forceinline__ int at_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
 
 struct Item {
   int b, l, g, N, P, entries, entry, rows;
   int from, to, cached;  // steps
-  int slot;              // of its part, or -1: the item is all of a tile
+  int slot, next_slot;   // of its part, or -1: the item is all of a tile; how much further that of a short tile's next head is
+  int heads;             // log2 of the heads of a short item
 };
 
 // Where a unit's rows are.
@@ -219,12 +234,13 @@ struct Unit {
   const uint8_t *ke, *ve;
   char *out;
   __device__ __forceinline__ Unit(const Q8AttnArgs &a, const Q8Layers &L, const Item &t) {
-    q = L.q[t.l] + t.b * a.qs[0] + t.g * a.rep * a.qs[2];
-    out = L.out[t.l] + t.b * a.os[0] + t.g * a.rep * a.os[2];
+    const Q8Layer &of = L.of[t.l];
     const int64_t c = t.b * a.cs[0] + t.g * a.cs[2], s = t.b * a.ks[0] + t.g * a.ks[2], e = (int64_t(t.b) * a.Hkv + t.g) * a.blocks;
-    kc = L.k_cache[t.l] + c; vc = L.v_cache[t.l] + c;
-    ks = L.k_suf[t.l] + s; vs = L.v_suf[t.l] + s;
-    ke = L.k_scale[t.l] + e; ve = L.v_scale[t.l] + e;
+    q = of.q + t.b * a.qs[0] + t.g * a.rep * a.qs[2];
+    out = of.out + t.b * a.os[0] + t.g * a.rep * a.os[2];
+    kc = of.k_cache + c; vc = of.v_cache + c;
+    ks = of.k_suf + s; vs = of.v_suf + s;
+    ke = of.k_scale + e; ve = of.v_scale + e;
   }
 };
 // entry e of a unit: its row and head
@@ -263,14 +279,17 @@ struct Keys {
     return (p ^ (D == 128 ? p >> 2 : p >> 2 & 3)) * row + 16 * (D == 128 ? lane % 8 : lane % 4);
   }
   typedef __attribute__((address_space(3))) void *Lds;
+  template <bool ONCE>
   static __device__ __forceinline__ void ask_keys(const Rows &k, int source, char *to) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(k.at, (Lds)(to + 1024 * i), 16, (D == 128 && (i & 1) ? source ^ 64 : source) + i * kRows * k.row, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(k.at, (Lds)(to + 1024 * i), 16, (D == 128 && (i & 1) ? source ^ 64 : source) + i * kRows * k.row, 0, 0,
+                                               ONCE ? kOnce : 0);
   }
+  template <bool ONCE>
   static __device__ __forceinline__ void ask_values(const Rows &v, int source, char *to) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(v.at, (Lds)(to + 1024 * i), 16, source + i * kRows * v.row, 0, 0, 0);
+    for (int i = 0; i < kLoads; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(v.at, (Lds)(to + 1024 * i), 16, source + i * kRows * v.row, 0, 0, ONCE ? kOnce : 0);
   }
   // What a lane reads first, in bytes of a slot.
   static __device__ __forceinline__ int key_place(int r, int h) { return D == 128 ? r * 128 + 16 * (h ^ r / 2 % 8) : r * 64 + 16 * (h ^ r / 4 % 4); }
@@ -467,9 +486,13 @@ struct Staged {
   uint32_t k[4][kQ8Block * D / 2], v[2][kStep * D / 2];
 };
 
-template <int D, int NB, int WAVES>
-__device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Joined<D, WAVES> &s, int lane, int wave) {
+template <int D, int NB, int WAVES, bool ONCE>
+__device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Q8Layers &L, Item t, Joined<D, WAVES> &s, int lane, int wave) {
   constexpr int VJ = D / 16;
+  const int sub = wave & ((1 << t.heads) - 1), turn = wave >> t.heads, turns = WAVES >> t.heads;
+  t.g += sub;
+  t.slot += sub * t.next_slot;
+  const Unit u(a, L, t);
   const int r = lane & 15, h = lane >> 4;
   // blocks of 32 keys: of the cache, the waves taking turns
   const int row = int(a.cs[1]), k_source = Keys<D>::key_source(lane, row), v_source = Keys<D>::value_source(lane, row);
@@ -479,48 +502,48 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, c
   const uint32_t k_at = at + Keys<D>::key_place(r, h), v_at = at + Keys<D>::value_place(r, h);
   // (beyond the last block the rows are none, and come as zeros: the waits count on as many loads everywhere)
   auto ask_keys = [&](int i, int j) {
-    Keys<D>::ask_keys(Rows(u.kc, a.cs[1], min(j, c_end - 1) * kQ8Block, min(t.P - j * kQ8Block, j < c_end ? kQ8Block : 0), D), anew(k_source),
+    Keys<D>::template ask_keys<ONCE>(Rows(u.kc, a.cs[1], min(j, c_end - 1) * kQ8Block, min(t.P - j * kQ8Block, j < c_end ? kQ8Block : 0), D), anew(k_source),
                       slots + i * 2 * Keys<D>::kBytes);
   };
   auto ask_values = [&](int i, int j) {
-    Keys<D>::ask_values(Rows(u.vc, a.cs[1], min(j, c_end - 1) * kQ8Block, min(t.P - j * kQ8Block, j < c_end ? kQ8Block : 0), D), anew(v_source),
+    Keys<D>::template ask_values<ONCE>(Rows(u.vc, a.cs[1], min(j, c_end - 1) * kQ8Block, min(t.P - j * kQ8Block, j < c_end ? kQ8Block : 0), D), anew(v_source),
                         slots + i * 2 * Keys<D>::kBytes + Keys<D>::kBytes);
   };
-  int j = 2 * t.from + wave;
+  int j = 2 * t.from + turn;
   Short<D, NB> x;
   x.start(a, u.q, t.entry, t.entries, r, h);
   while (j < c_end) {  // 64 of the wave's blocks at a time: lane i has the exponents of the i-th
-    const int first = j, end = min(c_end, j + kWave * WAVES), mine = min(j + lane * WAVES, c_end - 1);
+    int n = 0;
+    const int end = min(c_end, j + kWave * turns), mine = min(j + lane * turns, c_end - 1);
     uint32_t ke = u.ke[mine], ve = u.ve[mine];
-    ask_keys(0, j), ask_values(0, j), ask_keys(1, j + WAVES), ask_values(1, j + WAVES);
+    ask_keys(0, j), ask_values(0, j), ask_keys(1, j + turns), ask_values(1, j + turns);
     asm volatile("" : "+v"(ke), "+v"(ve));
     x.arrived();
     auto meet = [&](auto slot) {
       constexpr int I = decltype(slot)::value;
-      const int n = (j - first) / WAVES;
       x.meet(a.c, t.P - j * kQ8Block, h,
              [&](Keys<D> &k) {
                k.template read_keys<I>(k_at);
-               ask_keys(I, j + 2 * WAVES);
+               ask_keys(I, j + 2 * turns);
                return q8_scale(__builtin_amdgcn_readlane(ke, n));
              },
              [&](Keys<D> &k) {
                k.template read_values<I>(v_at, h);
-               ask_values(I, j + 2 * WAVES);
+               ask_values(I, j + 2 * turns);
                return q8_scale(__builtin_amdgcn_readlane(ve, n));
              });
     };
     for (;;) {
       meet(std::integral_constant<int, 0>());
-      if ((j += WAVES) >= end) break;
+      if (++n, (j += turns) >= end) break;
       meet(std::integral_constant<int, 1>());
-      if ((j += WAVES) >= end) break;
+      if (++n, (j += turns) >= end) break;
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing comes to the slots any more
   }
   // of the suffix
   const int s_end = min(2 * (t.to - t.cached), (t.N + kQ8Block - 1) / kQ8Block);
-  for (int i = 2 * max(t.from - t.cached, 0) + (WAVES - 1 - wave); i < s_end; i += WAVES) {
+  for (int i = 2 * max(t.from - t.cached, 0) + (turns - 1 - turn); i < s_end; i += turns) {
     const int valid = t.N - i * kQ8Block;
     x.meet_suffix(Rows(u.ks, a.ks[1], i * kQ8Block, min(valid, kQ8Block), 2 * D), Rows(u.vs, a.ks[1], i * kQ8Block, min(valid, kQ8Block), 2 * D), a.c, valid,
                   r, h);
@@ -535,11 +558,9 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, c
     if (h == 0) s.m[wave][r] = x.m[n], s.l[wave][r] = l;
     __syncthreads();
     float m = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s.m[w][r]);
+    for (int w = sub; w < WAVES; w += 1 << t.heads) m = fmaxf(m, s.m[w][r]);
     // (a wave that met no key has zeros)
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += s.l[w][r] != 0.f ? s.l[w][r] * __builtin_amdgcn_exp2f(s.m[w][r] - m) : 0.f;
+    for (int w = sub; w < WAVES; w += 1 << t.heads) sum += s.l[w][r] != 0.f ? s.l[w][r] * __builtin_amdgcn_exp2f(s.m[w][r] - m) : 0.f;
     const float f = l != 0.f ? __builtin_amdgcn_exp2f(x.m[n] - m) : 0.f;
 #pragma unroll
     for (int p = 0; p < VJ; ++p) {  // elements 4 p to 4 p + 3 of the lane's 4 VJ
@@ -551,10 +572,9 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Unit &u, c
     __syncthreads();
     const int e = 16 * n + r;
     if (t.entry + e < t.entries) {
-      for (int p = wave; p < VJ; p += WAVES) {
-        f32x4 y = s.o[0][p][lane];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) y += s.o[w][p][lane];
+      for (int p = turn; p < VJ; p += turns) {
+        f32x4 y = s.o[sub][p][lane];
+        for (int w = sub + (1 << t.heads); w < WAVES; w += 1 << t.heads) y += s.o[w][p][lane];
         const int d = 4 * VJ * h + 4 * p;
         if (t.slot < 0) {
           const float inv = 1.f / sum;
@@ -917,8 +937,7 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
 
 // ---- kernels ---------------------------------------------------------------------------
 // Workgroups that stay, and take every groups / 8-th item of their XCD's list.  In it: sequences; of a sequence this XCD's share of its units (so that what
-// meets the same keys shares an L2); of a unit its tiles, their parts.  Where a sequence's units are no multiple of 8, each unit's items are dealt out to
-// `pieces` XCDs.  does(item, unit)
+// meets the same keys shares an L2); of a unit its tiles, their parts.  does(item)
 template <typename F>
 __device__ __forceinline__ void all_items(const Q8AttnArgs &a, const Q8Layers &L, int lane, F does) {
   const int xcd = blockIdx.x % kXcds, stride = a.groups / kXcds;
@@ -937,10 +956,12 @@ __device__ __forceinline__ void all_items(const Q8AttnArgs &a, const Q8Layers &L
     t.cached = shape.cached;
     const int splits = plan.splits_of(shape), items = shape.tiles * splits;
     const int before = plan.base + (at > 0 ? at_lane(plan.end, max(at - 1, 0)) : 0), in_seq = q - before;
-    const int per_piece = (items + a.pieces - 1) / a.pieces, piece = in_seq / per_piece;
-    const int list = piece * kXcds + xcd, unit = list / a.pieces, item = (in_seq - piece * per_piece) * a.pieces + list % a.pieces;
+    const int heads = plan.heads_of(shape), pieces = plan.pieces_of(a.per_seq >> heads);
+    const int per_piece = (items + (1 << pieces) - 1) >> pieces, piece = in_seq / per_piece, list = piece * kXcds + xcd;
+    const int unit = (list >> pieces) << heads, item = ((in_seq - piece * per_piece) << pieces) + (list & ((1 << pieces) - 1));
     if (item >= items) continue;
     t.b = first_lane(t.b);
+    t.heads = heads;
     t.l = first_lane(quotient(unit, a.by_heads));
     t.g = first_lane(unit - t.l * a.Hkv);
     const int tile = item / splits, part = item - tile * splits;
@@ -948,11 +969,13 @@ __device__ __forceinline__ void all_items(const Q8AttnArgs &a, const Q8Layers &L
     t.from = first_lane(part * plan.chunk);
     t.to = splits == 1 ? shape.steps : min(t.from + plan.chunk, shape.steps);
     t.slot = -1;
+    t.next_slot = 0;
     if (splits > 1) {
       const int slots = plan.slot_base + (at > 0 ? at_lane(plan.slot_end, max(at - 1, 0)) : 0);
       t.slot = slots + (unit * items + item) * ((t.rows + 31) / 32);
+      t.next_slot = items;  // (of a short tile: that of the next head)
     }
-    does(t, Unit(a, L, t));
+    does(t);
     __syncthreads();
   }
 }
@@ -967,14 +990,15 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a,
   };
   __shared__ Shared s;
   const int lane = threadIdx.x & (kWave - 1), wave = first_lane(threadIdx.x / kWave);
-  all_items(a, L, lane, [&](const Item &t, const Unit &u) {
+  all_items(a, L, lane, [&](const Item &t) {
     const int own = anew(lane);  // (what an item makes of it is not kept for the next one, in registers that the other kinds of items need)
     if (TALL && t.rows > 32) {
-      if constexpr (TALL) tall_item<D, WAVES>(a, u, t, s.staged, own, wave);
+      if constexpr (TALL) tall_item<D, WAVES>(a, Unit(a, L, t), t, s.staged, own, wave);
     } else if (t.rows == 32) {
-      short_item<D, 2, WAVES>(a, u, t, s.joined, own, wave);
+      if (t.entries <= 32) short_item<D, 2, WAVES, true>(a, L, t, s.joined, own, wave);
+      else short_item<D, 2, WAVES, false>(a, L, t, s.joined, own, wave);
     } else {
-      short_item<D, 1, WAVES>(a, u, t, s.joined, own, wave);
+      short_item<D, 1, WAVES, true>(a, L, t, s.joined, own, wave);
     }
   });
 }
@@ -983,7 +1007,7 @@ template <int D>
 __global__ __launch_bounds__(512, 2) void attn_q8_tall_kernel(Q8AttnArgs a, Q8Layers L) {
   __shared__ Staged<D> s;
   const int lane = threadIdx.x & (kWave - 1), wave = first_lane(threadIdx.x / kWave);
-  all_items(a, L, lane, [&](const Item &t, const Unit &u) { tall_item<D, 8>(a, u, t, s, anew(lane), wave); });
+  all_items(a, L, lane, [&](const Item &t) { tall_item<D, 8>(a, Unit(a, L, t), t, s, anew(lane), wave); });
 }
 
 // The parts of divided tiles, joined: a wave to an entry.
@@ -999,7 +1023,7 @@ __device__ __forceinline__ void join(const Q8AttnArgs &a, const Q8Layers &L, int
     plan.b0 = b0;
     plan.take(a, lane);
     const Shape mine = shape_of(a, plan.n);
-    const int n = a.per_seq * mine.entries, splits_mine = plan.splits_of(mine), end = running_sum(n, lane), all = at_lane(end, kWave - 1);
+    const int n = a.per_seq * mine.entries, splits_mine = plan.splits_of(mine), end = running_sum(n), all = at_lane(end, kWave - 1);
     for (; first < before + all; first += waves) {
       const int at = __builtin_ctzll(__ballot(first < before + end));
       const int entries = at_lane(mine.entries, at), splits = at_lane(splits_mine, at), rows = at_lane(mine.rows, at), tiles = at_lane(mine.tiles, at);
@@ -1051,9 +1075,7 @@ template <int D>
 int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_t st) {
   Q8AttnArgs a = args;
   a.per_seq = layers * a.Hkv;
-  a.pieces = 1;
-  while ((int64_t(a.per_seq) * a.pieces) % kXcds != 0) a.pieces *= 2;
-  a.per_xcd = int32_t(int64_t(a.per_seq) * a.pieces / kXcds);
+  a.heads = a.Hkv % 4 == 0 ? 2 : a.Hkv % 2 == 0 ? 1 : 0;
   a.by_heads = div_by(a.Hkv);
   a.by_rep = div_by(a.rep);
   const int64_t entries = int64_t(a.rep) * a.S;
@@ -1145,11 +1167,11 @@ extern "C" int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *d, int32_t num_l
     const int nl = num_layers - l0 < kMaxAttnLayers ? num_layers - l0 : kMaxAttnLayers;
     Q8Layers L = {};
     for (int l = 0; l < nl; ++l) {
-      L.q[l] = static_cast<const char *>(q_layers[l0 + l]);
-      L.k_suf[l] = static_cast<const char *>(k_suf_layers[l0 + l]); L.v_suf[l] = static_cast<const char *>(v_suf_layers[l0 + l]);
-      L.k_cache[l] = static_cast<char *>(const_cast<void *>(k_cache_layers[l0 + l])); L.v_cache[l] = static_cast<char *>(const_cast<void *>(v_cache_layers[l0 + l]));
-      L.k_scale[l] = static_cast<uint8_t *>(const_cast<void *>(k_scale_layers[l0 + l])); L.v_scale[l] = static_cast<uint8_t *>(const_cast<void *>(v_scale_layers[l0 + l]));
-      L.out[l] = static_cast<char *>(out_layers[l0 + l]);
+      L.of[l].q = static_cast<const char *>(q_layers[l0 + l]);
+      L.of[l].k_suf = static_cast<const char *>(k_suf_layers[l0 + l]); L.of[l].v_suf = static_cast<const char *>(v_suf_layers[l0 + l]);
+      L.of[l].k_cache = static_cast<char *>(const_cast<void *>(k_cache_layers[l0 + l])); L.of[l].v_cache = static_cast<char *>(const_cast<void *>(v_cache_layers[l0 + l]));
+      L.of[l].k_scale = static_cast<uint8_t *>(const_cast<void *>(k_scale_layers[l0 + l])); L.of[l].v_scale = static_cast<uint8_t *>(const_cast<void *>(v_scale_layers[l0 + l]));
+      L.of[l].out = static_cast<char *>(out_layers[l0 + l]);
     }
     const int32_t r = c.D == 64 ? launch<64>(a, L, nl, static_cast<hipStream_t>(stream)) : launch<128>(a, L, nl, static_cast<hipStream_t>(stream));
     if (r != LSP_OK) return r;

@@ -104,9 +104,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(KvArgs a, Q8Layers L) 
   const int P = min(max(a.to[b], 0), a.C), n = min(min(max(a.from[b], 0), a.S), P), P0 = P - n;
   if (n == 0) return;
   const bool values = blockIdx.y & 1;
-  const char *suf = (values ? L.v_suf[l] : L.k_suf[l]) + b * a.ss[0];
-  char *cache = (values ? L.v_cache[l] : L.k_cache[l]) + b * a.cs[0];
-  uint8_t *scales = (values ? L.v_scale[l] : L.k_scale[l]) + int64_t(b) * a.Hkv * a.blocks;
+  const char *suf = (values ? L.of[l].v_suf : L.of[l].k_suf) + b * a.ss[0];
+  char *cache = (values ? L.of[l].v_cache : L.of[l].k_cache) + b * a.cs[0];
+  uint8_t *scales = (values ? L.of[l].v_scale : L.of[l].k_scale) + int64_t(b) * a.Hkv * a.blocks;
   const int first = P0 / kQ8Block, items = ((P - 1) / kQ8Block - first + 1) * a.Hkv;
   const int r = lane / kLanes, d = (lane % kLanes) * 8;
   for (int it = blockIdx.x * kWaves + threadIdx.x / kWave; it < items; it += gridDim.x * kWaves) {
@@ -177,9 +177,9 @@ __global__ __launch_bounds__(kThreads) void read_kernel(KvArgs a, Q8Layers L) {
   const int b = blockIdx.z, l = blockIdx.y >> 1;
   const int first = min(max(a.from[b], 0), a.C), end = min(max(a.to[b], first), a.C), n = min(end - first, a.S);
   const bool values = blockIdx.y & 1;
-  char *out = (values ? L.out[l] : const_cast<char *>(L.q[l])) + b * a.ss[0];
-  const char *cache = (values ? L.v_cache[l] : L.k_cache[l]) + b * a.cs[0];
-  const uint8_t *scales = (values ? L.v_scale[l] : L.k_scale[l]) + int64_t(b) * a.Hkv * a.blocks;
+  char *out = (values ? L.of[l].out : const_cast<char *>(L.of[l].q)) + b * a.ss[0];
+  const char *cache = (values ? L.of[l].v_cache : L.of[l].k_cache) + b * a.cs[0];
+  const uint8_t *scales = (values ? L.of[l].v_scale : L.of[l].k_scale) + int64_t(b) * a.Hkv * a.blocks;
   const int d = (threadIdx.x % kLanes) * 16;
   const int64_t items = int64_t(n) * a.Hkv;
   for (int64_t it = int64_t(blockIdx.x) * kHeads + threadIdx.x / kLanes; it < items; it += int64_t(gridDim.x) * kHeads) {
@@ -234,9 +234,9 @@ extern "C" int32_t lsp_kv_append_q8(const lsp_attn_desc *d, int32_t num_layers, 
     const int nl = num_layers - l0 < kMaxAttnLayers ? num_layers - l0 : kMaxAttnLayers;
     Q8Layers L = {};
     for (int l = 0; l < nl; ++l) {
-      L.k_suf[l] = static_cast<const char *>(k_suf_layers[l0 + l]); L.v_suf[l] = static_cast<const char *>(v_suf_layers[l0 + l]);
-      L.k_cache[l] = static_cast<char *>(k_cache_layers[l0 + l]); L.v_cache[l] = static_cast<char *>(v_cache_layers[l0 + l]);
-      L.k_scale[l] = static_cast<uint8_t *>(k_scale_layers[l0 + l]); L.v_scale[l] = static_cast<uint8_t *>(v_scale_layers[l0 + l]);
+      L.of[l].k_suf = static_cast<const char *>(k_suf_layers[l0 + l]); L.of[l].v_suf = static_cast<const char *>(v_suf_layers[l0 + l]);
+      L.of[l].k_cache = static_cast<char *>(k_cache_layers[l0 + l]); L.of[l].v_cache = static_cast<char *>(v_cache_layers[l0 + l]);
+      L.of[l].k_scale = static_cast<uint8_t *>(k_scale_layers[l0 + l]); L.of[l].v_scale = static_cast<uint8_t *>(v_scale_layers[l0 + l]);
     }
     const dim3 grid = grid_of(k, nl, most);
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -277,9 +277,9 @@ extern "C" int32_t lsp_kv_read_q8(const lsp_attn_desc *d, int32_t num_layers, co
     const int nl = num_layers - l0 < kMaxAttnLayers ? num_layers - l0 : kMaxAttnLayers;
     Q8Layers L = {};
     for (int l = 0; l < nl; ++l) {
-      L.k_cache[l] = static_cast<char *>(const_cast<void *>(k_cache_layers[l0 + l])); L.v_cache[l] = static_cast<char *>(const_cast<void *>(v_cache_layers[l0 + l]));
-      L.k_scale[l] = static_cast<uint8_t *>(const_cast<void *>(k_scale_layers[l0 + l])); L.v_scale[l] = static_cast<uint8_t *>(const_cast<void *>(v_scale_layers[l0 + l]));
-      L.q[l] = static_cast<char *>(k_out_layers[l0 + l]); L.out[l] = static_cast<char *>(v_out_layers[l0 + l]);
+      L.of[l].k_cache = static_cast<char *>(const_cast<void *>(k_cache_layers[l0 + l])); L.of[l].v_cache = static_cast<char *>(const_cast<void *>(v_cache_layers[l0 + l]));
+      L.of[l].k_scale = static_cast<uint8_t *>(const_cast<void *>(k_scale_layers[l0 + l])); L.of[l].v_scale = static_cast<uint8_t *>(const_cast<void *>(v_scale_layers[l0 + l]));
+      L.of[l].q = static_cast<char *>(k_out_layers[l0 + l]); L.of[l].out = static_cast<char *>(v_out_layers[l0 + l]);
     }
     const dim3 grid = grid_of(k, nl, most);
     hipStream_t st = static_cast<hipStream_t>(stream);

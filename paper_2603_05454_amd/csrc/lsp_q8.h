@@ -18,12 +18,16 @@ constexpr int kQ8Most = 246;  // the largest E: 1.75 * 2^127 is the largest magn
 // 2^(E - 127), E from 1 to 254
 __device__ __forceinline__ float q8_scale(uint32_t E) { return __uint_as_float(E << 23); }
 
-// Operands of the layers of one launch.
+// Operands of the layers of one launch: 64 bytes a layer, which a workgroup reads at once (arrays of each operand were eight reads in a chain,
+// 3 us of a short call).
+struct Q8Layer {
+  const char *q, *k_suf, *v_suf;
+  char *k_cache, *v_cache;
+  uint8_t *k_scale, *v_scale;
+  char *out;
+};
 struct Q8Layers {
-  const char *q[kMaxAttnLayers], *k_suf[kMaxAttnLayers], *v_suf[kMaxAttnLayers];
-  char *k_cache[kMaxAttnLayers], *v_cache[kMaxAttnLayers];
-  uint8_t *k_scale[kMaxAttnLayers], *v_scale[kMaxAttnLayers];
-  char *out[kMaxAttnLayers];
+  Q8Layer of[kMaxAttnLayers];
 };
 
 // Shapes and strides of caches in 8 bits beside buffers of the descriptor's type, checked and resolved.
