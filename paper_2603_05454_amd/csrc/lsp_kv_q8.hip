@@ -18,8 +18,8 @@ int32_t check_q8(const char *what, const lsp_attn_desc *d, bool queries, AttnArg
   const int32_t rc = check_attn(&c, a);
   if (rc != LSP_OK) return rc;
   LSP_CHECK_ARG(a.cs[0] % 16 == 0 && a.cs[1] % 16 == 0 && a.cs[2] % 16 == 0, "%s: cache strides must be multiples of 16 bytes", what);
-  LSP_CHECK_ARG(a.C <= 1 << 30 && a.S <= 1 << 30 && (a.S / kQ8Block + int64_t(2)) * a.Hkv < int64_t(1) << 30,
-                "%s: C and S must be <= 2^30, S / 32 * Hkv < 2^30", what);
+  LSP_CHECK_ARG(a.C <= 1 << 30 && a.S <= 1 << 30 && (a.S / kQ8Block + int64_t(2)) * a.Hkv < int64_t(1) << 31,
+                "%s: C and S must be <= 2^30, S / 32 * Hkv < 2^31", what);
   if (a.D != 64 && a.D != 128) {
     set_error("%s: head_dim %d (64 and 128 are built)", what, a.D);
     return LSP_ERR_UNSUPPORTED;

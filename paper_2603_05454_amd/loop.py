@@ -10,9 +10,10 @@ from __future__ import annotations
 
 import torch
 
-from . import (BY_PLACE, AttnLayerTable, LayerTable, LspError, ProgressPoll, _commit_out, _need, attn_key_weights_layers, attn_key_weights_workspace_bytes,
-               attn_step_layers, commit_step, confidence, confidence_workspace_bytes, kv_evict, kv_evict_workspace_bytes, kv_gather_append,
-               lm_head_confidence, lm_head_confidence_workspace_bytes, token_scores, token_scores_workspace_bytes)
+from . import (BY_PLACE, AttnLayerTable, LayerTable, LspError, ProgressPoll, Q8LayerTable, _commit_out, _need, attn_key_weights_layers,
+               attn_key_weights_workspace_bytes, attn_q8_workspace_bytes, attn_step_layers, attn_step_q8_layers, commit_step, confidence,
+               confidence_workspace_bytes, kv_append_q8, kv_evict, kv_evict_workspace_bytes, kv_gather_append, lm_head_confidence,
+               lm_head_confidence_workspace_bytes, token_scores, token_scores_workspace_bytes)
 
 
 def _need_on(device, name, t, *rest, **kw):
@@ -110,13 +111,40 @@ class _Budget:
                  token_len=None if self.positions is None else prefix_len, **self.kw)
 
 
+class _EightBits:
+    """Caches in 8 bits: the attention reads them as they are, and the rows that a step commits are quantised into them."""
+
+    def __init__(self, kv_layers, run_attention, tokens):
+        lists = [[L[k] for L in kv_layers] for k in ("k_suf", "v_suf", "k_cache", "v_cache", "k_scale", "v_scale")]
+        q = outs = None
+        if run_attention:     # (one output per layer: a denoiser consumes each of them)
+            q = [L["q"] for L in kv_layers]
+            outs = list(torch.empty((len(q), *q[0].shape), dtype=q[0].dtype, device=q[0].device).unbind(0))
+        self.table, k = Q8LayerTable(*lists, q=q, out=outs), lists[2][0]
+        if k.device != tokens.device:
+            raise LspError(f"decode_loop: the caches are on {k.device}, the sequences are on {tokens.device}")
+        if lists[0][0].shape[0] != tokens.shape[0]:
+            raise LspError(f"decode_loop: kv_layers of {lists[0][0].shape[0]} sequences for {tokens.shape[0]}")
+        if k.shape[1] < tokens.shape[1]:
+            raise LspError(f"decode_loop: caches of {k.shape[1]} rows for token buffers of {tokens.shape[1]}")
+        self.workspace = None
+
+    def attend(self, prefix_len, suffix_len):
+        if self.workspace is None:
+            d = self.table.desc
+            self.workspace = torch.empty(max(16, attn_q8_workspace_bytes(d.B, d.S, d.Hq, d.Hkv, d.D, d.C, self.table.n)), dtype=torch.uint8,
+                                         device=suffix_len.device)
+        attn_step_q8_layers(self.table, prefix_len, suffix_len, workspace=self.workspace)
+
+
 def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
                 prefix_len, suffix_len, tokens, kv_layers=None, gen_len=None, run_attention=False,
                 poll=1, max_steps=100000, stop_after=None, observer=None, timed=False, commit_kw=None,
                 graph=False, lm_head_weight=None, flip_window=None, flip_trace=False, state=None, scores=None, cache_budget=None):
     """logits_fn(step, prefix_len) -> device logits [B,S,V].  prefix_len,
     suffix_len, tokens and the caches in kv_layers (list of dicts q?, k_suf,
-    v_suf, k_cache, v_cache) are updated in place.
+    v_suf, k_cache, v_cache) are updated in place.  With k_scale and v_scale beside them the caches are in 8 bits (q8_cache): committed
+    rows are quantised into them (lsp_kv_append_q8) and attention reads them so (lsp_attn_step_q8_layers, bf16); not together with cache_budget.
     run_attention: also run the attention of every layer, behind the step's logits_fn, over what is
     then in the buffers of kv_layers; the outputs stay inside.
     commit_kw: extra keyword arguments of commit() (adaptive, alpha, beta, max_commit).
@@ -184,6 +212,11 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
         if lm_head_weight is not None:
             raise LspError("decode_loop: scores need the logits, which the fused output head does not store")
         said = _Scores(scores, tokens, V)
+    eight = kv_layers is not None and any("k_scale" in L or "v_scale" in L for L in kv_layers)
+    if eight and not all(k in L for L in kv_layers for k in ("k_scale", "v_scale")):
+        raise LspError("decode_loop: k_scale and v_scale come together, in every layer")
+    if eight and cache_budget is not None:
+        raise LspError("decode_loop: caches in 8 bits are not cut back (cache_budget)")
     if cache_budget is not None:
         if not run_attention or kv_layers is None:
             raise LspError("decode_loop: a cache budget goes by the attention of kv_layers (run_attention)")
@@ -200,7 +233,9 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
         progress = ProgressPoll()
         progress.start(suffix_len, None, prefix_len, base, counters)
     table = None
-    if kv_layers is not None:       # (built while the first test is under way)
+    if eight:
+        eight = _EightBits(kv_layers, run_attention, tokens)
+    elif kv_layers is not None:     # (built while the first test is under way)
         table = LayerTable(*[[L[k] for L in kv_layers] for k in ("k_suf", "v_suf", "k_cache", "v_cache")])
     if budget is not None:
         budget.start(table, prefix_len, suffix_len)
@@ -214,7 +249,9 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
 
     def one_step(z):
         nonlocal out, conf, attn_out, ws
-        if run_attention and kv_layers is not None:
+        if run_attention and eight:
+            eight.attend(prefix_len, suffix_len)
+        elif run_attention and kv_layers is not None:
             if attn_out is None:     # one output per layer (a denoiser consumes each of them), allocated once
                 q = kv_layers[0]["q"]
                 outs = torch.empty((len(kv_layers), *q.shape), dtype=q.dtype, device=q.device)
@@ -240,6 +277,8 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
                     **(commit_kw or {}))
         if said is not None:
             said.keep(prefix_len, out["commit_len"])
+        if eight:
+            kv_append_q8(eight.table, out["commit_len"], prefix_len)
         if budget is not None:
             budget.append(table, out["commit_len"], prefix_len)
 

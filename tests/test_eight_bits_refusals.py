@@ -177,3 +177,10 @@ def test_norm_rope_refuses_wrong_tensors(no_device, wrong):
     t.update(wrong)
     with pytest.raises(m.LspError):
         m.qk_norm_rope(t.pop("q"), t.pop("k"), t.pop("inv_freq"), **t)
+
+
+@pytest.mark.parametrize("S, C, word", [(1 << 20, 1 << 21, b"2^30"), (1 << 21, 1 << 20, b"2^30"), ((1 << 20) - 1, 1 << 21, b"layer 0"), (1 << 21, (1 << 20) - 1, b"layer 0")])
+def test_read_counts_rows_of_heads_in_32_bits(S, C, word):
+    d = _desc(S=S, C=C, Hq=1024, Hkv=1024, D=64)
+    assert m.lib().lsp_kv_read_q8(ctypes.byref(d), 1, ONE, ONE, ONE, ONE, _p(), _p(), ONE, NULL, None) == -1
+    assert word in m.lib().lsp_last_error(), m.lib().lsp_last_error()

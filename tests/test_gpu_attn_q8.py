@@ -224,3 +224,43 @@ def test_a_workspace_that_will_not_do(lsp, marshalled):
         out = torch.full((B, S, Hq, D), POISON, dtype=torch.bfloat16, device="cuda")
         lsp.attn_step_q8(*d, *lens, out=out, workspace=ws)
         _close(out, want, mass, N, S)
+
+
+def _run(lsp, B, S, Hq, H, D, C, P, N, seed, copies=1):
+    """A call whose layers are the same operands `copies` times, against the definition and each other."""
+    t = [x[0] for x in _operands(B, S, Hq, H, D, C, P, N, seed)]
+    want, mass = eight_bits.attention(*t[:3], eight_bits.values(t[3], t[5]), eight_bits.values(t[4], t[6]), P, N)
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (P, N)]
+    q, *rest = [x.cuda() for x in t]
+    out = torch.full((copies, B, S, Hq, D), POISON, dtype=torch.bfloat16, device="cuda")
+    table = lsp.Q8LayerTable(*[[x] * copies for x in rest], q=[q] * copies, out=list(out.unbind(0)))
+    lsp.attn_step_q8_layers(table, *lens)
+    _close(out[0], want, mass, N, S)
+    assert all(torch.equal(o, out[0]) for o in out[1:])
+
+
+EDGES = [15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 513]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("turn", [0, 7])
+def test_every_tile_in_one_batch(lsp, D, turn):
+    """Rows at the edges of the tiles, on prefixes at the edges of blocks and steps."""
+    P = [0, 1, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 300, 5]
+    _run(lsp, 16, 520, 2, 2, D, 300, P[turn:] + P[:turn], EDGES, 50 + turn)
+
+
+WHOLE = [   # ..., copies: work enough that a workgroup has several heads; keys that are divided among workgroups, in each kind of tile; more than 64 sequences
+    (9, 5, 8, 4, 128, 2300, [2300 - b for b in range(9)], [5, 4, 0, 3, 2, 1, 5, 5, 5], 32), (9, 6, 12, 6, 64, 2300, [2299] * 9, [3] * 9, 24),
+    (9, 33, 4, 4, 128, 1100, [1100] * 9, [33, 17, 32, 33, 1, 33, 33, 16, 33], 12), (5, 3, 5, 5, 128, 2300, [2300, 1, 2200, 2111, 2300], [3] * 5, 32),
+    (1, 20, 8, 8, 128, 66000, [65990], [20], 1), (1, 33, 6, 6, 64, 66000, [65999], [33], 1), (1, 4, 3, 3, 128, 66000, [65999], [3], 2),
+    (1, 100, 2, 2, 128, 6000, [5950], [100], 1), (1, 100, 2, 2, 64, 6000, [5950], [100], 1), (1, 300, 2, 2, 128, 6000, [6000], [300], 1),
+    (2, 300, 4, 2, 128, 4000, [3990, 10], [130, 300], 1), (5, 300, 16, 16, 128, 9000, [9000, 8999, 9000, 100, 8970], [17, 3, 33, 300, 16], 1),
+    (130, 9, 3, 3, 64, 50, [(7 * b) % 51 for b in range(130)], [b % 10 for b in range(130)], 1),
+    (70, 12, 4, 2, 128, 2100, [(301 * b) % 2101 for b in range(70)], [b % 13 for b in range(70)], 1)]
+
+
+@pytest.mark.parametrize("case", range(len(WHOLE)))
+def test_work_is_dealt_out_whole(lsp, case):
+    *shape, copies = WHOLE[case]
+    _run(lsp, *shape, 70 + case, copies)
