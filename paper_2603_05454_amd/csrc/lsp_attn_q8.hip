@@ -557,10 +557,17 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Q8Layers &
     if (n > 0) __syncthreads();
     if (h == 0) s.m[wave][r] = x.m[n], s.l[wave][r] = l;
     __syncthreads();
-    float m = -INFINITY, sum = 0.f;
-    for (int w = sub; w < WAVES; w += 1 << t.heads) m = fmaxf(m, s.m[w][r]);
+    float m = -INFINITY, sum = 0.f, ms[WAVES], ls[WAVES];
+    // (all reads at once, one behind the other they were 2 us of a short call; those of other heads' waves are not used)
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) {
+      const int w = (sub + (k << t.heads)) % WAVES;
+      ms[k] = s.m[w][r], ls[k] = k < turns ? s.l[w][r] : 0.f;
+      m = fmaxf(m, k < turns ? ms[k] : -INFINITY);
+    }
     // (a wave that met no key has zeros)
-    for (int w = sub; w < WAVES; w += 1 << t.heads) sum += s.l[w][r] != 0.f ? s.l[w][r] * __builtin_amdgcn_exp2f(s.m[w][r] - m) : 0.f;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) sum += ls[k] != 0.f ? ls[k] * __builtin_amdgcn_exp2f(ms[k] - m) : 0.f;
     const float f = l != 0.f ? __builtin_amdgcn_exp2f(x.m[n] - m) : 0.f;
 #pragma unroll
     for (int p = 0; p < VJ; ++p) {  // elements 4 p to 4 p + 3 of the lane's 4 VJ
@@ -573,8 +580,12 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Q8Layers &
     const int e = 16 * n + r;
     if (t.entry + e < t.entries) {
       for (int p = turn; p < VJ; p += turns) {
-        f32x4 y = s.o[sub][p][lane];
-        for (int w = sub + (1 << t.heads); w < WAVES; w += 1 << t.heads) y += s.o[w][p][lane];
+        f32x4 y = s.o[sub][p][lane], o[WAVES];
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) o[k] = s.o[(sub + (k << t.heads)) % WAVES][p][lane];
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k)
+          if (k < turns) y += o[k];
         const int d = 4 * VJ * h + 4 * p;
         if (t.slot < 0) {
           const float inv = 1.f / sum;
