@@ -21,18 +21,22 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLag = 8.f;      // octaves that a maximum may exceed the reference by before that moves
+// The reference before the first key: a number, so that weights of scores of -infinity are 0 whatever stands before them.
+constexpr float kLowest = -3.402823466e38f;
 constexpr int kStep = 64;        // keys of a step: of the cache or of the suffix
 constexpr int kShort = 64;       // entries of a unit up to which its tiles are short ones
 constexpr int kTall = 128;       // entries up to which, beyond that, a tile has as many
 constexpr int kTallest = 256;    // entries of a tile of the others (heads of 128)
 constexpr int kXcds = 8;
 constexpr int kSlots = 2048;     // parts of 32 entries in the workspace, for each of two kernels
-constexpr int kPartKeys = 2048;  // C + S beyond which keys are divided at all: one row on 2000 keys takes 16.8 us in one part and 17.0 in several, on 4000 keys 27.5 and 19.4
+// C + S beyond which keys are divided among workgroups at all: one row on 2000 keys takes 16.8 us in one part and 17.0 in several, on 4000 keys 27.5
+// and 19.4, on 12000 67.9 and 24.2; and where the plan divides nothing, the kernel that would join the parts takes 3 us.
+constexpr int kPartKeys = 2048;
 constexpr int kLeast = 4;        // steps of a part, at least
 constexpr int kOnce = 2;         // of a buffer read: nontemporal, the caches need not keep it
-// Steps of all short tiles from which on a workgroup's waves have up to four heads beside each other.  A row of the cache holds a head's 128 bytes beside the next one's: four
-// waves that read the same rows fetch 512 bytes in a piece (21 rows each on 533 keys of 16 sequences, 8 layers: 302 us where a workgroup's waves divide the keys
-// of one head among themselves 362).  With less to do the waves divide the keys, so that more of them work.
+// Steps of all short tiles from which on a workgroup's waves have up to four heads beside each other.  A row of the cache holds a head's 128 bytes beside
+// the next one's: four waves that read the same rows fetch 512 bytes in a piece (16 x 21 rows on 1515 keys in 8 layers: 302 us; where a workgroup's waves
+// divide one head's keys among themselves 362).  With less to do the waves divide the keys, so that more of them work.
 constexpr float kBeside = 8192;
 
 struct Q8AttnArgs {
@@ -71,20 +75,14 @@ struct Rows {
                                              __builtin_amdgcn_readfirstlane(valid > 0 ? (valid - 1) * int(stride) + bytes : 0), 0x00020000)),
         row(int(stride)) {}
 };
-// 16, 8 or 4 bytes, `rows` (the same for all lanes) behind byte v.  FULL: all rows are there, and the distance is the instruction's scalar offset; how that counts
-// where a read is to be found out of range is not relied on, elsewhere it is added.
-template <bool FULL>
+// 16, 8 or 4 bytes, `rows` behind byte v
 __device__ __forceinline__ u32x4 load16(const Rows &r, int v, int rows) {
-  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r.at, FULL ? v : v + rows * r.row, FULL ? rows * r.row : 0, 0));
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r.at, v + rows * r.row, 0, 0));
 }
-template <bool FULL>
 __device__ __forceinline__ u32x2 load8(const Rows &r, int v, int rows) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r.at, FULL ? v : v + rows * r.row, FULL ? rows * r.row : 0, 0));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r.at, v + rows * r.row, 0, 0));
 }
-template <bool FULL>
-__device__ __forceinline__ uint32_t load4(const Rows &r, int v, int rows) {
-  return __builtin_amdgcn_raw_buffer_load_b32(r.at, FULL ? v : v + rows * r.row, FULL ? rows * r.row : 0, 0);
-}
+__device__ __forceinline__ uint32_t load4(const Rows &r, int v, int rows) { return __builtin_amdgcn_raw_buffer_load_b32(r.at, v + rows * r.row, 0, 0); }
 // The compiler takes what is made of x for new every time: it is not kept in registers from one step to the next.
 __device__ __forceinline__ int anew(int x) {
   asm volatile("" : "+v"(x));
@@ -257,9 +255,11 @@ __device__ __forceinline__ float *part_stats(const Q8AttnArgs &a, int slot, int 
 // ---- short tiles -----------------------------------------------------------------------
 // Lanes l % 16 = r, l / 16 = h.  Of the keys: rows 16 k + r of the block, elements 64 i + 16 h of 16; of the values: rows 16 k + 4 h + e, of which
 // VJ elements from VJ r on.
-// A block of the cache comes to LDS by loads that go straight there, each of whole rows (as loads to registers, of which neighbouring lanes belong to
-// different rows, 16 x 21 rows on 1515 took 376 us), and stays the wave's own.  Its 16-byte pieces are exchanged, those of keys at p ^ (row / 2 % 8) (heads of 64: row / 4 % 4), the values' rows with
-// their neighbours where row / 4 is odd (heads of 64: at row ^ (row / 4 % 4)), so that what lanes read together lies in different banks.
+// A block of the cache comes to LDS by loads that go straight there, each of whole rows, and stays the wave's own: two blocks are on their way at any time, without a
+// register (as loads to registers, of which neighbouring lanes belong to different rows, the 16 x 21 rows above took 395 us instead of 362).  Where a unit
+// has one tile its keys are read once, and nontemporally (277 us instead of 302).  The 16-byte pieces in LDS are exchanged, those of keys at p ^ (row / 2 % 8)
+// (heads of 64: row / 4 % 4), the values' rows with their neighbours where row / 4 is odd (heads of 64: at row ^ (row / 4 % 4)), so that
+// what lanes read together lies in different banks.
 template <int D>
 struct Keys {
   static constexpr int KI = D / 64, KC = D / 32, VJ = D / 16;
@@ -365,7 +365,7 @@ struct Short {
       for (int c = 0; c < KC; ++c) q[n][c] = *reinterpret_cast<const bf16x8 *>(p + 128 * (c >> 1) + 32 * h + 16 * (c & 1));
 #pragma unroll
       for (int j = 0; j < VJ; ++j) o[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m[n] = -INFINITY;
+      m[n] = kLowest;
       l[n] = 0.f;
     }
   }
@@ -441,7 +441,7 @@ struct Short {
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int k = 0; k < KC; ++k) {
-        const bf16x8 f = __builtin_bit_cast(bf16x8, load16<false>(kr, kv + 128 * (k >> 1) + 16 * (k & 1), 16 * b));
+        const bf16x8 f = __builtin_bit_cast(bf16x8, load16(kr, kv + 128 * (k >> 1) + 16 * (k & 1), 16 * b));
 #pragma unroll
         for (int n = 0; n < NB; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[n][k], s[n][b], 0, 0, 0);
       }
@@ -449,11 +449,11 @@ struct Short {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if constexpr (VJ == 8) {
-        const u32x4 x = load16<false>(vr, vv, Keys<D>::value_row(0, e));
+        const u32x4 x = load16(vr, vv, Keys<D>::value_row(0, e));
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[e][j] = x[j];
       } else {
-        const u32x2 x = load8<false>(vr, vv, Keys<D>::value_row(0, e));
+        const u32x2 x = load8(vr, vv, Keys<D>::value_row(0, e));
         w[e][0] = x[0], w[e][1] = x[1];
       }
     }
@@ -630,16 +630,16 @@ struct Tall {
     if (!cached) {
 #pragma unroll
       for (int p = 0; p < KP; ++p) {
-        const u32x4 x = load16<false>(k, at + 16 * p, 0);
+        const u32x4 x = load16(k, at + 16 * p, 0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) rk[i][4 * p + j] = x[j];
       }
     } else if constexpr (D == 128) {
-      const u32x4 x = load16<false>(k, at, 0);
+      const u32x4 x = load16(k, at, 0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) rk[i][j] = x[j];
     } else {
-      const u32x2 x = load8<false>(k, at, 0);
+      const u32x2 x = load8(k, at, 0);
       rk[i][0] = x[0], rk[i][1] = x[1];
     }
   }
@@ -656,14 +656,14 @@ struct Tall {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (bytes == 16) {
-        const u32x4 x = load16<false>(v, vv, i);
+        const u32x4 x = load16(v, vv, i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) rv[4 * i + j] = x[j];
       } else if (bytes == 8) {
-        const u32x2 x = load8<false>(v, vv, i);
+        const u32x2 x = load8(v, vv, i);
         rv[2 * i] = x[0], rv[2 * i + 1] = x[1];
       } else {
-        rv[i] = load4<false>(v, vv, i);
+        rv[i] = load4(v, vv, i);
       }
     }
   }
@@ -723,7 +723,7 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m = kLowest, l = 0.f;
 
   const int last_block = (t.P + kQ8Block - 1) / kQ8Block - 1, end = 2 * t.to;
   auto valid_in = [&](int j) { return j < t.cached ? t.P - j * kStep : t.N - (j - t.cached) * kStep; };  // keys of step j that there are

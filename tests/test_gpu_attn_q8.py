@@ -264,3 +264,21 @@ WHOLE = [   # ..., copies: work enough that a workgroup has several heads; keys 
 def test_work_is_dealt_out_whole(lsp, case):
     *shape, copies = WHOLE[case]
     _run(lsp, *shape, 70 + case, copies)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("S, Hq, P, first", [(40, 2, 0, 32), (64, 2, 70, 33), (140, 2, 0, 64), (140, 2, 33, 96), (300, 2, 0, 32), (3, 8, 0, 1), (40, 2, 2100, 40)])
+def test_scores_of_minus_infinity_weigh_nothing(lsp, D, S, Hq, P, first):
+    """The first suffix keys' scores are -infinity: a whole block's, a step's, all that a wave meets."""
+    B, H = 2, 2
+    t = [x[0] for x in _operands(B, S, Hq, H, D, P + 20, [P, P], [S, S - 1], 6)]
+    t[0][..., 0] = t[0][..., 0].abs() + 0.5
+    t[1][:, :first, :, 0] = -math.inf
+    if P == 0 and first >= S - 1:
+        t[1][:, S - 1:, :, 0] = 0.0
+    N = [S, S - 1]
+    want, mass = eight_bits.attention(*t[:3], eight_bits.values(t[3], t[5]), eight_bits.values(t[4], t[6]), [P, P], N)
+    assert not want[0].isnan().any()
+    out = torch.full((B, S, Hq, D), POISON, dtype=torch.bfloat16, device="cuda")
+    lsp.attn_step_q8(*[x.cuda() for x in t], *[torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([P, P], N)], out=out)
+    _close(out, want, mass, N, S)
