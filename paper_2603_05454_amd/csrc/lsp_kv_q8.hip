@@ -45,21 +45,31 @@ struct KvArgs {
 struct Eight {
   float x[8];
 };
-// What a call reads or writes once need not stay in the caches: appending 4 x 4096 rows of 32 heads in two layers, 0.8 GB, takes 133 us so and 147 without,
-// and with the reading back 305 and 327.  (Only the reading's own writes are faster as plain ones: 167 us against 174.)
-template <typename V>
-__device__ __forceinline__ V load_once(const char *p) { return __builtin_nontemporal_load(reinterpret_cast<const V *>(p)); }
-template <typename V>
-__device__ __forceinline__ void store_once(char *p, V x) { __builtin_nontemporal_store(x, reinterpret_cast<V *>(p)); }
+// ONCE: nontemporal.  Where the buffers are larger than the last cache (256 MB), what a call reads or writes once need not stay there: 4 x 4096 rows of 32 heads
+// in two layers, 0.8 GB, are appended in 131 us so and 148 without, and appended and read back in 303 and 328; where they are smaller it is better kept: 64
+// rows of 8 sequences in four layers 37 and 32 us.  The reading's own writes are plain ones: 167 us against 174.
+constexpr int64_t kLastCache = int64_t(256) << 20;
+template <bool ONCE, typename V>
+__device__ __forceinline__ V load_once(const char *p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+  else return *reinterpret_cast<const V *>(p);
+}
+template <bool ONCE, typename V>
+__device__ __forceinline__ void store_once(char *p, V x) {
+  if constexpr (ONCE) __builtin_nontemporal_store(x, reinterpret_cast<V *>(p));
+  else *reinterpret_cast<V *>(p) = x;
+}
+template <bool ONCE>
 __device__ __forceinline__ Eight load8(const char *p, const uint16_t *) {
-  const u32x4 w = load_once<u32x4>(p);
+  const u32x4 w = load_once<ONCE, u32x4>(p);
   Eight r;
 #pragma unroll
   for (int k = 0; k < 4; ++k) r.x[2 * k] = bf16_lo(w[k]), r.x[2 * k + 1] = bf16_hi(w[k]);
   return r;
 }
+template <bool ONCE>
 __device__ __forceinline__ Eight load8(const char *p, const float *) {
-  const f32x4 a = load_once<f32x4>(p), b = load_once<f32x4>(p + 16);
+  const f32x4 a = load_once<ONCE, f32x4>(p), b = load_once<ONCE, f32x4>(p + 16);
   return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
 
@@ -103,7 +113,7 @@ __device__ __forceinline__ int exponent_of(float a) {
 
 // A lane has eight numbers (16 or 32 bytes) of every fourth row (of every eighth, where heads are of 64), so that a wave's loads are of whole rows and
 // the block is in registers between its maximum and its rounding: one pass over the new rows.
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(kThreads) void append_kernel(KvArgs a, Q8Layers L) {
   constexpr int kLanes = D / 8, kRows = kWave / kLanes, kSteps = kQ8Block / kRows;
   const int b = blockIdx.z, l = blockIdx.y >> 1, lane = threadIdx.x & (kWave - 1);
@@ -121,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(KvArgs a, Q8Layers L) 
     float most = 0.f;
 #pragma unroll
     for (int k = 0; k < kSteps; ++k)  // (rows that are not new repeat one that is)
-      x[k] = load8(suf + int64_t(min(max(t0 + k * kRows + r, P0), P - 1) - P0) * a.ss[1] + g * a.ss[2] + d * int(sizeof(T)), static_cast<T *>(nullptr));
+      x[k] = load8<ONCE>(suf + int64_t(min(max(t0 + k * kRows + r, P0), P - 1) - P0) * a.ss[1] + g * a.ss[2] + d * int(sizeof(T)), static_cast<T *>(nullptr));
 #pragma unroll
     for (int k = 0; k < kSteps; ++k)
 #pragma unroll
@@ -151,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(KvArgs a, Q8Layers L) 
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
       const int t = t0 + k * kRows + r;
-      if (t >= P0 && t < P) store_once(to + int64_t(t) * a.cs[1], round8(x[k], inverse));
+      if (t >= P0 && t < P) store_once<ONCE>(to + int64_t(t) * a.cs[1], round8(x[k], inverse));
     }
     if (lane == 0) *s = uint8_t(E);
   }
@@ -178,7 +188,7 @@ __device__ __forceinline__ void store16(char *p, u32x4 w, float scale, const flo
 
 constexpr int kAtOnce = 4;
 // 16 values a lane and step, four steps at once.  Exact in both types.
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(kThreads) void read_kernel(KvArgs a, Q8Layers L) {
   constexpr int kLanes = D / 16, kHeads = kThreads / kLanes;
   const int b = blockIdx.z, l = blockIdx.y >> 1;
@@ -198,7 +208,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(KvArgs a, Q8Layers L) {
       const int at = min(it + int64_t(k) * step, int64_t(items - 1));
       i[k] = quotient(at, a.by_heads), g[k] = at - i[k] * a.Hkv;
       const int t = first + i[k];
-      w[k] = load_once<u32x4>(cache + int64_t(t) * a.cs[1] + g[k] * a.cs[2] + d);
+      w[k] = load_once<ONCE, u32x4>(cache + int64_t(t) * a.cs[1] + g[k] * a.cs[2] + d);
       E[k] = scales[int64_t(g[k]) * a.blocks + t / kQ8Block];
     }
 #pragma unroll
@@ -219,6 +229,29 @@ KvArgs kv_args(const AttnArgs &a, const lsp_attn_desc *d, const int32_t *from, c
   }
   return k;
 }
+
+template <bool ONCE>
+void launch_append(int32_t dtype, int D, dim3 grid, hipStream_t st, const KvArgs &k, const Q8Layers &L) {
+  if (dtype == LSP_F32) {
+    if (D == 64) append_kernel<float, 64, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+    else append_kernel<float, 128, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+  } else {
+    if (D == 64) append_kernel<uint16_t, 64, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+    else append_kernel<uint16_t, 128, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+  }
+}
+template <bool ONCE>
+void launch_read(int32_t dtype, int D, dim3 grid, hipStream_t st, const KvArgs &k, const Q8Layers &L) {
+  if (dtype == LSP_F32) {
+    if (D == 64) read_kernel<float, 64, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+    else read_kernel<float, 128, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+  } else {
+    if (D == 64) read_kernel<uint16_t, 64, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+    else read_kernel<uint16_t, 128, ONCE><<<grid, kThreads, 0, st>>>(k, L);
+  }
+}
+// whether the buffers of a launch, beside the caches, are larger than the last cache; bytes: of a head's row
+bool is_large(const KvArgs &k, int layers, size_t bytes) { return double(2 * layers) * k.B * k.S * k.Hkv * double(bytes) > double(kLastCache); }
 
 // workgroups in x: all that there is work for, or what makes kGroups of them
 dim3 grid_of(const KvArgs &k, int layers, int64_t most) {
@@ -258,14 +291,10 @@ extern "C" int32_t lsp_kv_append_q8(const lsp_attn_desc *d, int32_t num_layers, 
       L.of[l].k_scale = static_cast<uint8_t *>(k_scale_layers[l0 + l]); L.of[l].v_scale = static_cast<uint8_t *>(v_scale_layers[l0 + l]);
     }
     const dim3 grid = grid_of(k, nl, most);
+    const bool once = is_large(k, nl, elem_size(d->dtype) * a.D);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (d->dtype == LSP_F32) {
-      if (a.D == 64) append_kernel<float, 64><<<grid, kThreads, 0, st>>>(k, L);
-      else append_kernel<float, 128><<<grid, kThreads, 0, st>>>(k, L);
-    } else {
-      if (a.D == 64) append_kernel<uint16_t, 64><<<grid, kThreads, 0, st>>>(k, L);
-      else append_kernel<uint16_t, 128><<<grid, kThreads, 0, st>>>(k, L);
-    }
+    if (once) launch_append<true>(d->dtype, a.D, grid, st, k, L);
+    else launch_append<false>(d->dtype, a.D, grid, st, k, L);
     LSP_CHECK_LAUNCH("lsp_kv_append_q8: launch");
   }
   return LSP_OK;
@@ -302,14 +331,10 @@ extern "C" int32_t lsp_kv_read_q8(const lsp_attn_desc *d, int32_t num_layers, co
       L.of[l].q = static_cast<char *>(k_out_layers[l0 + l]); L.of[l].out = static_cast<char *>(v_out_layers[l0 + l]);
     }
     const dim3 grid = grid_of(k, nl, most);
+    const bool once = is_large(k, nl, elem_size(d->dtype) * a.D);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (d->dtype == LSP_F32) {
-      if (a.D == 64) read_kernel<float, 64><<<grid, kThreads, 0, st>>>(k, L);
-      else read_kernel<float, 128><<<grid, kThreads, 0, st>>>(k, L);
-    } else {
-      if (a.D == 64) read_kernel<uint16_t, 64><<<grid, kThreads, 0, st>>>(k, L);
-      else read_kernel<uint16_t, 128><<<grid, kThreads, 0, st>>>(k, L);
-    }
+    if (once) launch_read<true>(d->dtype, a.D, grid, st, k, L);
+    else launch_read<false>(d->dtype, a.D, grid, st, k, L);
     LSP_CHECK_LAUNCH("lsp_kv_read_q8: launch");
   }
   return LSP_OK;
