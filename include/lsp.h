@@ -576,7 +576,7 @@ int32_t lsp_kv_append_q8(const lsp_attn_desc *desc, int32_t num_layers, const vo
  * Rows [first_row[b], end_row[b]) of the caches as the values they stand for, in rows 0, 1, ... of
  * k_out, v_out [B, S, Hkv, D] (of the descriptor's dtype and S, strides kv_suf_stride; cut to S rows; first_row is cut to 0..C, end_row
  * to first_row..C).  Exact in fp32, and in bf16 from E = 10 on (below, what is subnormal there is rounded).  The rest of
- * the outputs is not written.
+ * the outputs is not written.  Limits of both: C, S <= 2^30, S / 32 * Hkv < 2^31; here min(S, C) * Hkv < 2^30.
  */
 int32_t lsp_kv_read_q8(const lsp_attn_desc *desc, int32_t num_layers, const void *const *k_cache_layers,
                        const void *const *v_cache_layers, const void *const *k_scale_layers,
@@ -586,9 +586,10 @@ int32_t lsp_kv_read_q8(const lsp_attn_desc *desc, int32_t num_layers, const void
 /*
  * lsp_attn_step over caches in 8 bits: the P_b cached rows are the values they stand for, the suffix K/V, queries
  * and outputs bf16 (dtype LSP_BF16 only).  Arguments as there beside the scales; cache_stride as above.
- * workspace: device, 16-byte aligned, lsp_attn_q8_workspace_bytes(desc, num_layers) bytes of any content,
- * for this call alone until it has run; with it the keys of few rows are divided between workgroups, without
- * (NULL, or fewer bytes) a tile's keys are one workgroup's.
+ * workspace: device, 16-byte aligned, lsp_attn_q8_workspace_bytes(desc, num_layers) bytes of any content
+ * (none up to C + S = 2048, else 0.27 MB x D, twice that where D = 128 and S * Hq / Hkv > 128), for this call alone until
+ * it has run; with it the keys of few rows are divided between workgroups, without (NULL, or fewer bytes) a tile's
+ * keys are one workgroup's.  Parts are added in order: the same operands give the same bits, with a workspace of one kind.
  * Limits: those of lsp_attn_step; C, S <= 2^30, B * Hkv < 2^23, B * S * Hq and S * Hq / Hkv < 2^30; a row stride of K and V of
  * at least D.
  */
@@ -597,7 +598,8 @@ int32_t lsp_attn_step_q8(const lsp_attn_desc *desc, const void *q, const void *k
                          const void *k_cache, const void *v_cache, const uint8_t *k_scale, const uint8_t *v_scale,
                          const int32_t *prefix_len, const int32_t *suffix_len, void *out, void *workspace,
                          size_t workspace_bytes, void *stream);
-/* and for every layer in one launch (32 layers to a launch), as lsp_attn_step_layers */
+/* and for every layer at once, as lsp_attn_step_layers: for each 32 layers one launch, a second one where S * Hq / Hkv > 128 and
+ * D = 128 (units of more and of fewer rows), and one that adds the parts where there is a workspace */
 int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *desc, int32_t num_layers, const void *const *q_layers,
                                 const void *const *k_suf_layers, const void *const *v_suf_layers,
                                 const void *const *k_cache_layers, const void *const *v_cache_layers,

@@ -1,12 +1,13 @@
-// lsp_attn_step_q8: attention of the active rows over [cached rows in 8 bits || suffix rows].
+// lsp_attn_step_q8: attention of the active rows over [cached rows in 8 bits || suffix rows], out = softmax(q K^T scale) V in one pass over the keys.
 //
 // A unit is (layer, sequence, KV head); the rows of all heads of its group are one list (entry e: row e / rep of head e % rep), since they meet
-// the same keys.  A wave has tiles of 16 entries and goes over blocks of 32 keys, those that share a scale:
-//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, keys x entries: a lane's scores are of ONE entry, and of those keys of which
-//   O^T += V^T P^T  has its probabilities as operand: they go from one product to the other in the lane's registers.
-// The order of a head's elements and of a block's keys within the products is of no matter, so both operands are taken as a lane loads them: 16 bytes of a
-// key's row; a few elements of eight keys' rows, turned in registers, a byte each, before they become bf16 (v_cvt_scalef32_pk_bf16_fp8, with the
-// block's scale: exact).
+// the same keys.  Tiles of entries go over blocks of 32 keys, those that share a scale, with a running reference m and sum l of the weights 2^(s - m):
+//   S^T = K Q^T   keys x entries: a lane's scores are of ONE entry, and of those keys of which
+//   O^T += V^T P^T  has its probabilities as operand: they go from one product to the other in the lane's registers, rounded to bf16 (2^-8 of each).
+// m moves only when a maximum exceeds it by more than 8 octaves: weights stay below 2^8, and sums seldom have to be multiplied.  A scale is a power of two,
+// so that e4m3 values become bf16 exactly (v_cvt_scalef32_pk_bf16_fp8).  Sums are 32 bits.
+// Short tiles (units of up to 64 entries) are bound by the cache's bytes: each wave takes blocks by itself.  Tall ones are bound by matrix and vector instructions: waves share
+// blocks in LDS, made bf16 once for all.
 #include <math.h>
 
 #include <type_traits>
@@ -253,7 +254,8 @@ template <int D>
 __device__ __forceinline__ float *part_stats(const Q8AttnArgs &a, int slot, int row) { return a.parts + (int64_t(slot) + (row >> 5)) * 32 * (D + 2) + 32 * D + 2 * (row & 31); }
 
 // ---- short tiles -----------------------------------------------------------------------
-// Lanes l % 16 = r, l / 16 = h.  Of the keys: rows 16 k + r of the block, elements 64 i + 16 h of 16; of the values: rows 16 k + 4 h + e, of which
+// v_mfma_f32_16x16x32_bf16.  The order of a head's elements and of a block's keys within the products is of no matter, so both operands are taken as a lane reads them: 16
+// bytes of a key's row; a few elements of eight keys' rows, turned in registers, a byte each, before they become bf16.  Lanes l % 16 = r, l / 16 = h.  Of the keys: rows 16 k + r of the block, elements 64 i + 16 h of 16; of the values: rows 16 k + 4 h + e, of which
 // VJ elements from VJ r on.
 // A block of the cache comes to LDS by loads that go straight there, each of whole rows, and stays the wave's own: two blocks are on their way at any time, without a
 // register (as loads to registers, of which neighbouring lanes belong to different rows, the 16 x 21 rows above took 395 us instead of 362).  Where a unit
@@ -1082,6 +1084,10 @@ bool divides(int64_t C, int64_t S) { return C + S > kPartKeys; }
 bool has_tallest(int64_t entries, int D) { return D == 128 && entries > kTall; }
 size_t parts_bytes(int D) { return size_t(kSlots) * 32 * (D + 2) * sizeof(float); }
 
+// Two workgroups of four waves, or one of eight, stay on each compute unit.  Units of more entries than 128 (heads of 128) have a kernel of their own, of eight waves and 256
+// entries, so that every key that is made bf16 and laid out in LDS meets twice as many queries: 8 x 1024 rows on 5120 keys of 32 heads, 275 GFLOP, take 730 us
+// on a cool card (0.94 PFLOP/s; 1.2 is what a large library product reaches), 843 in tiles of 128.  Of it the laying out is 130, the exponentials are 60:
+// they, the matrix instructions and the power that both draw are what bounds it.
 template <int D>
 int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_t st) {
   Q8AttnArgs a = args;
@@ -1091,6 +1097,7 @@ int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_
   a.by_rep = div_by(a.rep);
   const int64_t entries = int64_t(a.rep) * a.S;
   const bool tall = entries > kShort, tallest = has_tallest(entries, D);
+  // Few units have eight waves to each: 4 x 32 of them on 32 768 keys take 173 us so and 188 with four, 512 of them on 533 keys 30 and 22.
   const bool wide = !tall && int64_t(a.per_seq) * a.B <= 256;
   a.groups = wide ? 256 : 512;
   a.above = 0;

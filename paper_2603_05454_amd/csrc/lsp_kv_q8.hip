@@ -2,7 +2,8 @@
 //
 // A block is 32 rows of one head, one wave's.  With a = the largest finite magnitude of its new rows and 448 that of e4m3, E is the smallest
 // exponent byte with a <= 448 * 2^(E - 127); powers of two cost an e4m3 value nothing (its own exponent takes them up) and make multiplying by a
-// scale, and rounding again under a larger one, exact but for what becomes subnormal.
+// scale, and rounding again under a larger one, exact but for what becomes subnormal.  Bound by the bytes: 16 bits read and 8 written for each number, or the other way
+// round (the prompt below: 6.1 TB/s written, 4.7 read back; a large copy reaches 4.9).
 #include "lsp_q8.h"
 
 namespace lsp {
