@@ -76,14 +76,13 @@ struct Rows {
                                              __builtin_amdgcn_readfirstlane(valid > 0 ? (valid - 1) * int(stride) + bytes : 0), 0x00020000)),
         row(int(stride)) {}
 };
-// 16, 8 or 4 bytes, `rows` behind byte v
+// 16 or 8 bytes, `rows` behind byte v
 __device__ __forceinline__ u32x4 load16(const Rows &r, int v, int rows) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r.at, v + rows * r.row, 0, 0));
 }
 __device__ __forceinline__ u32x2 load8(const Rows &r, int v, int rows) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r.at, v + rows * r.row, 0, 0));
 }
-__device__ __forceinline__ uint32_t load4(const Rows &r, int v, int rows) { return __builtin_amdgcn_raw_buffer_load_b32(r.at, v + rows * r.row, 0, 0); }
 // The compiler takes what is made of x for new every time: it is not kept in registers from one step to the next.
 __device__ __forceinline__ int anew(int x) {
   asm volatile("" : "+v"(x));
@@ -483,9 +482,9 @@ union Joined {
   };
   char slots[WAVES][4 * Keys<D>::kBytes];
 };
-template <int D>
+template <int D, int AHEAD>
 struct Staged {
-  uint32_t k[4][kQ8Block * D / 2], v[2][kStep * D / 2];
+  uint32_t k[4 * AHEAD][kQ8Block * D / 2], v[2 * AHEAD][kStep * D / 2];
 };
 
 template <int D, int NB, int WAVES, bool ONCE>
@@ -602,103 +601,73 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Q8Layers &
   }
 }
 
+// values of eight keys, four from p on and four that are NEXT words on, of one element a lane
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+template <int NEXT>
+__device__ __forceinline__ bf16x8 turned(const uint32_t *__restrict__ p) {
+  typedef __attribute__((address_space(3))) s16x4 *At;
+  const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p)));
+  const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p + NEXT)));
+  return fragment(a[0], a[1], b[0], b[1]);
+}
+
 // ---- tall tiles ------------------------------------------------------------------------
 // Waves of 32 entries each, which share keys and values in LDS, bf16 by then.  The scores of a wave are keys x entries (32x32x16): lane l has those
 // of entry l % 32 with keys 8 j + 4 h + i of 32, h = l / 32, and these are, eight at a time, the operand of the second product, whose other one is
-// V^T: eight keys' values of one element, 16 bytes.  So the values are turned as they are written to LDS: row d holds for each (32 keys, 16 of them,
-// h) the eight keys 8 x + 4 h + i in the order of x, i.
-// 16-byte pieces are exchanged against bank conflicts: piece p of a key's 256 bytes at p ^ (key % 16) (of 128: p ^ (key / 2 % 8)); piece p of
-// the 128 bytes of element d at p ^ (d / 2 % 8), and ^ 6 for every other sixteen, which serves both the writes, of every eighth d, and the reads, of
-// neighbours (a wave's read of 1 KB takes 4.3 clocks so, 8.1 with any two of its lanes in the same place).
+// V^T: of one element those of keys 16 t + 8 x + 4 h + i.  Values lie in LDS as keys do, row by row, and are turned as they are read (ds_read_b64_tr_b16: lane
+// s of 16 points at columns 4 (s % 4) of row s / 4 and receives column s of four rows).
+// 16-byte pieces are exchanged against bank conflicts: piece p of a key's 256 bytes at p ^ (key % 16) (of 128: p ^ (key / 2 % 8)); of a value's at
+// p ^ (4 (key % 4) + key % 2) (of 128: p ^ 4 (key / 2 % 2)): the four rows of a turning read then have all banks between them, and so have a write's two.
 template <int D, int WAVES>
 struct Tall {
   static constexpr int KC = D / 16, DB = D / 32;
-  static constexpr int VB = 4 * D / (16 * WAVES), kTurning = D / VB;  // elements of four keys' values that a thread turns; threads that have those of four keys
-  static constexpr int KP = D / 64;                                   // pieces of a block's keys that a thread has
-  static constexpr int kSets = 8 / WAVES;                             // of a step's two blocks
+  static constexpr int KP = D / 64;        // pieces of a block's keys that a thread has
+  static constexpr int kSets = 8 / WAVES;  // of a step's two blocks
 
   // in words
   static __device__ __forceinline__ int key_piece(int key, int p) {
     return D == 128 ? key * 64 + 4 * (p ^ (key & 15)) : key * 32 + 4 * (p ^ (key >> 1 & 7));
   }
-  static __device__ __forceinline__ int value_piece(int d, int p) { return d * 32 + 4 * (p ^ ((d >> 1 ^ (d & 16 ? 6 : 0)) & 7)); }
+  static __device__ __forceinline__ int value_piece(int key, int p) {
+    return D == 128 ? key * 64 + 4 * (p ^ (4 * (key & 3) + (key & 1))) : key * 32 + 4 * (p ^ 4 * (key >> 1 & 1));
+  }
+  // where a lane's part of the first transposed read is
+  static __device__ __forceinline__ int value_start(int lane) {
+    const int s = lane & 15;
+    return value_piece(4 * (lane >> 5) + s / 4, 2 * (lane >> 4 & 1) + s % 4 / 2) + 2 * (s & 1);
+  }
 
-  // what a thread has on its way: of two blocks of 32 keys, of a step's values (half as much of the cache), and of their exponents (the keys': a byte each)
-  uint32_t rk[kSets][4 * KP], rv[2 * VB], ke, ve;
+  // what a thread has on its way, of a block's keys and of one's values, or of two blocks': D / 8 elements of key tid / 8 % 32; and their exponents, a byte each
+  uint32_t rk[kSets][4 * KP], rv[kSets][4 * KP], ke, ve;
 
-  // a block's keys: a thread has D / 8 elements of key tid / 8 % 32
-  __device__ __forceinline__ void load_keys(int i, const Rows &k, int tid, bool cached) {
+  static __device__ __forceinline__ void load(uint32_t (&to)[4 * KP], const Rows &k, int tid, bool cached) {
     const int at = anew(tid / 8 % 32 * k.row + tid % 8 * (cached ? D / 8 : D / 4));
     if (!cached) {
 #pragma unroll
       for (int p = 0; p < KP; ++p) {
         const u32x4 x = load16(k, at + 16 * p, 0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) rk[i][4 * p + j] = x[j];
+        for (int j = 0; j < 4; ++j) to[4 * p + j] = x[j];
       }
     } else if constexpr (D == 128) {
       const u32x4 x = load16(k, at, 0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) rk[i][j] = x[j];
+      for (int j = 0; j < 4; ++j) to[j] = x[j];
     } else {
       const u32x2 x = load8(k, at, 0);
-      rk[i][0] = x[0], rk[i][1] = x[1];
+      to[0] = x[0], to[1] = x[1];
     }
   }
-  __device__ __forceinline__ void store_keys(int i, uint32_t *k, float s, int tid, bool cached) const {
-    const int k0 = anew(key_piece(tid / 8 % 32, KP * (tid % 8)));
+  // place: of the thread's first piece
+  static __device__ __forceinline__ void store(const uint32_t (&from)[4 * KP], uint32_t *to, int place, float s, bool cached) {
+    const int k0 = anew(place);
 #pragma unroll
     for (int p = 0; p < KP; ++p)
-      *reinterpret_cast<u32x4 *>(k + (k0 ^ 4 * p)) = cached ? u32x4{low(rk[i][2 * p], s), high(rk[i][2 * p], s), low(rk[i][2 * p + 1], s), high(rk[i][2 * p + 1], s)}
-                                                            : u32x4{rk[i][4 * p], rk[i][4 * p + 1], rk[i][4 * p + 2], rk[i][4 * p + 3]};
+      *reinterpret_cast<u32x4 *>(to + (k0 ^ 4 * p)) = cached ? u32x4{low(from[2 * p], s), high(from[2 * p], s), low(from[2 * p + 1], s), high(from[2 * p + 1], s)}
+                                                             : u32x4{from[4 * p], from[4 * p + 1], from[4 * p + 2], from[4 * p + 3]};
   }
-  // a step's values: VB elements of four keys
-  __device__ __forceinline__ void load_values(const Rows &v, int tid, bool cached) {
-    const int vv = anew(tid / kTurning * 4 * v.row + tid % kTurning * (cached ? VB : 2 * VB)), bytes = cached ? VB : 2 * VB;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (bytes == 16) {
-        const u32x4 x = load16(v, vv, i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) rv[4 * i + j] = x[j];
-      } else if (bytes == 8) {
-        const u32x2 x = load8(v, vv, i);
-        rv[2 * i] = x[0], rv[2 * i + 1] = x[1];
-      } else {
-        rv[i] = load4(v, vv, i);
-      }
-    }
-  }
-  // Where the thread's values of four keys go: keys 4 f to 4 f + 3, f = tid / kTurning = 8 kb + 4 t + 2 x + h, are half x of piece 4 kb + 2 t + h of row d.  Every
-  // other thread stores its rows 2 i + 1 before 2 i: rows of one parity share 32 banks (a wave's store of 8 bytes 16 clocks, 8 so).
-  static __device__ __forceinline__ int value_base(int tid) {
-    const int f = tid / kTurning;
-    return value_piece(tid % kTurning * VB, f >> 3 << 2 | (f >> 2 & 1) << 1 | (f & 1)) + 2 * (f >> 1 & 1);
-  }
-  __device__ __forceinline__ void store_values(uint32_t *v, float s, int tid, bool cached) const {
-    const int base = anew(value_base(tid)), odd = tid & 1, to0 = base + 32 * odd, to1 = base + 32 - 32 * odd;
-    const uint32_t even_first = 0x05040100, odd_first = 0x07060302, s0 = odd ? odd_first : even_first, s1 = odd ? even_first : odd_first;
-    auto at = [&](int j) { return reinterpret_cast<u32x2 *>(v + ((j & 1 ? to1 : to0) ^ 4 * (j >> 1)) + 64 * (j >> 1)); };
-    if (cached) {
-      constexpr int W = VB / 4;
-#pragma unroll
-      for (int q = 0; q < W; ++q) {
-        const uint32_t a = rv[q], b = rv[W + q], c = rv[2 * W + q], d = rv[3 * W + q];
-        const uint32_t ab = pick(b, a, 0x05010400), cd = pick(d, c, 0x05010400), ab2 = pick(b, a, 0x07030602), cd2 = pick(d, c, 0x07030602);
-        const uint32_t t[4] = {pick(cd, ab, s0), pick(cd, ab, s1), pick(cd2, ab2, s0), pick(cd2, ab2, s1)};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) *at(4 * q + j) = u32x2{low(t[j], s), high(t[j], s)};
-      }
-    } else {
-      constexpr int W = VB / 2;
-#pragma unroll
-      for (int j = 0; j < VB; ++j) {
-        const int q = j >> 1;
-        const uint32_t sel = j & 1 ? s1 : s0;
-        *at(j) = u32x2{pick(rv[W + q], rv[q], sel), pick(rv[3 * W + q], rv[2 * W + q], sel)};
-      }
-    }
-  }
+  static __device__ __forceinline__ int key_place(int tid) { return key_piece(tid / 8 % 32, KP * (tid % 8)); }
+  static __device__ __forceinline__ int value_place(int tid) { return value_piece(tid / 8 % 32, KP * (tid % 8)); }
 };
 
 // What stands before it is issued before what stands behind.
@@ -706,9 +675,11 @@ __device__ __forceinline__ void here() { __builtin_amdgcn_sched_barrier(0); }
 
 // Blocks of 32 keys: the scores of the next block (eight matrix instructions) stand beside the exponentials of this one, and this one's values (eight) beside
 // the next one's maximum; a slice of vector instructions behind every matrix instruction, laid by hand.  Operands are read from LDS four
-// instructions ahead.  The keys are in LDS a block earlier than the values: a ring of four blocks, two of which are read and two written in a step of two.
-template <int D, int WAVES>
-__device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Staged<D> &s, int lane, int wave) {
+// instructions ahead.  A step is two blocks; step j writes what step j + AHEAD reads, its values and the keys of the blocks behind its first one, and waves meet every AHEAD
+// steps: rings of 4 AHEAD blocks of keys and 2 AHEAD steps of values, half of which are read and half written between two meetings.  AHEAD is 2 where a workgroup has
+// the compute unit to itself (8 x 1024 rows on 5120 keys: 726 us, 734 with 1).
+template <int D, int WAVES, int AHEAD>
+__device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Staged<D, AHEAD> &s, int lane, int wave) {
   typedef Tall<D, WAVES> T;
   constexpr int KC = T::KC, DB = T::DB;
   const int tid = wave * kWave + lane, r = lane & 31, h = lane >> 5;
@@ -727,43 +698,47 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = kLowest, l = 0.f;
 
-  const int last_block = (t.P + kQ8Block - 1) / kQ8Block - 1, end = 2 * t.to;
+  const int last_block = (t.P + kQ8Block - 1) / kQ8Block - 1, end = 2 * t.to, second = wave / 4;  // (of eight waves four have the one of two blocks, four the other)
   auto valid_in = [&](int j) { return j < t.cached ? t.P - j * kStep : t.N - (j - t.cached) * kStep; };  // keys of step j that there are
   auto load_keys = [&](T &to, int i, int b) {  // block b
     const int j = b >> 1, valid = min(valid_in(j) - (b & 1) * kQ8Block, kQ8Block);
     if (b >= end || valid <= 0) return;
     if (j < t.cached) {
-      const Rows k(u.kc, a.cs[1], b * kQ8Block, valid, D);
-      to.load_keys(i, k, tid, true);
+      T::load(to.rk[i], Rows(u.kc, a.cs[1], b * kQ8Block, valid, D), tid, true);
       to.ke = i == 0 ? u.ke[b] : to.ke | u.ke[b] << 8;
     } else {
-      const Rows k(u.ks, a.ks[1], (b - 2 * t.cached) * kQ8Block, valid, 2 * D);
-      to.load_keys(i, k, tid, false);
+      T::load(to.rk[i], Rows(u.ks, a.ks[1], (b - 2 * t.cached) * kQ8Block, valid, 2 * D), tid, false);
       to.ke = i == 0 ? 127 : to.ke | 127 << 8;
     }
   };
-  auto load_values = [&](T &to, int j) {
+  auto load_values = [&](T &to, int j) {  // (those that are not there come as zeros, and have a scale)
     if (j >= t.to) return;
-    const int valid = min(valid_in(j), kStep);
-    if (j < t.cached) {
-      const Rows v(u.vc, a.cs[1], j * kStep, valid, D);
-      to.load_values(v, tid, true);
-      to.ve = u.ve[min(2 * j + tid / (32 * WAVES), last_block)];
-    } else {
-      const Rows v(u.vs, a.ks[1], (j - t.cached) * kStep, valid, 2 * D);
-      to.load_values(v, tid, false);
-      to.ve = 127;
+#pragma unroll
+    for (int i = 0; i < T::kSets; ++i) {
+      const int b = 2 * j + second + i, valid = min(valid_in(j) - (b & 1) * kQ8Block, kQ8Block);
+      if (j < t.cached) {
+        T::load(to.rv[i], Rows(u.vc, a.cs[1], b * kQ8Block, valid, D), tid, true);
+        const uint32_t e = u.ve[min(b, last_block)];
+        to.ve = i == 0 ? e : to.ve | e << 8;
+      } else {
+        T::load(to.rv[i], Rows(u.vs, a.ks[1], (b - 2 * t.cached) * kQ8Block, valid, 2 * D), tid, false);
+        to.ve = 127;
+      }
     }
   };
   auto store_keys = [&](const T &from, int i, int b) {
     if (b >= end) return;
-    if (b < 2 * t.cached) from.store_keys(i, s.k[b & 3], q8_scale(i == 0 ? from.ke & 255 : from.ke >> 8), tid, true);
-    else from.store_keys(i, s.k[b & 3], 1.f, tid, false);
+    if (b < 2 * t.cached) T::store(from.rk[i], s.k[b & (4 * AHEAD - 1)], T::key_place(tid), q8_scale(i == 0 ? from.ke & 255 : from.ke >> 8), true);
+    else T::store(from.rk[i], s.k[b & (4 * AHEAD - 1)], T::key_place(tid), 1.f, false);
   };
   auto store_values = [&](const T &from, int j) {
     if (j >= t.to) return;
-    if (j < t.cached) from.store_values(s.v[j & 1], q8_scale(from.ve), tid, true);
-    else from.store_values(s.v[j & 1], 1.f, tid, false);
+#pragma unroll
+    for (int i = 0; i < T::kSets; ++i) {
+      uint32_t *to = s.v[j & (2 * AHEAD - 1)] + (second + i) * (kQ8Block * D / 2);
+      if (j < t.cached) T::store(from.rv[i], to, T::value_place(tid), q8_scale(i == 0 ? from.ve & 255 : from.ve >> 8), true);
+      else T::store(from.rv[i], to, T::value_place(tid), 1.f, false);
+    }
   };
   auto mask = [&](f32x16 &z, int b) {
     const int valid = valid_in(b >> 1) - (b & 1) * kQ8Block;
@@ -793,10 +768,10 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
   auto block = [&](int b, f32x16 &z, f32x16 &y, auto more, auto pair) {
     constexpr bool MORE = decltype(more)::value;
     constexpr int PAIR = decltype(pair)::value;
-    const uint32_t *k = s.k[(b + 1) & 3], *v = s.v[b >> 1 & 1];
-    const int k0 = anew(T::key_piece(r, h)), v0 = anew(T::value_piece(r, h) ^ 16 * (b & 1));
+    const uint32_t *k = s.k[(b + 1) & (4 * AHEAD - 1)], *v = s.v[b >> 1 & (2 * AHEAD - 1)] + (b & 1) * (kQ8Block * D / 2);
+    const int k0 = anew(T::key_piece(r, h)), v0 = anew(T::value_start(lane));
     auto key = [&](int c) { return *reinterpret_cast<const bf16x8 *>(k + (k0 ^ 8 * c)); };
-    auto value = [&](int i) { return *reinterpret_cast<const bf16x8 *>(v + (v0 ^ 8 * (i / DB)) + 1024 * (i % DB)); };
+    auto value = [&](int i) { return turned<8 * D / 2>(v + (v0 ^ 16 * (i % DB)) + i / DB * (16 * D / 2)); };
     u32x4 P[2];
     float part[2] = {0.f, 0.f};
     if (MORE) {
@@ -835,7 +810,7 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
     for (int i = 0; i < kValues; ++i) {
       o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], __builtin_bit_cast(bf16x8, P[i / DB]), o[i % DB], 0, 0, 0);
       if (i + kAhead < kValues) f[i % kAhead] = value(i + kAhead);
-      else if (PAIR == 1) f[i % kAhead] = *reinterpret_cast<const bf16x8 *>(s.k[(b + 2) & 3] + (k0 ^ 8 * (i + kAhead - kValues)));
+      else if (PAIR == 1) f[i % kAhead] = *reinterpret_cast<const bf16x8 *>(s.k[(b + 2) & (4 * AHEAD - 1)] + (k0 ^ 8 * (i + kAhead - kValues)));
       if (MORE)
 #pragma unroll
         for (int e = 16 * i / kValues; e < 16 * (i + 1) / kValues; e += 2) most = fmaxf(fmaxf(most, y[e]), y[e + 1]);
@@ -844,53 +819,61 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
     if (MORE) look(most);
   };
 
-  const int b0 = 2 * t.from, second = wave / 4;  // (of eight waves four have the one of two blocks, four the other)
+  const int b0 = 2 * t.from;
   // what step j stores.  (A new one each time: what a load leaves out is not the former's.)
   auto load_next = [&](int j) {
     T n;
-    const int b = 2 * j + 3 + second;
-    if (j + 2 < min(t.to, t.cached)) {  // all of it of the cache: one run of loads
-      const Rows v(u.vc, a.cs[1], (j + 1) * kStep, kStep, D);
+    const int b = 2 * (j + AHEAD) + 1 + second;
+    const int bv = 2 * (j + AHEAD) + second;
+    if (j + 1 + AHEAD < min(t.to, t.cached)) {  // all of it of the cache: one run of loads
 #pragma unroll
-      for (int i = 0; i < T::kSets; ++i) n.load_keys(i, Rows(u.kc, a.cs[1], (b + i) * kQ8Block, min(t.P - (b + i) * kQ8Block, kQ8Block), D), tid, true);
-      n.load_values(v, tid, true);
+      for (int i = 0; i < T::kSets; ++i) T::load(n.rk[i], Rows(u.kc, a.cs[1], (b + i) * kQ8Block, min(t.P - (b + i) * kQ8Block, kQ8Block), D), tid, true);
+#pragma unroll
+      for (int i = 0; i < T::kSets; ++i) T::load(n.rv[i], Rows(u.vc, a.cs[1], (bv + i) * kQ8Block, kQ8Block, D), tid, true);
       if constexpr (T::kSets == 2) {
         uint16_t two;
         __builtin_memcpy(&two, u.ke + b, 2);
         n.ke = two;
+        __builtin_memcpy(&two, u.ve + bv, 2);
+        n.ve = two;
       } else {
-        n.ke = u.ke[b];
+        n.ke = u.ke[b], n.ve = u.ve[bv];
       }
-      n.ve = u.ve[2 * (j + 1) + tid / (32 * WAVES)];
-    } else if (j + 1 >= t.cached && j + 2 < t.to) {
-      const int at = (b - 2 * t.cached) * kQ8Block;
-      const Rows v(u.vs, a.ks[1], (j + 1 - t.cached) * kStep, kStep, 2 * D);
+    } else if (j + AHEAD >= t.cached && j + 1 + AHEAD < t.to) {
+      const int at = (b - 2 * t.cached) * kQ8Block, at_v = (bv - 2 * t.cached) * kQ8Block;
 #pragma unroll
-      for (int i = 0; i < T::kSets; ++i) n.load_keys(i, Rows(u.ks, a.ks[1], at + i * kQ8Block, min(t.N - at - i * kQ8Block, kQ8Block), 2 * D), tid, false);
-      n.load_values(v, tid, false);
+      for (int i = 0; i < T::kSets; ++i) T::load(n.rk[i], Rows(u.ks, a.ks[1], at + i * kQ8Block, min(t.N - at - i * kQ8Block, kQ8Block), 2 * D), tid, false);
+#pragma unroll
+      for (int i = 0; i < T::kSets; ++i) T::load(n.rv[i], Rows(u.vs, a.ks[1], at_v + i * kQ8Block, kQ8Block, 2 * D), tid, false);
       n.ke = u.ke[0], n.ve = u.ve[0];  // (of no use, but a constant in their place would wait for the loads before)
     } else {
 #pragma unroll
       for (int i = 0; i < T::kSets; ++i) load_keys(n, i, b + i);
-      load_values(n, j + 1);
+      load_values(n, j + AHEAD);
     }
     return n;
   };
   auto store_next = [&](const T &n, int j) {
 #pragma unroll
-    for (int i = 0; i < T::kSets; ++i) store_keys(n, i, 2 * j + 3 + second + i);
-    store_values(n, j + 1);
+    for (int i = 0; i < T::kSets; ++i) store_keys(n, i, 2 * (j + AHEAD) + 1 + second + i);
+    store_values(n, j + AHEAD);
   };
   {
-    T n, third;
+    T n[AHEAD], last;
 #pragma unroll
-    for (int i = 0; i < T::kSets; ++i) load_keys(n, i, b0 + second + i);
-    if (second == 0) load_keys(third, 0, b0 + 2);
-    load_values(n, t.from);
+    for (int p = 0; p < AHEAD; ++p) {
 #pragma unroll
-    for (int i = 0; i < T::kSets; ++i) store_keys(n, i, b0 + second + i);
-    if (second == 0) store_keys(third, 0, b0 + 2);
-    store_values(n, t.from);
+      for (int i = 0; i < T::kSets; ++i) load_keys(n[p], i, b0 + 2 * p + second + i);
+      load_values(n[p], t.from + p);
+    }
+    if (second == 0) load_keys(last, 0, b0 + 2 * AHEAD);
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+#pragma unroll
+      for (int i = 0; i < T::kSets; ++i) store_keys(n[p], i, b0 + 2 * p + second + i);
+      store_values(n[p], t.from + p);
+    }
+    if (second == 0) store_keys(last, 0, b0 + 2 * AHEAD);
   }
   T next = load_next(t.from);
   __syncthreads();
@@ -898,7 +881,7 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
     f32x16 z, y;
     clear(z);
     {
-      const uint32_t *k = s.k[b0 & 3];
+      const uint32_t *k = s.k[b0 & (4 * AHEAD - 1)];
       const int k0 = T::key_piece(r, h);
 #pragma unroll
       for (int c = 0; c < KC; ++c) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(k + (k0 ^ 8 * c)), q[c], z, 0, 0, 0);
@@ -914,7 +897,7 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
       next = load_next(j + 1);
       block(2 * j, z, y, std::true_type(), std::integral_constant<int, 1>());
       block(2 * j + 1, y, z, std::true_type(), std::integral_constant<int, 2>());
-      __syncthreads();
+      if (AHEAD == 1 || (j - t.from) % AHEAD == AHEAD - 1) __syncthreads();
     }
     block(end - 2, z, y, std::true_type(), std::integral_constant<int, 0>());
     block(end - 1, y, z, std::false_type(), std::integral_constant<int, 0>());
@@ -923,7 +906,7 @@ __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, co
     for (int j = t.from; j + 1 < t.to; ++j) {
       store_next(next, j);
       next = load_next(j + 1);
-      __syncthreads();
+      if (AHEAD == 1 || (j - t.from) % AHEAD == AHEAD - 1) __syncthreads();
     }
   }
   if (!live || mine + r >= t.entries) return;
@@ -998,7 +981,7 @@ template <int D, int WAVES, bool TALL>
 __global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a, Q8Layers L) {
   union alignas(1024) Shared {
     Joined<D, WAVES> joined;
-    Staged<TALL ? D : 64> staged;
+    Staged<TALL ? D : 64, 1> staged;
     __device__ Shared() {}
   };
   __shared__ Shared s;
@@ -1006,7 +989,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a,
   all_items(a, L, lane, [&](const Item &t) {
     const int own = anew(lane);  // (what an item makes of it is not kept for the next one, in registers that the other kinds of items need)
     if (TALL && t.rows > 32) {
-      if constexpr (TALL) tall_item<D, WAVES>(a, Unit(a, L, t), t, s.staged, own, wave);
+      if constexpr (TALL) tall_item<D, WAVES, 1>(a, Unit(a, L, t), t, s.staged, own, wave);
     } else if (t.rows == 32) {
       if (t.entries <= 32) short_item<D, 2, WAVES, true>(a, L, t, s.joined, own, wave);
       else short_item<D, 2, WAVES, false>(a, L, t, s.joined, own, wave);
@@ -1018,9 +1001,9 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_q8_kernel(Q8AttnArgs a,
 // Tall tiles of eight waves.
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_q8_tall_kernel(Q8AttnArgs a, Q8Layers L) {
-  __shared__ Staged<D> s;
+  __shared__ Staged<D, 2> s;
   const int lane = threadIdx.x & (kWave - 1), wave = first_lane(threadIdx.x / kWave);
-  all_items(a, L, lane, [&](const Item &t) { tall_item<D, 8>(a, Unit(a, L, t), t, s, anew(lane), wave); });
+  all_items(a, L, lane, [&](const Item &t) { tall_item<D, 8, 2>(a, Unit(a, L, t), t, s, anew(lane), wave); });
 }
 
 // The parts of divided tiles, joined: a wave to an entry.
