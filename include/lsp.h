@@ -564,7 +564,7 @@ int32_t lsp_qk_norm_rope(const lsp_qk_norm_rope_desc *desc, const void *q, const
  * No length is changed: lsp_commit (with num_layers = 0 and this C) has advanced them; a prompt is
  * appended with commit_len = prefix_len = its length, S being the rows of the buffers that hold its K/V.
  * desc: dtype (of the suffix buffers, LSP_F32 or LSP_BF16), B, S, Hkv, D, C, kv_suf_stride, cache_stride
- * (a cache's rows must be those of one sequence); the rest is not used.  *_layers: HOST arrays of num_layers
+ * (a cache's rows must be those of one sequence, and of one layer's keys or values); the rest is not used.  *_layers: HOST arrays of num_layers
  * DEVICE pointers, as for lsp_commit; buffers 16-byte aligned, scales of any alignment.
  */
 int32_t lsp_kv_append_q8(const lsp_attn_desc *desc, int32_t num_layers, const void *const *k_suf_layers,

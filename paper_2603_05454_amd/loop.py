@@ -127,7 +127,7 @@ class _EightBits:
             raise LspError(f"decode_loop: kv_layers of {lists[0][0].shape[0]} sequences for {tokens.shape[0]}")
         if k.shape[1] < tokens.shape[1]:
             raise LspError(f"decode_loop: caches of {k.shape[1]} rows for token buffers of {tokens.shape[1]}")
-        self.workspace = None
+        self.rows, self.workspace = lists[0][0].shape[1], None
 
     def attend(self, prefix_len, suffix_len):
         if self.workspace is None:
@@ -249,6 +249,8 @@ def decode_loop(logits_fn, bitmap, V, tau, window, min_commit, snap_enabled,
 
     def one_step(z):
         nonlocal out, conf, attn_out, ws
+        if eight and eight.rows < z.shape[1]:
+            raise LspError(f"decode_loop: suffix buffers of {eight.rows} rows for logits of {z.shape[1]}")
         if run_attention and eight:
             eight.attend(prefix_len, suffix_len)
         elif run_attention and kv_layers is not None:

@@ -201,3 +201,14 @@ def test_a_decoder_s_step(lsp):
         assert all(torch.equal(one[k], two[k]) for k in ("prefix_len", "suffix_len", "tokens"))
         assert all(torch.equal(a, b) for a, b in zip(_caches(one["eight"]), _caches(two["eight"])))
     assert torch.equal(one["tokens"], s["tokens"]) and all(torch.equal(a, b) for a, b in zip(_caches(one["eight"]), _caches(s["eight"])))
+
+
+def test_loop_refuses_suffix_buffers_that_lack_rows(lsp):
+    """Rows that a step commits have to be there to be appended."""
+    w = _work()
+    s = _start(lsp, w)
+    kept = [s[k].clone() for k in ("prefix_len", "suffix_len", "tokens")]
+    for attend in (False, True):
+        with pytest.raises(lsp.LspError, match="rows for logits"):
+            _loop(w, s, [{k: v[:, :w.S - 1] if k in ("q", "k_suf", "v_suf") else v for k, v in L.items()} for L in s["eight"]], run_attention=attend)
+    assert all(torch.equal(a, s[k]) for a, k in zip(kept, ("prefix_len", "suffix_len", "tokens")))
