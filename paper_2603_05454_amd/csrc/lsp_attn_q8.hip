@@ -160,8 +160,8 @@ struct Plan {
   // Items are dealt out to the XCDs by unit (of a short tile: by its heads); where a sequence's units are no multiple of 8, each unit's items to 2^pieces of them.
   __device__ __forceinline__ static int pieces_of(int units) { return 3 - min(__builtin_ctz(units), 3); }
   __device__ __forceinline__ int splits_of(const Shape &s) const { return split ? (s.steps + chunk - 1) / chunk : 1; }  // of a tile
-  __device__ __forceinline__ void take(const Q8AttnArgs &a, int lane) {
-    n = lens_of(a, b0 + lane);
+  __device__ __forceinline__ void take(const Q8AttnArgs &a, int lane, bool first = false) {  // first: the lanes have the lengths already
+    if (b0 > 0 || !first) n = lens_of(a, b0 + lane);
     const Shape s = shape_of(a, n);
     const int items = s.tiles * splits_of(s), units = a.per_seq >> heads_of(s), pieces = pieces_of(units);
     end = running_sum((units << pieces) / kXcds * ((items + (1 << pieces) - 1) >> pieces));
@@ -173,11 +173,12 @@ struct Plan {
     chunk = 1 << 30;
     split = false;
     heads = 0;
+    n = lens_of(a, lane);
     if (a.parts != nullptr || a.heads > 0) {
       int all = 0, slots = 0, most = 0;
       float work = 0.f;
       for (int b = 0; b < a.B; b += kWave) {
-        const Shape x = shape_of(a, lens_of(a, b + lane));
+        const Shape x = shape_of(a, b == 0 ? n : lens_of(a, b + lane));
         all += a.per_seq * x.tiles;
         slots += a.per_seq * x.tiles * ((x.rows + 31) / 32);
         most = max(most, x.tiles > 0 ? x.steps : 0);
@@ -203,7 +204,7 @@ struct Plan {
       }
     }
     b0 = base = slot_base = 0;
-    take(a, lane);
+    take(a, lane, true);
   }
   // Brings the lanes to the sequence of item q of an XCD's list: its lane, or -1 behind the last item.
   __device__ __forceinline__ int find(const Q8AttnArgs &a, int q, int lane) {
@@ -550,43 +551,44 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Q8Layers &
                   r, h);
   }
 
-  // The waves' parts: what all have in a place of their lanes is added by one of them.
+  // The waves' parts: what all have in a place of their lanes is added by one of them, each times what its reference is to the largest.  (A wave that met no key
+  // has zeros; all reads at once, and those of other heads' waves are not used.)
   __syncthreads();
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const float l = quad_sum(x.l[n]);
     if (n > 0) __syncthreads();
     if (h == 0) s.m[wave][r] = x.m[n], s.l[wave][r] = l;
-    __syncthreads();
-    float m = -INFINITY, sum = 0.f, ms[WAVES], ls[WAVES];
-    // (all reads at once, one behind the other they were 2 us of a short call; those of other heads' waves are not used)
-#pragma unroll
-    for (int k = 0; k < WAVES; ++k) {
-      const int w = (sub + (k << t.heads)) % WAVES;
-      ms[k] = s.m[w][r], ls[k] = k < turns ? s.l[w][r] : 0.f;
-      m = fmaxf(m, k < turns ? ms[k] : -INFINITY);
-    }
-    // (a wave that met no key has zeros)
-#pragma unroll
-    for (int k = 0; k < WAVES; ++k) sum += ls[k] != 0.f ? ls[k] * __builtin_amdgcn_exp2f(ms[k] - m) : 0.f;
-    const float f = l != 0.f ? __builtin_amdgcn_exp2f(x.m[n] - m) : 0.f;
 #pragma unroll
     for (int p = 0; p < VJ; ++p) {  // elements 4 p to 4 p + 3 of the lane's 4 VJ
       f32x4 y;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = f * x.o[n][(4 * p + j) % VJ][(4 * p + j) / VJ];
+      for (int j = 0; j < 4; ++j) y[j] = x.o[n][(4 * p + j) % VJ][(4 * p + j) / VJ];
       s.o[wave][p][lane] = y;
     }
     __syncthreads();
     const int e = 16 * n + r;
     if (t.entry + e < t.entries) {
+      float m = kLowest, sum = 0.f, f[WAVES], ls[WAVES];
+#pragma unroll
+      for (int k = 0; k < WAVES; ++k) {
+        const int w = (sub + (k << t.heads)) % WAVES;
+        f[k] = k < turns ? s.m[w][r] : kLowest;
+        ls[k] = s.l[w][r];
+        m = fmaxf(m, f[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < WAVES; ++k) {
+        f[k] = __builtin_amdgcn_exp2f(f[k] - m);
+        if (k < turns) sum += f[k] * ls[k];
+      }
       for (int p = turn; p < VJ; p += turns) {
-        f32x4 y = s.o[sub][p][lane], o[WAVES];
+        f32x4 y = {0.f, 0.f, 0.f, 0.f}, o[WAVES];
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k) o[k] = s.o[(sub + (k << t.heads)) % WAVES][p][lane];
+        for (int k = 0; k < WAVES; ++k) o[k] = s.o[(sub + (k << t.heads)) % WAVES][p][lane];
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k)
-          if (k < turns) y += o[k];
+        for (int k = 0; k < WAVES; ++k)
+          if (k < turns) y += f[k] * o[k];
         const int d = 4 * VJ * h + 4 * p;
         if (t.slot < 0) {
           const float inv = 1.f / sum;
@@ -953,14 +955,14 @@ __device__ __forceinline__ void all_items(const Q8AttnArgs &a, const Q8Layers &L
     const int splits = plan.splits_of(shape), items = shape.tiles * splits;
     const int before = plan.base + (at > 0 ? at_lane(plan.end, max(at - 1, 0)) : 0), in_seq = q - before;
     const int heads = plan.heads_of(shape), pieces = plan.pieces_of(a.per_seq >> heads);
-    const int per_piece = (items + (1 << pieces) - 1) >> pieces, piece = in_seq / per_piece, list = piece * kXcds + xcd;
+    const int per_piece = (items + (1 << pieces) - 1) >> pieces, piece = per_piece == 1 ? in_seq : in_seq / per_piece, list = piece * kXcds + xcd;
     const int unit = (list >> pieces) << heads, item = ((in_seq - piece * per_piece) << pieces) + (list & ((1 << pieces) - 1));
     if (item >= items) continue;
     t.b = first_lane(t.b);
     t.heads = heads;
     t.l = first_lane(quotient(unit, a.by_heads));
     t.g = first_lane(unit - t.l * a.Hkv);
-    const int tile = item / splits, part = item - tile * splits;
+    const int tile = splits == 1 ? item : item / splits, part = item - tile * splits;
     t.entry = first_lane(tile * t.rows);
     t.from = first_lane(part * plan.chunk);
     t.to = splits == 1 ? shape.steps : min(t.from + plan.chunk, shape.steps);
