@@ -4,7 +4,7 @@
 // Bound by the bytes of the rows, read once and written once.  All heads of a row turn by the same angles: a workgroup works them out once, a thread
 // each, into LDS.  The product position * inv_freq is taken in 64 bits (in 32 the angle of position 100 000 is off by up to 0.004) and reduced there to
 // an eighth of a turn about a quarter; sine and cosine of that are their power series in 32 bits, to x^9 and x^10, whose next terms are below
-// 2e-9 and 1e-10.  Everything behind is 32 bits, rounded once.  8192 rows of 64 heads of 128, 268 MB in and out, take 44 us (6.1 TB/s); one row 2.6 us.
+// 2e-9 and 1e-10.  Everything behind is 32 bits, rounded once.  8192 rows of 64 heads of 128, 268 MB in and out, take 41 us (6.5 TB/s); one row 2.6 us.
 #include <math.h>
 
 #include "lsp_q8.h"
@@ -130,8 +130,9 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, bool in
 
 template <typename T>
 void launch(const RopeArgs &a, int B, int D, bool interleaved, hipStream_t st) {
-  // Few rows: a workgroup each.
-  const bool few = int64_t(B) * a.S <= 1024;
+  // A workgroup has one row where its heads are work for all threads (8192 rows of 64 heads of 128: 41 us, with four rows 44; 1024 of 32 heads 5.6 and 7.4), or
+  // where rows are few (512 of 10 heads: 4.0 and 4.7); else four, which share the angles' latency (8192 rows of 10 heads: 12.5 with one, 10.2).
+  const bool few = a.heads * (D * int64_t(sizeof(T)) / 32) >= kThreads || int64_t(B) * a.S <= 2048;
   const dim3 grid(unsigned(few ? a.S : (a.S + 3) / 4), unsigned(B));
   if (D == 64) {
     if (few) norm_rope_kernel<T, 64, 1><<<grid, kThreads, 0, st>>>(a, interleaved);
