@@ -4,6 +4,8 @@
 // exponent byte with a <= 448 * 2^(E - 127); powers of two cost an e4m3 value nothing (its own exponent takes them up) and make multiplying by a
 // scale, and rounding again under a larger one, exact but for what becomes subnormal.  Bound by the bytes: 16 bits read and 8 written for each number, or the other way
 // round (the prompt below: 6.1 TB/s written, 4.7 read back; a large copy reaches 4.9).
+#include <type_traits>
+
 #include "lsp_q8.h"
 
 namespace lsp {
@@ -200,23 +202,24 @@ __global__ __launch_bounds__(kThreads) void read_kernel(KvArgs a, Q8Layers L) {
   const uint8_t *scales = (values ? L.of[l].v_scale : L.of[l].k_scale) + int64_t(b) * a.Hkv * a.blocks;
   const int d = (threadIdx.x % kLanes) * 16;
   const int items = n * a.Hkv, step = gridDim.x * kHeads;
-  for (int it = blockIdx.x * kHeads + threadIdx.x / kLanes; it < items; it += kAtOnce * step) {
-    u32x4 w[kAtOnce];
-    uint32_t E[kAtOnce];
-    int i[kAtOnce], g[kAtOnce];
+  int it = blockIdx.x * kHeads + threadIdx.x / kLanes;
+  auto some = [&](auto count) {
+    constexpr int N = decltype(count)::value;
+    u32x4 w[N];
+    uint32_t E[N];
+    char *to[N];
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int at = min(it + int64_t(k) * step, int64_t(items - 1));
-      i[k] = quotient(at, a.by_heads), g[k] = at - i[k] * a.Hkv;
-      const int t = first + i[k];
-      w[k] = load_once<ONCE, u32x4>(cache + int64_t(t) * a.cs[1] + g[k] * a.cs[2] + d);
-      E[k] = scales[int64_t(g[k]) * a.blocks + t / kQ8Block];
+    for (int k = 0; k < N; ++k, it += step) {
+      const int i = quotient(it, a.by_heads), g = it - i * a.Hkv, t = first + i;
+      w[k] = load_once<ONCE, u32x4>(cache + int64_t(t) * a.cs[1] + g * a.cs[2] + d);
+      E[k] = scales[int64_t(g) * a.blocks + t / kQ8Block];
+      to[k] = out + int64_t(i) * a.ss[1] + g * a.ss[2] + d * int(sizeof(T));
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k)
-      if (it + int64_t(k) * step < items)
-        store16(out + int64_t(i[k]) * a.ss[1] + g[k] * a.ss[2] + d * int(sizeof(T)), w[k], q8_scale(E[k]), static_cast<T *>(nullptr));
-  }
+    for (int k = 0; k < N; ++k) store16(to[k], w[k], q8_scale(E[k]), static_cast<T *>(nullptr));
+  };
+  while (it + int64_t(kAtOnce - 1) * step < items) some(std::integral_constant<int, kAtOnce>());
+  while (it < items) some(std::integral_constant<int, 1>());
 }
 
 KvArgs kv_args(const AttnArgs &a, const lsp_attn_desc *d, const int32_t *from, const int32_t *to) {
