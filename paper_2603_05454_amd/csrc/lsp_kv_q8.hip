@@ -3,7 +3,7 @@
 // A block is 32 rows of one head, one wave's.  With a = the largest finite magnitude of its new rows and 448 that of e4m3, E is the smallest
 // exponent byte with a <= 448 * 2^(E - 127); powers of two cost an e4m3 value nothing (its own exponent takes them up) and make multiplying by a
 // scale, and rounding again under a larger one, exact but for what becomes subnormal.  Bound by the bytes: 16 bits read and 8 written for each number, or the other way
-// round (the prompt below: 6.1 TB/s written, 4.7 read back; a large copy reaches 4.9).
+// round (the prompt below: 6.1 TB/s written, 5.1 read back; a large copy reaches 4.9).
 #include <type_traits>
 
 #include "lsp_q8.h"
@@ -49,8 +49,8 @@ struct Eight {
   float x[8];
 };
 // ONCE: nontemporal.  Where the buffers are larger than the last cache (256 MB), what a call reads or writes once need not stay there: 4 x 4096 rows of 32 heads
-// in two layers, 0.8 GB, are appended in 131 us so and 148 without, and appended and read back in 303 and 328; where they are smaller it is better kept: 64
-// rows of 8 sequences in four layers 37 and 32 us.  The reading's own writes are plain ones: 167 us against 174.
+// in two layers, 0.8 GB, are appended in 131 us so and 148 without, and appended and read back in 294 and 314; where they are smaller it is better kept: 64
+// rows of 8 sequences in four layers 36 and 31 us.  The reading's own writes are plain ones: 156 us against 167.
 constexpr int64_t kLastCache = int64_t(256) << 20;
 template <bool ONCE, typename V>
 __device__ __forceinline__ V load_once(const char *p) {
@@ -190,7 +190,7 @@ __device__ __forceinline__ void store16(char *p, u32x4 w, float scale, const flo
 }
 
 constexpr int kAtOnce = 4;
-// 16 values a lane and step, four steps at once.  Exact in both types.
+// 16 values a lane and step, four steps at once (of 32 layers' 8 x 64 rows 76 us, with two 83, with eight 81), what is left singly.
 template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(kThreads) void read_kernel(KvArgs a, Q8Layers L) {
   constexpr int kLanes = D / 16, kHeads = kThreads / kLanes;
