@@ -135,3 +135,24 @@ def test_graph(lsp):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_offsets_beyond_32_bits(lsp):
+    """2.2e9 numbers, in place: rows on both sides of 2^31 elements and bytes."""
+    B, S, Hq, H, D = 2, 8300, 1024, 1, 128
+    g = torch.Generator().manual_seed(8)
+    q, k = torch.zeros((B, S, Hq, D), dtype=torch.bfloat16, device="cuda"), torch.randn((B, S, H, D), generator=g).to(torch.bfloat16).cuda()
+    rows = [(0, 0), (0, 4095), (0, 4096), (0, 8191), (0, 8192), (0, 8299), (1, 0), (1, 8083), (1, 8084), (1, 8298)]
+    x = torch.randn((len(rows), Hq, D), generator=g).to(torch.bfloat16)
+    for i, (b, u) in enumerate(rows):
+        q[b, u] = x[i].cuda()
+    q[1, 8299] = 3.0
+    w = torch.randn(D, generator=g)
+    f, lens = _freq(D), [torch.tensor(v, dtype=torch.int32) for v in ([5, 9], [S, S - 1])]
+    lsp.qk_norm_rope(q, k, f.cuda(), q_weight=w.cuda(), k_weight=w.cuda(), eps=1e-5, prefix_len=lens[0].cuda(), suffix_len=lens[1].cuda(), out=(q, k))
+    for i, (b, u) in enumerate(rows):
+        pos = torch.tensor([[int(lens[0][b]) + u]], dtype=torch.int32)
+        (want, size), _ = eight_bits.norm_rope(x[i].view(1, 1, Hq, D), x[i].view(1, 1, Hq, D), f, w, w, eps=1e-5, positions=pos)
+        _close(q[b, u].view(1, 1, Hq, D), want, size, x[i].view(1, 1, Hq, D), torch.bfloat16, [1])
+    assert (q[1, 8299] == 3.0).all()
+    assert q[0, 1].abs().max() == 0 and q[1, 4000].abs().max() == 0
