@@ -169,7 +169,8 @@ struct Plan {
   }
   // How long the items are: all keys of a tile, or, where workgroups would be without one, part of them.  Lane i looks at i + 1 parts (from 32 on at
   // multiples of 8).  A round of items takes its steps and about four steps' time to begin and end, joining the parts as much again.
-  __device__ __forceinline__ void start(const Q8AttnArgs &a, int lane) {
+  // false: there is nothing to do, as for one of two kernels often (which then ends as early as it can).
+  __device__ __forceinline__ bool choose(const Q8AttnArgs &a, int lane) {
     chunk = 1 << 30;
     split = false;
     heads = 0;
@@ -185,12 +186,15 @@ struct Plan {
         work += x.rows > 32 ? 0.f : float(a.per_seq * x.tiles) * float(x.steps);
       }
       all = wave_sum(all);
+      if (all == 0) return false;
+      if (a.heads > 0) {
+        const int total = at_lane(running(__float_as_int(work), 0, [](int p, int q) { return __float_as_int(__int_as_float(p) + __int_as_float(q)); }), kWave - 1);
+        if (__int_as_float(total) >= kBeside) heads = a.heads;
+      }
       slots = wave_sum(slots);
-      most = at_lane(running(most, 0, [](int p, int q) { return max(p, q); }), kWave - 1);
-      const int total = at_lane(running(__float_as_int(work), 0, [](int p, int q) { return __float_as_int(__int_as_float(p) + __int_as_float(q)); }), kWave - 1);
-      if (__int_as_float(total) >= kBeside) heads = a.heads;
-      const int tiles = (all + (1 << heads) - 1) >> heads;
-      if (a.parts != nullptr && tiles > 0 && slots <= kSlots / 2) {
+      if (a.parts != nullptr && slots <= kSlots / 2) {
+        const int tiles = (all + (1 << heads) - 1) >> heads;
+        most = at_lane(running(most, 0, [](int p, int q) { return max(p, q); }), kWave - 1);
         const int k = lane < 32 ? lane + 1 : 32 + 8 * (lane - 31), part = (most + k - 1) / k;
         const bool fits = k == 1 || (int64_t(slots) * k <= kSlots && part >= kLeast);
         const int64_t rounds = (int64_t(tiles) * k + a.groups - 1) / a.groups, cost = rounds * ((part << heads) + 4) + (k > 1 ? 4 + k / 8 : 0);
@@ -203,8 +207,13 @@ struct Plan {
         }
       }
     }
+    return true;
+  }
+  __device__ __forceinline__ bool start(const Q8AttnArgs &a, int lane) {
+    if (!choose(a, lane)) return false;
     b0 = base = slot_base = 0;
     take(a, lane, true);
+    return true;
   }
   // Brings the lanes to the sequence of item q of an XCD's list: its lane, or -1 behind the last item.
   __device__ __forceinline__ int find(const Q8AttnArgs &a, int q, int lane) {
@@ -940,7 +949,7 @@ template <typename F>
 __device__ __forceinline__ void all_items(const Q8AttnArgs &a, const Q8Layers &L, int lane, F does) {
   const int xcd = blockIdx.x % kXcds, stride = a.groups / kXcds;
   Plan plan;
-  plan.start(a, lane);
+  if (!plan.start(a, lane)) return;
   for (int q = blockIdx.x / kXcds;; q += stride) {
     const int at = plan.find(a, q, lane);
     if (at < 0) break;
@@ -1012,8 +1021,7 @@ __global__ __launch_bounds__(512, 2) void attn_q8_tall_kernel(Q8AttnArgs a, Q8La
 template <int D>
 __device__ __forceinline__ void join(const Q8AttnArgs &a, const Q8Layers &L, int lane) {
   Plan plan;
-  plan.start(a, lane);
-  if (!plan.split) return;
+  if (!plan.choose(a, lane) || !plan.split) return;
   // entries of all units of sequences, instead of items of an XCD
   const int waves = gridDim.x * 4;
   int first = blockIdx.x * 4 + first_lane(threadIdx.x / kWave), slots = 0, before = 0;
@@ -1093,6 +1101,7 @@ int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_
   b.above = kTall;
   b.up_to = 1 << 30;
   b.tall = kTallest;
+  b.heads = 0;
   if (a.parts != nullptr) b.parts = a.parts + parts_bytes(D) / sizeof(float);
   if constexpr (D == 128)
     if (tallest) attn_q8_tall_kernel<D><<<b.groups, 512, 0, st>>>(b, L);
