@@ -1017,7 +1017,8 @@ __global__ __launch_bounds__(512, 2) void attn_q8_tall_kernel(Q8AttnArgs a, Q8La
   all_items(a, L, lane, [&](const Item &t) { tall_item<D, 8, 2>(a, Unit(a, L, t), t, s, anew(lane), wave); });
 }
 
-// The parts of divided tiles, joined: a wave to an entry.
+constexpr int kAtOnce = 8;
+// The parts of divided tiles, joined: a wave to an entry, which has eight parts on their way at once.
 template <int D>
 __device__ __forceinline__ void join(const Q8AttnArgs &a, const Q8Layers &L, int lane) {
   Plan plan;
@@ -1038,17 +1039,30 @@ __device__ __forceinline__ void join(const Q8AttnArgs &a, const Q8Layers &L, int
       const int per_part = (rows + 31) / 32, items = tiles * splits;
       const int slot = slots + (at_lane(plan.slot_end, at) - a.per_seq * items * per_part) + (unit * items + tile * splits) * per_part;
       const int row = e - tile * rows;
-      float m = -INFINITY;
+      float m = kLowest;
       for (int k = lane; k < splits; k += kWave) m = fmaxf(m, part_stats<D>(a, slot + k * per_part, row)[0]);
-#pragma unroll
-      for (int x = 1; x < kWave; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+      m = __int_as_float(at_lane(running(__float_as_int(m), __float_as_int(kLowest), [](int p, int q) { return __float_as_int(fmaxf(__int_as_float(p), __int_as_float(q))); }),
+                                 kWave - 1));
       float o[D / kWave] = {}, sum = 0.f;
-      for (int k = 0; k < splits; ++k) {
-        const float *st = part_stats<D>(a, slot + k * per_part, row), *p = part_at<D>(a, slot + k * per_part, row) + lane * (D / kWave);
-        const float f = __builtin_amdgcn_exp2f(st[0] - m);
-        sum += st[1] * f;
+      for (int k0 = 0; k0 < splits; k0 += kAtOnce) {
+        f32x2 st[kAtOnce];
+        float p[kAtOnce][D / kWave];
 #pragma unroll
-        for (int j = 0; j < D / kWave; ++j) o[j] += p[j] * f;
+        for (int k = 0; k < kAtOnce; ++k) {
+          const int part = slot + min(k0 + k, splits - 1) * per_part;
+          st[k] = *reinterpret_cast<const f32x2 *>(part_stats<D>(a, part, row));
+#pragma unroll
+          for (int j = 0; j < D / kWave; ++j) p[k][j] = part_at<D>(a, part, row)[lane * (D / kWave) + j];
+        }
+        here();
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const bool there = k0 + k < splits;
+          const float f = __builtin_amdgcn_exp2f(st[k][0] - m);
+          sum = there ? sum + st[k][1] * f : sum;
+#pragma unroll
+          for (int j = 0; j < D / kWave; ++j) o[j] = there ? o[j] + p[k][j] * f : o[j];
+        }
       }
       Item t = {};
       t.b = b0 + at;
