@@ -587,7 +587,8 @@ int32_t lsp_kv_read_q8(const lsp_attn_desc *desc, int32_t num_layers, const void
  * lsp_attn_step over caches in 8 bits: the P_b cached rows are the values they stand for, the suffix K/V, queries
  * and outputs bf16 (dtype LSP_BF16 only).  Arguments as there beside the scales; cache_stride as above.
  * workspace: device, 16-byte aligned, lsp_attn_q8_workspace_bytes(desc, num_layers) bytes of any content
- * (none up to C + S = 2048, else 0.27 MB x D, twice that where D = 128 and S * Hq / Hkv > 128), for this call alone until
+ * (none up to C + S = 1024, or 2048 where B * Hkv * num_layers (32 at most) > 64; else 0.27 MB x D, twice that where D = 128 and
+ * S * Hq / Hkv > 128), for this call alone until
  * it has run; with it the keys of few rows are divided between workgroups, without (NULL, or fewer bytes) a tile's
  * keys are one workgroup's.  Parts are added in order: the same operands give the same bits, with a workspace of one kind.
  * Limits: those of lsp_attn_step; C, S <= 2^30, B * Hkv < 2^23, B * S * Hq and S * Hq / Hkv < 2^30; a row stride of K and V of

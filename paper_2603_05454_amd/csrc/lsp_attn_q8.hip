@@ -30,9 +30,9 @@ constexpr int kTall = 128;       // entries up to which, beyond that, a tile has
 constexpr int kTallest = 256;    // entries of a tile of the others (heads of 128)
 constexpr int kXcds = 8;
 constexpr int kSlots = 2048;     // parts of 32 entries in the workspace, for each of two kernels
-// C + S beyond which keys are divided among workgroups at all: one row on 2000 keys takes 16.8 us in one part and 17.0 in several, on 4000 keys 27.5
-// and 19.4, on 12000 67.9 and 24.2; and where the plan divides nothing, the kernel that would join the parts takes 3 us.
-constexpr int kPartKeys = 2048;
+// C + S beyond which keys are divided among workgroups at all, with up to so many units and with more: one row of 4 heads on 2000 keys takes 17.2 us in one part and 15.2 in
+// several, on 12 000 68 and 18.6; but where units are work for all (256 of them on 1024 keys: 21.2 us) the kernel that would join the parts takes 3 us.
+constexpr int kFewUnits = 64, kPartKeysFew = 1024, kPartKeys = 2048;
 constexpr int kLeast = 4;        // steps of a part, at least
 constexpr int kOnce = 2;         // of a buffer read: nontemporal, the caches need not keep it
 // Steps of all short tiles from which on a workgroup's waves have up to four heads beside each other.  A row of the cache holds a head's 128 bytes beside
@@ -187,12 +187,15 @@ struct Plan {
       }
       all = wave_sum(all);
       if (all == 0) return false;
+      slots = wave_sum(slots);
+      const bool divides = a.parts != nullptr && slots <= kSlots / 2;
       if (a.heads > 0) {
         const int total = at_lane(running(__float_as_int(work), 0, [](int p, int q) { return __float_as_int(__int_as_float(p) + __int_as_float(q)); }), kWave - 1);
         if (__int_as_float(total) >= kBeside) heads = a.heads;
+        // fewer where workgroups would be without work (8 x 32 units on 2000 keys: 30 us, with four heads 52), unless keys are to be divided in any case
+        while (heads > 0 && (all >> heads) < a.groups && (!divides || all >= a.groups)) --heads;
       }
-      slots = wave_sum(slots);
-      if (a.parts != nullptr && slots <= kSlots / 2) {
+      if (divides) {
         const int tiles = (all + (1 << heads) - 1) >> heads;
         most = at_lane(running(most, 0, [](int p, int q) { return max(p, q); }), kWave - 1);
         const int k = lane < 32 ? lane + 1 : 32 + 8 * (lane - 31), part = (most + k - 1) / k;
@@ -1086,7 +1089,7 @@ __global__ __launch_bounds__(256) void join_kernel(Q8AttnArgs a, Q8AttnArgs tall
   if (tallest.groups > 0) join<D>(tallest, L, lane);
 }
 
-bool divides(int64_t C, int64_t S) { return C + S > kPartKeys; }
+bool divides(int64_t C, int64_t S, int64_t units) { return C + S > (units <= kFewUnits ? kPartKeysFew : kPartKeys); }
 // whether some unit may have more entries than tiles of four waves are for
 bool has_tallest(int64_t entries, int D) { return D == 128 && entries > kTall; }
 size_t parts_bytes(int D) { return size_t(kSlots) * 32 * (D + 2) * sizeof(float); }
@@ -1158,7 +1161,8 @@ extern "C" size_t lsp_attn_q8_workspace_bytes(const lsp_attn_desc *d, int32_t nu
   using namespace lsp;
   AttnArgs c;
   if (check("lsp_attn_q8_workspace_bytes", d, num_layers, c) != LSP_OK) return 0;
-  return divides(c.C, c.S) ? parts_bytes(c.D) * (has_tallest(int64_t(c.S) * (c.Hq / c.Hkv), c.D) ? 2 : 1) : 0;
+  const int64_t units = int64_t(c.B) * c.Hkv * (num_layers < kMaxAttnLayers ? num_layers : kMaxAttnLayers);
+  return divides(c.C, c.S, units) ? parts_bytes(c.D) * (has_tallest(int64_t(c.S) * (c.Hq / c.Hkv), c.D) ? 2 : 1) : 0;
 }
 
 extern "C" int32_t lsp_attn_step_q8_layers(const lsp_attn_desc *d, int32_t num_layers, const void *const *q_layers, const void *const *k_suf_layers,

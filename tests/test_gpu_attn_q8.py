@@ -282,3 +282,10 @@ def test_scores_of_minus_infinity_weigh_nothing(lsp, D, S, Hq, P, first):
     out = torch.full((B, S, Hq, D), POISON, dtype=torch.bfloat16, device="cuda")
     lsp.attn_step_q8(*[x.cuda() for x in t], *[torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([P, P], N)], out=out)
     _close(out, want, mass, N, S)
+
+
+@pytest.mark.parametrize("B, H, L, P", [(8, 32, 1, 1900), (1, 32, 16, 1000), (3, 16, 8, 1300), (2, 20, 9, 1500)])
+def test_few_heads_beside_each_other(lsp, B, H, L, P):
+    """Work enough for heads beside each other, but not for all workgroups: fewer heads to each."""
+    N = [4 - b % 3 for b in range(B)]
+    _run(lsp, B, 4, H, H, 64, P + 10, [P - b for b in range(B)], N, 90 + H, L)
