@@ -309,25 +309,23 @@ struct Keys {
   static __device__ __forceinline__ int key_place(int r, int h) { return D == 128 ? r * 128 + 16 * (h ^ r / 2 % 8) : r * 64 + 16 * (h ^ r / 4 % 4); }
   static __device__ __forceinline__ int value_place(int r, int h) { return D == 128 ? 4 * h * 128 + 8 * r : 4 * h * 64 + 4 * r; }
   // Waits for a block's keys (or values), behind which three times as many loads have been asked for, reads them and waits for that, in one.
-  template <int SLOT>
   __device__ __forceinline__ void read_keys(uint32_t at) {
     if constexpr (D == 128) {
       asm volatile(
           "s_waitcnt vmcnt(12)\n\tds_read_b128 %0, %4 offset:%6\n\tds_read_b128 %1, %5 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %5 offset:%7\n\t"
           "s_waitcnt lgkmcnt(0)"
           : "=&v"(kw[0][0]), "=&v"(kw[0][1]), "=&v"(kw[1][0]), "=&v"(kw[1][1])
-          : "v"(at), "v"(at ^ 64), "i"(SLOT * 2 * kBytes), "i"(SLOT * 2 * kBytes + 2048)
+          : "v"(at), "v"(at ^ 64), "i"(0), "i"(2048)
           : "memory");
     } else {
       asm volatile("s_waitcnt vmcnt(6)\n\tds_read_b128 %0, %2 offset:%3\n\tds_read_b128 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
                    : "=&v"(kw[0][0]), "=&v"(kw[1][0])
-                   : "v"(at), "i"(SLOT * 2 * kBytes), "i"(SLOT * 2 * kBytes + 1024)
+                   : "v"(at), "i"(0), "i"(1024)
                    : "memory");
     }
   }
-  template <int SLOT>
   __device__ __forceinline__ void read_values(uint32_t at, int h) {
-    constexpr int V = SLOT * 2 * kBytes + kBytes;
+    constexpr int V = kBytes;
     if constexpr (D == 128) {
       const uint32_t a = at + 128 * (h & 1), b = at + 128 - 128 * (h & 1);
       u32x2 x[8];
@@ -533,24 +531,19 @@ __device__ __forceinline__ void short_item(const Q8AttnArgs &a, const Q8Layers &
     ask_keys(0, j), ask_values(0, j), ask_keys(1, j + turns), ask_values(1, j + turns);
     asm volatile("" : "+v"(ke), "+v"(ve));
     x.arrived();
-    auto meet = [&](auto slot) {
-      constexpr int I = decltype(slot)::value;
+    for (int slot = 0;; slot ^= 1) {
+      const int in_slot = slot * 2 * Keys<D>::kBytes;
       x.meet(a.c, t.P - j * kQ8Block, h,
              [&](Keys<D> &k) {
-               k.template read_keys<I>(k_at);
-               ask_keys(I, j + 2 * turns);
+               k.read_keys(k_at + in_slot);
+               ask_keys(slot, j + 2 * turns);
                return q8_scale(__builtin_amdgcn_readlane(ke, n));
              },
              [&](Keys<D> &k) {
-               k.template read_values<I>(v_at, h);
-               ask_values(I, j + 2 * turns);
+               k.read_values(v_at + in_slot, h);
+               ask_values(slot, j + 2 * turns);
                return q8_scale(__builtin_amdgcn_readlane(ve, n));
              });
-    };
-    for (;;) {
-      meet(std::integral_constant<int, 0>());
-      if (++n, (j += turns) >= end) break;
-      meet(std::integral_constant<int, 1>());
       if (++n, (j += turns) >= end) break;
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing comes to the slots any more
