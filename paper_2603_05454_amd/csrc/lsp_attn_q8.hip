@@ -484,7 +484,8 @@ struct Short {
   }
 };
 
-// LDS of a workgroup.  Short tiles: two blocks' keys and values of each wave, then what the waves join.  Tall ones: four blocks' keys [32][D] and two steps' values [D][64], bf16.
+// LDS of a workgroup.  Short tiles: two blocks' keys and values of each wave, then what the waves join.  Tall ones: 4 AHEAD blocks' keys [32][D] and 2 AHEAD
+// steps' values [64][D], bf16.
 template <int D, int WAVES>
 union Joined {
   struct {
@@ -1088,8 +1089,8 @@ bool has_tallest(int64_t entries, int D) { return D == 128 && entries > kTall; }
 size_t parts_bytes(int D) { return size_t(kSlots) * 32 * (D + 2) * sizeof(float); }
 
 // Two workgroups of four waves, or one of eight, stay on each compute unit.  Units of more entries than 128 (heads of 128) have a kernel of their own, of eight waves and 256
-// entries, so that every key that is made bf16 and laid out in LDS meets twice as many queries: 8 x 1024 rows on 5120 keys of 32 heads, 275 GFLOP, take 730 us
-// on a cool card (0.94 PFLOP/s; 1.2 is what a large library product reaches), 843 in tiles of 128.  Of it the laying out is 130, the exponentials are 60:
+// entries, so that every key that is made bf16 and laid out in LDS meets twice as many queries: 8 x 1024 rows on 5120 keys of 32 heads, 687 GFLOP, take 726 us
+// (0.95 PFLOP/s; 1.2 is what a large library product reaches), 843 in tiles of 128.  Of it the laying out is 110, the exponentials are 60:
 // they, the matrix instructions and the power that both draw are what bounds it.
 template <int D>
 int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_t st) {
