@@ -309,9 +309,16 @@ class AttnLayerTable:
         self.out = out
 
 
+def _need_table(table, kind):
+    """Tables of another kind have their lists of addresses in another order."""
+    if not isinstance(table, kind):
+        raise LspError(f"the call takes a {kind.__name__}, got {type(table).__name__}")
+
+
 def attn_step_layers(table: AttnLayerTable, prefix_len, suffix_len, scale=0.0, workspace=None):
     """lsp_attn_step_layers: the attention of every layer of `table` in one launch.
     Returns the list of per-layer outputs (table.out).  workspace as in attn_step."""
+    _need_table(table, AttnLayerTable)
     if _nat is not None:
         rc = _nat.attn_step_layers(table.desc, table.n, table.arrays, prefix_len, suffix_len, scale, workspace)
         if rc is not None:
@@ -823,6 +830,7 @@ def attn_key_weights(q, k_suf, k_cache, prefix_len, suffix_len, weights, decay=1
 
 def attn_key_weights_layers(table: AttnLayerTable, prefix_len, suffix_len, weights, decay=1.0, scale=0.0, workspace=None):
     """lsp_attn_key_weights for every layer of `table` in the launches of one: weights fp32 [layers,B,Hkv,C], as in attn_key_weights."""
+    _need_table(table, AttnLayerTable)
     d, a = table.desc, table.arrays
     _table_here(table.keep[0][0])
     if _nat is not None:
@@ -1011,6 +1019,7 @@ def kv_append_q8(layers: Q8LayerTable, commit_len, prefix_len):
     """lsp_kv_append_q8: the rows that commit(..., layers=None, C=...) has committed go into the caches of `layers`: rows [prefix_len[b] - commit_len[b],
     prefix_len[b]) receive suffix rows [0, commit_len[b]), quantised as they are written.  prefix_len: as commit leaves it, with the new
     rows.  A prompt: commit_len = prefix_len = its length."""
+    _need_table(layers, Q8LayerTable)
     _table_here(layers.keep[2][0])
     if _nat is not None:
         rc = _nat.kv_append_q8(layers.packed, layers.n, layers.arrays, commit_len, prefix_len)
@@ -1027,6 +1036,7 @@ def kv_append_q8(layers: Q8LayerTable, commit_len, prefix_len):
 def kv_read_q8(layers: Q8LayerTable, first_row, end_row, k_out, v_out):
     """lsp_kv_read_q8: rows first_row[b] to end_row[b] of the caches of `layers` as the values they stand for, in the rows from 0 on of k_out, v_out
     (lists of a tensor [B,R,Hkv,D], bf16 or fp32, per layer).  Returns (k_out, v_out)."""
+    _need_table(layers, Q8LayerTable)
     _table_here(layers.keep[2][0])
     if _nat is not None:
         rc = _nat.kv_read_q8(layers.packed, layers.n, layers.arrays, first_row, end_row, k_out, v_out)
@@ -1093,6 +1103,7 @@ def attn_step_q8(q, k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, prefix_len
 
 def attn_step_q8_layers(table: Q8LayerTable, prefix_len, suffix_len, scale=0.0, workspace=None):
     """lsp_attn_step_q8_layers: the attention of every layer of `table` (with q and out) in one launch.  Returns table.out."""
+    _need_table(table, Q8LayerTable)
     if table.out is None:
         raise LspError("attn_step_q8_layers: the table has no q and out")
     _table_here(table.keep[0][0])
