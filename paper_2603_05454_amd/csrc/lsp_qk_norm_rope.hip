@@ -132,7 +132,8 @@ template <typename T>
 void launch(const RopeArgs &a, int B, int D, bool interleaved, hipStream_t st) {
   // A workgroup has one row where its heads are work for all threads (8192 rows of 64 heads of 128: 41 us, with four rows 44; 1024 of 32 heads 5.6 and 7.4), or
   // where rows are few (512 of 10 heads: 4.0 and 4.7); else four, which share the angles' latency (8192 rows of 10 heads: 12.5 with one, 10.2).
-  const bool few = a.heads * (D * int64_t(sizeof(T)) / 32) >= kThreads || int64_t(B) * a.S <= 2048;
+  // (A launch has fewer than 2^32 threads in x: the most rows that the call takes are four to a workgroup in any case.)
+  const bool few = (a.heads * (D * int64_t(sizeof(T)) / 32) >= kThreads || int64_t(B) * a.S <= 2048) && int64_t(a.S) * kThreads < int64_t(1) << 32;
   const dim3 grid(unsigned(few ? a.S : (a.S + 3) / 4), unsigned(B));
   if (D == 64) {
     if (few) norm_rope_kernel<T, 64, 1><<<grid, kThreads, 0, st>>>(a, interleaved);
