@@ -43,3 +43,31 @@ def test_the_most_rows(lsp, dtype, S):
     # 21 roundings of 2^-24 and the rounding to the type, as in the call's own test
     tol = 21 * 2.0 ** -24 * size + (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24) * y.abs() + 1e-30
     assert ((want[0].cpu().double() - y).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("R", [16, 48, "D"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_four_rows_to_a_workgroup(lsp, dtype, D, R, interleaved, given):
+    """More than 2048 rows of few heads, every kind of pair, positions by length and given; lengths that leave one to four rows to the last workgroup."""
+    B, S, Hq, H = 5, 701, 5, 2
+    R = D if R == "D" else R
+    g = torch.Generator().manual_seed(D + R)
+    q, k = ((torch.randn((B, S, h, D), generator=g) * torch.exp(torch.randn((B, S, h, 1), generator=g))).to(dtype) for h in (Hq, H))
+    w = [torch.randn(D, generator=g) for _ in range(2)] if R != 48 else [None, None]
+    N, P = torch.tensor([701, 700, 3, 698, -1], dtype=torch.int32), torch.tensor([0, 4093, 100003, 17, 5], dtype=torch.int32)
+    pos = torch.randint(0, 1 << 30, (B, S), generator=g, dtype=torch.int32) if given else None
+    f = _freq(R)
+    want = eight_bits.norm_rope(q, k, f, *w, eps=1e-5, prefix_len=P, suffix_len=N, positions=pos, interleaved=interleaved)
+    dev = lambda t: None if t is None else t.cuda()      # noqa: E731
+    out = [torch.full_like(x, 7.0).cuda() for x in (q, k)]
+    lsp.qk_norm_rope(q.cuda(), k.cuda(), f.cuda(), dev(w[0]), dev(w[1]), 1e-5, P.cuda(), N.cuda(), dev(pos), interleaved, out)
+    for o, (y, size) in zip(out, want):
+        got = o.cpu().double()
+        for b in range(B):
+            n = max(int(N[b]), 0)
+            # as above
+            tol = 21 * 2.0 ** -24 * size[b, :n] + (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24) * y[b, :n].abs() + 1e-30
+            assert ((got[b, :n] - y[b, :n]).abs() <= tol).all() and (got[b, n:] == 7).all()
