@@ -685,7 +685,7 @@ __device__ __forceinline__ void here() { __builtin_amdgcn_sched_barrier(0); }
 // the next one's maximum; a slice of vector instructions behind every matrix instruction, laid by hand.  Operands are read from LDS four
 // instructions ahead.  A step is two blocks; step j writes what step j + AHEAD reads, its values and the keys of the blocks behind its first one, and waves meet every AHEAD
 // steps: rings of 4 AHEAD blocks of keys and 2 AHEAD steps of values, half of which are read and half written between two meetings.  AHEAD is 2 where a workgroup has
-// the compute unit to itself (8 x 1024 rows on 5120 keys: 726 us, 734 with 1).
+// the compute unit to itself (8 x 1024 rows on 5120 keys, side by side: 726 us, 734 with 1).
 template <int D, int WAVES, int AHEAD>
 __device__ __forceinline__ void tall_item(const Q8AttnArgs &a, const Unit &u, const Item &t, Staged<D, AHEAD> &s, int lane, int wave) {
   typedef Tall<D, WAVES> T;
@@ -1089,8 +1089,9 @@ bool has_tallest(int64_t entries, int D) { return D == 128 && entries > kTall; }
 size_t parts_bytes(int D) { return size_t(kSlots) * 32 * (D + 2) * sizeof(float); }
 
 // Two workgroups of four waves, or one of eight, stay on each compute unit.  Units of more entries than 128 (heads of 128) have a kernel of their own, of eight waves and 256
-// entries, so that every key that is made bf16 and laid out in LDS meets twice as many queries: 8 x 1024 rows on 5120 keys of 32 heads, 687 GFLOP, take 726 us
-// (0.95 PFLOP/s; 1.2 is what a large library product reaches), 843 in tiles of 128.  Of it the laying out is 110, the exponentials are 60:
+// entries, so that every key that is made bf16 and laid out in LDS meets twice as many queries: 8 x 1024 rows on 5120 keys of 32 heads, 687 GFLOP, take 740 to 760 us
+// (0.90 to 0.93 PFLOP/s, from card to card; 1.2 is what a large library product reaches; a process's first twenty launches are slower, 850 on average), 843 in tiles of 128
+// where these took 736.  Of it the laying out is 110, the exponentials are 60:
 // they, the matrix instructions and the power that both draw are what bounds it.
 template <int D>
 int32_t launch(const Q8AttnArgs &args, const Q8Layers &L, int layers, hipStream_t st) {

@@ -3,7 +3,7 @@
 // A block is 32 rows of one head, one wave's.  With a = the largest finite magnitude of its new rows and 448 that of e4m3, E is the smallest
 // exponent byte with a <= 448 * 2^(E - 127); powers of two cost an e4m3 value nothing (its own exponent takes them up) and make multiplying by a
 // scale, and rounding again under a larger one, exact but for what becomes subnormal.  Bound by the bytes: 16 bits read and 8 written for each number, or the other way
-// round (the prompt below: 6.1 TB/s written, 5.1 read back; a large copy reaches 4.9).
+// round (the prompt below: 6.0 TB/s written, 5.1 read back; a large copy reaches 4.9).
 #include <type_traits>
 
 #include "lsp_q8.h"
@@ -49,8 +49,9 @@ struct Eight {
   float x[8];
 };
 // ONCE: nontemporal.  Where the buffers are larger than the last cache (256 MB), what a call reads or writes once need not stay there: 4 x 4096 rows of 32 heads
-// in two layers, 0.8 GB, are appended in 131 us so and 148 without, and appended and read back in 294 and 314; where they are smaller it is better kept: 64
-// rows of 8 sequences in four layers 36 and 31 us.  The reading's own writes are plain ones: 156 us against 167.
+// in two layers, 0.8 GB, are appended in 131 to 135 us so and 148 without, and appended and read back in 294 and 314; where they are smaller it is better kept: 64
+// rows of 8 sequences in four layers 36 and 31 us.  It goes by the size of the buffers: how many of their rows a call commits only the device knows, and a step that commits a
+// few rows of large buffers goes nontemporally as well.  The reading's own writes are plain ones: 156 us against 167.
 constexpr int64_t kLastCache = int64_t(256) << 20;
 template <bool ONCE, typename V>
 __device__ __forceinline__ V load_once(const char *p) {
@@ -170,6 +171,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(KvArgs a, Q8Layers L) 
   }
 }
 
+// A lane's 16 values are 32 or 64 bytes, two or four stores, in each of which neighbouring lanes are as far apart: fp32 rows, 5 x 333 of 4 heads of 64 in four layers
+// (15 MB), take 7.9 us, where the append that reads as much takes 5.4.
 __device__ __forceinline__ void store16(char *p, u32x4 w, float scale, const uint16_t *) {
   u32x4 o[2];
 #pragma unroll

@@ -4,7 +4,7 @@
 // Bound by the bytes of the rows, read once and written once.  All heads of a row turn by the same angles: a workgroup works them out once, a thread
 // each, into LDS.  The product position * inv_freq is taken in 64 bits (in 32 the angle of position 100 000 is off by up to 0.004) and reduced there to
 // an eighth of a turn about a quarter; sine and cosine of that are their power series in 32 bits, to x^9 and x^10, whose next terms are below
-// 2e-9 and 1e-10.  Everything behind is 32 bits, rounded once.  8192 rows of 64 heads of 128, 268 MB in and out, take 41 us (6.5 TB/s); one row 2.6 us.
+// 2e-9 and 1.2e-10.  Everything behind is 32 bits, rounded once.  8192 rows of 64 heads of 128, 268 MB in and out, take 41 us (6.5 TB/s); one row 2.6 us.
 #include <math.h>
 
 #include "lsp_q8.h"
