@@ -591,8 +591,9 @@ int32_t lsp_kv_read_q8(const lsp_attn_desc *desc, int32_t num_layers, const void
  * S * Hq / Hkv > 128), for this call alone until
  * it has run; with it the keys of few rows are divided between workgroups, without (NULL, or fewer bytes) a tile's
  * keys are one workgroup's.  Parts are added in order: the same operands give the same bits, with a workspace of one kind.
- * Where many rows meet the same keys (S * Hq / Hkv from some hundred on) keys made 16 bits once are quicker: lsp_kv_read_q8 into buffers of the caller's and
- * lsp_attn_step over these take 51 us for 4 x 497 rows of 28/4 heads on 1021 keys, this call 64; 733 and 755 for 8 x 1024 rows of 32/32 heads on 4096.
+ * Where many rows of grouped heads meet the same keys (S * Hq / Hkv from some hundred on) keys made 16 bits once are quicker: lsp_kv_read_q8 into buffers of the caller's and
+ * lsp_attn_step over these take 51 us for 4 x 497 rows of 28/4 heads on 1021 keys, this call 64 (8 x 1024 rows
+ * of 32/32 heads on 4096: alike, 733 and 730 to 755).
  * Limits: those of lsp_attn_step; C, S <= 2^30, B * Hkv < 2^23, B * S * Hq and S * Hq / Hkv < 2^30; a row stride of K and V of
  * at least D.
  */

@@ -1085,8 +1085,8 @@ def _attn_q8(d, n, arrays, prefix_len, suffix_len, scale, workspace, device):
 
 def attn_step_q8(q, k_suf, v_suf, k_cache, v_cache, k_scale, v_scale, prefix_len, suffix_len, scale=0.0, out=None, workspace=None):
     """lsp_attn_step_q8: attn_step over a cache in 8 bits (bf16 queries and suffix): k_cache/v_cache torch.float8_e4m3fn [B,C,Hkv,D], k_scale/v_scale
-    uint8 [B,Hkv,ceil(C/32)].  Returns out [B,S,Hq,D]; rows >= suffix_len[b] are not written.  Where many rows meet the same keys, kv_read_q8 and
-    attn_step are quicker (include/lsp.h has figures).
+    uint8 [B,Hkv,ceil(C/32)].  Returns out [B,S,Hq,D]; rows >= suffix_len[b] are not written.  Where many rows of grouped heads meet the same keys,
+    kv_read_q8 and attn_step are quicker (include/lsp.h has figures).
     workspace: contiguous device memory of attn_q8_workspace_bytes(...) bytes and any content, aligned to 16 bytes, for this call alone
     until it has run; without one that will do, a call that wants one takes its own from torch's allocator."""
     if out is None:

@@ -1089,8 +1089,8 @@ bool has_tallest(int64_t entries, int D) { return D == 128 && entries > kTall; }
 size_t parts_bytes(int D) { return size_t(kSlots) * 32 * (D + 2) * sizeof(float); }
 
 // Two workgroups of four waves, or one of eight, stay on each compute unit.  Units of more entries than 128 (heads of 128) have a kernel of their own, of eight waves and 256
-// entries, so that every key that is made bf16 and laid out in LDS meets twice as many queries: 8 x 1024 rows on 5120 keys of 32 heads, 687 GFLOP, take 740 to 760 us
-// (0.90 to 0.93 PFLOP/s, from card to card; 1.2 is what a large library product reaches; a process's first twenty launches are slower, 850 on average), 843 in tiles of 128
+// entries, so that every key that is made bf16 and laid out in LDS meets twice as many queries: 8 x 1024 rows on 5120 keys of 32 heads, 687 GFLOP, take 730 to 760 us
+// (0.90 to 0.94 PFLOP/s, from card to card; 1.2 is what a large library product reaches; a process's first twenty launches are slower, 850 on average), 843 in tiles of 128
 // where these took 736.  Of it the laying out is 110, the exponentials are 60:
 // they, the matrix instructions and the power that both draw are what bounds it.
 template <int D>
